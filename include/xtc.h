@@ -27,7 +27,8 @@
  *   synchronise.  Faults during execution surface at the caller's next
  *   synchronisation on that stream, not in the return value.
  * - The return value is the only error channel.
- * - Element offsets are 32-bit inside the kernels: every operand's span
+ * - Element offsets of the matmul and conv2d entry points are 32-bit inside
+ *   the kernels: every operand's span
  *   (bytes from its first to its last addressed element) must be at most
  *   0x7FFFFFD0 bytes (2^31 - 48), else XTC_ERR_TOO_LARGE.  Elements
  *   outside an operand (ragged edges, zero padding) are read through a
@@ -44,8 +45,10 @@ extern "C" {
 #endif
 
 /* Element types.  XTC_BF16: inputs are bf16 bit patterns (uint16), products
- * are exact in fp32, accumulation and output are fp32. */
-typedef enum { XTC_F32 = 0, XTC_BF16 = 1 } xtc_dtype;
+ * are exact in fp32, accumulation and output are fp32.  XTC_FP8: OCP e4m3
+ * (4 exponent and 3 mantissa bits, no infinities, largest value 448), only
+ * where an entry point names it. */
+typedef enum { XTC_F32 = 0, XTC_BF16 = 1, XTC_FP8 = 2 } xtc_dtype;
 
 typedef enum { XTC_OP_MATMUL = 0, XTC_OP_CONV2D = 1 } xtc_op;
 
@@ -53,13 +56,15 @@ typedef enum {
     XTC_OK = 0,
     XTC_ERR_NULL_POINTER = 1,         /* a tensor or output pointer is NULL   */
     XTC_ERR_BAD_SHAPE = 2,            /* negative or inconsistent extents     */
-    XTC_ERR_BAD_LEADING_DIM = 3,      /* lda < K, ldb < N or ldc < N          */
+    XTC_ERR_BAD_LEADING_DIM = 3,      /* lda < K, ldb < N or ldc < N (or      */
+                                      /* matrices of a family that overlap)   */
     XTC_ERR_BAD_DTYPE = 4,            /* unknown dtype, or not supported here */
     XTC_ERR_BAD_SCHEDULE = 5,         /* illegal field values / combination   */
     XTC_ERR_UNSUPPORTED_SCHEDULE = 6, /* legal but not among compiled ones    */
     XTC_ERR_TOO_LARGE = 7,            /* an operand span above 0x7FFFFFD0     */
                                       /* bytes, or a conv stride/pad/extent   */
-                                      /* above 2^30                           */
+                                      /* above 2^30; for the operators on     */
+                                      /* blocks, groups and norms see there   */
     XTC_ERR_HIP = 8,                  /* a HIP call failed (see below)        */
     XTC_ERR_MISALIGNED = 9            /* a tensor pointer is not aligned to   */
                                       /* its element size                     */
@@ -270,6 +275,153 @@ xtc_status xtc_conv2d_nchw_relu(int64_t N, int64_t C, int64_t H, int64_t W,
                                 int64_t pad_h, int64_t pad_w,
                                 const void *X, const void *Wt, float *Y,
                                 xtc_dtype dtype, const xtc_sched *sched, void *stream);
+
+/*
+ * Operators around the products of a transformer block: the norm in front of
+ * them, products of 8-bit operands whose values share scales, and products of
+ * rows that belong to different matrices (the experts of a mixture).
+ *
+ * Limits of these entry points: extents at most 0x7FFFFF00, row strides at most
+ * 2^30 elements, matrices of a family at most 2^50 elements apart, and a launch
+ * of fewer than 2^24 workgroups, else XTC_ERR_TOO_LARGE.  Offsets are 64-bit:
+ * operands may exceed 2^31 bytes.  Every row stride is at least the row's
+ * length, else XTC_ERR_BAD_LEADING_DIM.  Rows may start at any element boundary;
+ * 16-byte aligned rows of a multiple of 16 bytes run the faster kernels.
+ *
+ * 8-bit operands.  A matrix of e4m3 values has fp32 scales S for blocks of 128
+ * consecutive values of a row: value (i, j) stands for Q[i][j] * S[i][j/128], or
+ * S[i/128][j/128] where 128 rows share scales; the last blocks may be cut.
+ */
+
+/*
+ * xtc_rmsnorm -- root-mean-square norm of each row of X + R:
+ *   h = X + R (fp32), rstd = 1 / sqrt(sum_j h_j^2 / D + eps),
+ *   Y_j = W_j * h_j * rstd, rounded once.
+ *
+ *  T, D       rows and columns, >= 0; either 0 is a no-op.
+ *  X, R       device, dtype (XTC_F32 or XTC_BF16), row strides ldx, ldr.  R NULL:
+ *             nothing is added.
+ *  W          device, D values of w_dtype: dtype or XTC_F32.
+ *  eps        >= 0, else XTC_ERR_BAD_SHAPE.
+ *  Y          device, out_dtype: dtype, or XTC_FP8 with the scales S (fp32,
+ *             T x ceil(D/128), row stride lds): S = max(amax / 448, 2^-126), amax
+ *             the largest finite magnitude of the block's 128 unrounded outputs,
+ *             each then divided by S and rounded to nearest even; an output
+ *             that is not finite becomes e4m3's NaN.
+ *  H          device, dtype: h rounded once (the residual of the next norm), or
+ *             NULL.  Needs R.
+ *  rstd       device, T fp32 values for the gradient, or NULL.
+ * Errors: XTC_ERR_BAD_DTYPE, XTC_ERR_BAD_SHAPE, XTC_ERR_TOO_LARGE,
+ * XTC_ERR_BAD_LEADING_DIM, XTC_ERR_NULL_POINTER, XTC_ERR_MISALIGNED, XTC_ERR_HIP.
+ */
+xtc_status xtc_rmsnorm(int64_t T, int64_t D, const void *X, int64_t ldx,
+                       const void *R, int64_t ldr, const void *W, float eps,
+                       void *Y, int64_t ldy, float *S, int64_t lds,
+                       void *H, int64_t ldh, float *rstd,
+                       xtc_dtype dtype, xtc_dtype w_dtype, xtc_dtype out_dtype, void *stream);
+
+/*
+ * xtc_rmsnorm_backward -- the norm's gradient.  X is what was normalised (H
+ * where a residual was added) and rstd what xtc_rmsnorm kept; with
+ * xh = X * rstd and g = DY * W,
+ *   DX = rstd * (g - xh * sum_j(g_j xh_j) / D) + DR,  DW_j = sum_t DY_tj xh_tj.
+ * DX is the gradient of both summands of X + R.
+ *
+ *  DY, X, DX  device, dtype, row strides lddy, ldx, lddx.
+ *  DR         gradient that reaches the sum from elsewhere (row stride lddr), or
+ *             NULL.
+ *  DW         device, D fp32 values (overwritten; zeros when T == 0).
+ *  workspace  device, workspace_bytes >= xtc_rmsnorm_backward_workspace(T, D),
+ *             16-byte aligned, written by the call; too small is
+ *             XTC_ERR_BAD_SHAPE.
+ * Sums are fp32 in an order that depends on T and D alone.
+ * Errors as for xtc_rmsnorm.
+ */
+xtc_status xtc_rmsnorm_backward(int64_t T, int64_t D, const void *DY, int64_t lddy,
+                                const void *X, int64_t ldx, const void *W, const float *rstd,
+                                const void *DR, int64_t lddr, void *DX, int64_t lddx, float *DW,
+                                void *workspace, int64_t workspace_bytes,
+                                xtc_dtype dtype, xtc_dtype w_dtype, void *stream);
+
+/* Bytes of workspace for T rows of D columns; -1 for extents outside the limits.  Pure host function. */
+int64_t xtc_rmsnorm_backward_workspace(int64_t T, int64_t D);
+
+/*
+ * xtc_quantize_fp8 -- X [M, K] (dtype, row stride ldx) as e4m3 values Q (row
+ * stride ldq) and scales S (row stride lds): one for each block_rows x 128
+ * values, block_rows 1 (activations) or 128 (weights), else XTC_ERR_BAD_SHAPE.
+ * S = max(amax / 448, 2^-126) over the block's finite magnitudes, Q = X / S
+ * rounded to nearest even; what is not finite becomes NaN.  M or K 0: no-op.
+ * Errors as for xtc_rmsnorm.
+ */
+xtc_status xtc_quantize_fp8(int64_t M, int64_t K, const void *X, int64_t ldx, int64_t block_rows,
+                            void *Q, int64_t ldq, float *S, int64_t lds,
+                            xtc_dtype dtype, void *stream);
+
+/*
+ * xtc_matmul_fp8 -- C = A * B^T of block-scaled e4m3 operands:
+ *   C[m][n] = sum_b SA[m][b] SB[n/128][b] sum_{k in block b} A[m][k] B[n][k],
+ * the inner sums and the outer one in fp32, rounded once into C.
+ *
+ *  A   e4m3 M x K, row stride lda; SA its scales, one per row and 128 k, row
+ *      stride ldsa.
+ *  B   e4m3 N x K (a row holds the weights of one output), row stride ldb; SB
+ *      its scales, one per 128 rows and 128 k, row stride ldsb.
+ *  C   out_dtype XTC_F32 or XTC_BF16, M x N, row stride ldc.
+ *  relu  nonzero: C holds v < 0 ? 0 : v (a NaN stays NaN).
+ * M or N 0 is a no-op; K 0 gives zeros.  Errors as for xtc_rmsnorm.
+ */
+xtc_status xtc_matmul_fp8(int64_t M, int64_t N, int64_t K,
+                          const void *A, int64_t lda, const float *SA, int64_t ldsa,
+                          const void *B, int64_t ldb, const float *SB, int64_t ldsb,
+                          void *C, int64_t ldc, xtc_dtype out_dtype, int32_t relu, void *stream);
+
+/*
+ * xtc_matmul_grouped -- products of the rows of A with the matrix of their
+ * group: C[i] = A[i] * B[g] for the rows i of group g.
+ *
+ *  G, T   groups (>= 1, else XTC_ERR_BAD_SHAPE) and rows of A.
+ *  ends   device, G values: group g holds the rows from ends[g-1] (0 for the
+ *         first) to ends[g]; they ascend to at most T.  A value below an earlier
+ *         one makes an empty group, one above T counts as T.  Rows from
+ *         ends[G-1] to T belong to no group: C is zero there.
+ *  A      bf16 (dtype XTC_BF16, else XTC_ERR_BAD_DTYPE) T x K, row stride lda.
+ *  B      G matrices stride_b elements apart, each K x N with row stride ldb,
+ *         or N x K where transpose_b is nonzero (the gradient of A is the
+ *         product of C's gradient with the same B and the other transpose_b).
+ *  C      out_dtype XTC_F32 or XTC_BF16, T x N, row stride ldc; fp32 sums,
+ *         rounded once.
+ *  relu   as for xtc_matmul_fp8.
+ * The sizes of the groups stay on the device.  Errors as for xtc_rmsnorm.
+ */
+xtc_status xtc_matmul_grouped(int64_t G, int64_t T, int64_t N, int64_t K,
+                              const void *A, int64_t lda,
+                              const void *B, int64_t ldb, int64_t stride_b, int32_t transpose_b,
+                              const int32_t *ends, void *C, int64_t ldc,
+                              xtc_dtype dtype, xtc_dtype out_dtype, int32_t relu, void *stream);
+
+/*
+ * xtc_matmul_grouped_wgrad -- the gradient of B: DB[g] = A_g^T * DY_g over the
+ * rows of group g (zeros for an empty one).  A is T x K, DY T x N, both bf16;
+ * DB holds G matrices K x N of out_dtype (XTC_F32 or XTC_BF16) stride_db
+ * elements apart, row stride lddb.  ends and errors as for xtc_matmul_grouped.
+ */
+xtc_status xtc_matmul_grouped_wgrad(int64_t G, int64_t T, int64_t N, int64_t K,
+                                    const void *A, int64_t lda, const void *DY, int64_t lddy,
+                                    const int32_t *ends, void *DB, int64_t lddb, int64_t stride_db,
+                                    xtc_dtype dtype, xtc_dtype out_dtype, void *stream);
+
+/*
+ * xtc_matmul_grouped_fp8 -- xtc_matmul_grouped of block-scaled e4m3 operands
+ * (see xtc_matmul_fp8): B holds G matrices N x K stride_b elements apart, SB
+ * their scales stride_sb values apart.
+ */
+xtc_status xtc_matmul_grouped_fp8(int64_t G, int64_t T, int64_t N, int64_t K,
+                                  const void *A, int64_t lda, const float *SA, int64_t ldsa,
+                                  const void *B, int64_t ldb, int64_t stride_b,
+                                  const float *SB, int64_t ldsb, int64_t stride_sb,
+                                  const int32_t *ends, void *C, int64_t ldc,
+                                  xtc_dtype out_dtype, int32_t relu, void *stream);
 
 /*
  * xtc_default_schedule -- the schedule used when sched == NULL, chosen from

@@ -3,13 +3,24 @@
 // schedules and the launch on the caller's stream.
 #include <string.h>
 
+#include "operators.h"
 #include "xtc_internal.h"
+
+namespace {
+thread_local int32_t g_last_hip_error = 0;
+}
+
+namespace xtc {
+xtc_status hip_status(hipError_t e) {
+    if (e == hipSuccess) return XTC_OK;
+    g_last_hip_error = (int32_t)e;
+    return XTC_ERR_HIP;
+}
+}  // namespace xtc
 
 namespace {
 
 using namespace xtc;
-
-thread_local int32_t g_last_hip_error = 0;
 
 // Largest operand span in bytes.  Kernels use 32-bit buffer offsets, and
 // an element outside an operand is read through the offset kOOB
@@ -129,12 +140,6 @@ const ConvInstance *find_conv(xtc_dtype dt, const xtc_sched &s) {
     for (int i = 0; i < n; ++i)
         if (same_instance(tab[i].sched, s)) return &tab[i];
     return nullptr;
-}
-
-xtc_status hip_status(hipError_t e) {
-    if (e == hipSuccess) return XTC_OK;
-    g_last_hip_error = (int32_t)e;
-    return XTC_ERR_HIP;
 }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -362,7 +367,7 @@ const char *xtc_status_str(xtc_status s) {
         case XTC_ERR_BAD_DTYPE: return "bad or unsupported dtype";
         case XTC_ERR_BAD_SCHEDULE: return "illegal schedule";
         case XTC_ERR_UNSUPPORTED_SCHEDULE: return "schedule not among the compiled instances";
-        case XTC_ERR_TOO_LARGE: return "operand too large for 32-bit offsets";
+        case XTC_ERR_TOO_LARGE: return "operand too large";
         case XTC_ERR_HIP: return "HIP error";
         case XTC_ERR_MISALIGNED: return "pointer not aligned to its element size";
     }
