@@ -1,87 +1,10 @@
 // Products with the rows of A in groups, each with its own B, and the 8-bit
-// products with block scales (of one group or several).
-//
-// The matrix-core instructions take B's side (the columns of C) as their first
-// operand and A's rows as their second, so that a lane's accumulators are four
-// consecutive columns of one row of C, and an e4m3 row's scale is one value per
-// lane: sum_k over a block of 128 is computed from zero, then added to the
-// fp32 accumulators times the product of the two scales.
-#include "groups.h"
-#include "mfma_fp8.h"
-#include "operators.h"
+// products with block scales (of one group or several): the choice of the
+// kernel, and the kernel for operands of any alignment.
+#include "grouped.h"
 
 namespace xtc {
 namespace {
-
-// A tile of one member of the family.
-struct Tile {
-    const unsigned char *A, *B;   // row (or k) 0 of the tile's operands
-    int64_t lda, ldb;             // bytes
-    int m, n, k;                  // extents from the tile's corner (k: the whole reduction)
-    const float *SA, *SB;
-    unsigned char *C;
-};
-
-enum Kind { kFp8, kBf16N, kBf16T, kWgrad };   // B [N, K] e4m3; bf16 [K, N]; bf16 [N, K]; both [T, .]
-
-template <Kind KIND, int BM, int BN>
-__device__ __forceinline__ bool find_tile(const GroupedArgs &p, Tile &t) {
-    constexpr int E = KIND == kFp8 ? 1 : 2;
-    const int tiles_n = (p.N + BN - 1) / BN;
-    const int out = p.out_bf16 ? 2 : 4;
-    const unsigned char *A = static_cast<const unsigned char *>(p.A), *B = static_cast<const unsigned char *>(p.B);
-    unsigned char *C = static_cast<unsigned char *>(p.C);
-    t.lda = p.lda * E;
-    t.ldb = p.ldb * E;
-    t.SA = t.SB = nullptr;
-    if constexpr (KIND == kWgrad) {
-        // rows of C: columns of A
-        const int tiles_m = (p.K + BM - 1) / BM, per = tiles_m * tiles_n;
-        const int g = (int)(blockIdx.x / per), r = (int)(blockIdx.x - (unsigned)g * per);
-        const int m0 = r / tiles_n * BM, n0 = r % tiles_n * BN;
-        const RowTile w = find_group(p.ends, (int)p.T, g);
-        t.A = A + w.row0 * t.lda + (int64_t)m0 * E;
-        t.B = B + w.row0 * t.ldb + (int64_t)n0 * E;
-        t.m = p.K - m0;
-        t.n = p.N - n0;
-        t.k = w.rows;
-        t.C = C + (g * p.stride_c + m0 * p.ldc + n0) * out;
-        return true;
-    }
-    const int im = (int)(blockIdx.x / tiles_n), n0 = (int)(blockIdx.x - (unsigned)im * tiles_n) * BN;
-    RowTile w;
-    if (p.ends) {
-        w = find_row_tile<BM>(p.ends, p.G, (int)p.T, im);
-    } else {
-        const int row0 = im * BM;
-        w = RowTile{0, row0, p.T - row0 < BM ? (int)(p.T - row0) : BM};
-    }
-    if (w.group < 0) return false;
-    const bool none = w.group >= p.G;
-    t.A = A + w.row0 * t.lda;
-    t.B = none ? B : B + w.group * p.stride_b * E + (KIND == kBf16N ? (int64_t)n0 * E : n0 * t.ldb);
-    t.m = w.rows;
-    t.n = p.N - n0;
-    t.k = none ? 0 : p.K;
-    if constexpr (KIND == kFp8) {
-        t.SA = p.SA + w.row0 * p.ldsa;
-        t.SB = none ? p.SB : p.SB + w.group * p.stride_sb + n0 / kScaleBlock * p.ldsb;
-    }
-    t.C = C + (w.row0 * p.ldc + n0) * out;
-    return true;
-}
-
-// Writes v[0 .. 3], the columns n .. n + 3 of a row of C at `c`.
-__device__ __forceinline__ void write4(const GroupedArgs &p, unsigned char *c, int n, int left, float (&v)[4]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (p.relu && v[i] < 0.f) v[i] = 0.f;
-        if (i < left) {
-            if (p.out_bf16) reinterpret_cast<__bf16 *>(c)[n + i] = (__bf16)v[i];
-            else reinterpret_cast<float *>(c)[n + i] = v[i];
-        }
-    }
-}
 
 // Rows, columns and strides of any alignment: operands through registers into
 // one padded LDS buffer, k innermost.  64 x 64 tiles of four 32 x 32 waves.
@@ -196,25 +119,27 @@ __global__ void __launch_bounds__(256) grouped_any_kernel(GroupedArgs p) {
         }
 }
 
-int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
-// Tiles of bm rows that a launch has to hold for whatever groups the GPU finds.
-int64_t row_tiles(const GroupedArgs &a, int bm) { return a.ends ? a.T / bm + a.G + 1 : cdiv(a.T, bm); }
+}  // namespace
 
 template <Kind KIND>
 xtc_status launch_any(const GroupedArgs &a, hipStream_t s) {
-    const int64_t tiles = KIND == kWgrad ? cdiv(a.K, 64) * a.G : row_tiles(a, 64);
-    if (tiles * cdiv(a.N, 64) >= kMostGroups) return XTC_ERR_TOO_LARGE;
-    grouped_any_kernel<KIND><<<(unsigned)(tiles * cdiv(a.N, 64)), 256, 0, s>>>(a);
+    const int64_t tiles = tile_count<KIND>(a, 64, 64);
+    if (tiles >= kMostGroups) return XTC_ERR_TOO_LARGE;
+    grouped_any_kernel<KIND><<<(unsigned)tiles, 256, 0, s>>>(a);
     return hip_status(hipGetLastError());
 }
 
+namespace {
+template <Kind KIND>
+xtc_status launch(const GroupedArgs &a, hipStream_t s) {
+    return tile_takes<KIND>(a) ? launch_tile<KIND>(a, s) : launch_any<KIND>(a, s);
+}
 }  // namespace
 
-xtc_status launch_grouped_fp8(const GroupedArgs &a, hipStream_t s) { return launch_any<kFp8>(a, s); }
+xtc_status launch_grouped_fp8(const GroupedArgs &a, hipStream_t s) { return launch<kFp8>(a, s); }
 xtc_status launch_grouped_bf16(const GroupedArgs &a, bool b_rows_n, hipStream_t s) {
-    return b_rows_n ? launch_any<kBf16T>(a, s) : launch_any<kBf16N>(a, s);
+    return b_rows_n ? launch<kBf16T>(a, s) : launch<kBf16N>(a, s);
 }
-xtc_status launch_grouped_wgrad(const GroupedArgs &a, hipStream_t s) { return launch_any<kWgrad>(a, s); }
+xtc_status launch_grouped_wgrad(const GroupedArgs &a, hipStream_t s) { return launch<kWgrad>(a, s); }
 
 }  // namespace xtc

@@ -34,36 +34,63 @@ __device__ __forceinline__ int scan_sum(int v, int lane) {
     return v;
 }
 
-// Tile `index` of the groups' rows cut into tiles of BM, groups in order.
-// Every lane of a wave calls it with the same index: 64 groups a step.  At
-// most T / BM + G + 1 tiles exist.
+// The groups' rows cut into tiles of BM, groups in order: how many tiles there
+// are (at most T / BM + G + 1) and which rows tile `index` holds.  Every lane of
+// a wave calls it with the same arguments: 64 groups a step.
 template <int BM>
-__device__ __forceinline__ RowTile find_row_tile(const int32_t *ends, int G, int T, int index) {
-    const int lane = threadIdx.x & 63;
-    int before = 0, prev = 0;       // tiles and rows of the groups of earlier steps
-    for (int g0 = 0; g0 <= G; g0 += 64) {
-        const int g = g0 + lane;
+struct RowTiles {
+    const int32_t *ends;
+    int G, T;
+    int total;
+
+    struct Step {
+        int start, end, tiles, upto;    // of this lane's group; tiles of the step's groups up to it
+    };
+    // Groups g0 .. g0 + 63, the rows before them ending at prev.
+    __device__ __forceinline__ Step step(int g0, int prev) const {
+        const int lane = threadIdx.x & 63, g = g0 + lane;
+        Step s;
         int end = g < G ? ends[g] : T;
         end = end > T ? T : end;
-        end = scan_max(end > prev ? end : prev, lane);
-        int start = __shfl_up(end, 1, 64);
-        if (lane == 0) start = prev;
-        const int tiles = g <= G ? (end - start + BM - 1) / BM : 0;
-        const int upto = scan_sum(tiles, lane);
-        const bool mine = index >= before + upto - tiles && index < before + upto;
-        const unsigned long long who = __ballot(mine);
-        if (who) {
-            const int l = __ffsll((long long)who) - 1;
-            const int s = __shfl(start, l, 64), e = __shfl(end, l, 64), u = __shfl(upto - tiles, l, 64);
-            const int row0 = s + (index - before - u) * BM;
-            return RowTile{__builtin_amdgcn_readfirstlane(g0 + l), __builtin_amdgcn_readfirstlane(row0),
-                           __builtin_amdgcn_readfirstlane(e - row0 < BM ? e - row0 : BM)};
-        }
-        before += __shfl(upto, 63, 64);
-        prev = __shfl(end, 63, 64);
+        s.end = scan_max(end > prev ? end : prev, lane);
+        s.start = __shfl_up(s.end, 1, 64);
+        if (lane == 0) s.start = prev;
+        s.tiles = g <= G ? (s.end - s.start + BM - 1) / BM : 0;
+        s.upto = scan_sum(s.tiles, lane);
+        return s;
     }
-    return RowTile{-1, 0, 0};
-}
+    Step first;
+
+    __device__ __forceinline__ RowTiles(const int32_t *ends_, int G_, int T_) : ends(ends_), G(G_), T(T_) {
+        first = step(0, 0);
+        total = __shfl(first.upto, 63, 64);
+        int prev = __shfl(first.end, 63, 64);
+        for (int g0 = 64; g0 <= G; g0 += 64) {
+            const Step s = step(g0, prev);
+            total += __shfl(s.upto, 63, 64);
+            prev = __shfl(s.end, 63, 64);
+        }
+        total = __builtin_amdgcn_readfirstlane(total);
+    }
+
+    __device__ __forceinline__ RowTile find(int index) const {
+        Step s = first;
+        int before = 0;
+        for (int g0 = 0;; g0 += 64) {
+            const unsigned long long who = __ballot(index >= before + s.upto - s.tiles && index < before + s.upto);
+            if (who) {
+                const int l = __ffsll((long long)who) - 1;
+                const int row0 = __shfl(s.start, l, 64) + (index - before - __shfl(s.upto - s.tiles, l, 64)) * BM;
+                const int left = __shfl(s.end, l, 64) - row0;
+                return RowTile{__builtin_amdgcn_readfirstlane(g0 + l), __builtin_amdgcn_readfirstlane(row0),
+                               __builtin_amdgcn_readfirstlane(left < BM ? left : BM)};
+            }
+            if (g0 + 64 > G) return RowTile{-1, 0, 0};
+            before += __shfl(s.upto, 63, 64);
+            s = step(g0 + 64, __shfl(s.end, 63, 64));
+        }
+    }
+};
 
 // The rows of group g (g < G).
 __device__ __forceinline__ RowTile find_group(const int32_t *ends, int T, int g) {
