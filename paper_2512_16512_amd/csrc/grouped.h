@@ -28,67 +28,88 @@ constexpr int kBand = 4;
 
 enum Kind { kFp8, kBf16N, kBf16T, kWgrad };   // B [N, K] e4m3; bf16 [K, N]; bf16 [N, K]; both [T, .]
 
-template <Kind KIND, int BM, int BN>
-__device__ __forceinline__ bool find_tile(const GroupedArgs &p, Tile &t) {
+// Where a tile lies: what its operands' addresses follow from.
+struct Place {
+    int group;          // p.G: rows past every group, without a B
+    int row0, rows;     // of the group's rows: the tile's, or for a weights' gradient all of them
+    int m0, n0;         // corner in C (m0: weights' gradient only)
+};
+
+template <Kind KIND>
+__device__ __forceinline__ Tile make_tile(const GroupedArgs &p, const Place &w) {
     constexpr int E = KIND == kFp8 ? 1 : 2;
-    const int tiles_n = (p.N + BN - 1) / BN;
     const int out = p.out_bf16 ? 2 : 4;
+    const bool none = w.group >= p.G;
     const unsigned char *A = static_cast<const unsigned char *>(p.A), *B = static_cast<const unsigned char *>(p.B);
-    unsigned char *C = static_cast<unsigned char *>(p.C);
+    Tile t;
     t.lda = p.lda * E;
     t.ldb = p.ldb * E;
     t.SA = t.SB = nullptr;
-    if constexpr (KIND == kWgrad) {
-        // rows of C: columns of A
-        const int tiles_m = (p.K + BM - 1) / BM, per = tiles_m * tiles_n;
-        const int g = (int)(blockIdx.x / per), r = (int)(blockIdx.x - (unsigned)g * per);
-        const int m0 = r / tiles_n * BM, n0 = r % tiles_n * BN;
-        const RowTile w = find_group(p.ends, (int)p.T, g);
-        t.A = A + w.row0 * t.lda + (int64_t)m0 * E;
-        t.B = B + w.row0 * t.ldb + (int64_t)n0 * E;
-        t.m = p.K - m0;
-        t.n = p.N - n0;
-        t.k = w.rows;
-        t.C = C + (g * p.stride_c + m0 * p.ldc + n0) * out;
-        return true;
-    }
-    // Tiles that run together on one XCD are neighbours: bands of kBand row
-    // tiles, walked column by column.
-    RowTile w;
-    int n0;
-    if (p.ends) {
-        const RowTiles<BM> tiles(p.ends, p.G, (int)p.T);
-        if (blockIdx.x >= (unsigned)(tiles.total * tiles_n)) return false;   // (the launch holds the most there can be)
-        int im, in;
-        tile_coords((int)blockIdx.x, tiles.total * tiles_n, tiles.total, tiles_n, kBand, 1, im, in);
-        n0 = in * BN;
-        w = tiles.find(im);
-    } else {
-        int im, in;
-        tile_coords((int)blockIdx.x, (int)gridDim.x, (int)((p.T + BM - 1) / BM), tiles_n, kBand, 1, im, in);
-        n0 = in * BN;
-        const int row0 = im * BM;
-        w = RowTile{0, row0, p.T - row0 < BM ? (int)(p.T - row0) : BM};
-    }
-    const bool none = w.group >= p.G;
+    t.n = p.N - w.n0;
     t.A = A + w.row0 * t.lda;
-    t.B = none ? B : B + w.group * p.stride_b * E + (KIND == kBf16N ? (int64_t)n0 * E : n0 * t.ldb);
-    t.m = w.rows;
-    t.n = p.N - n0;
-    t.k = none ? 0 : p.K;
-    if constexpr (KIND == kFp8) {
-        t.SA = p.SA + w.row0 * p.ldsa;
-        t.SB = none ? p.SB : p.SB + w.group * p.stride_sb + n0 / kScaleBlock * p.ldsb;
+    unsigned char *C = static_cast<unsigned char *>(p.C);
+    if constexpr (KIND == kWgrad) {
+        t.A += (int64_t)w.m0 * E;
+        t.B = B + w.row0 * t.ldb + (int64_t)w.n0 * E;
+        t.m = p.K - w.m0;
+        t.k = w.rows;
+        t.C = C + (w.group * p.stride_c + w.m0 * p.ldc + w.n0) * out;
+    } else {
+        t.B = none ? B : B + w.group * p.stride_b * E + (KIND == kBf16N ? (int64_t)w.n0 * E : w.n0 * t.ldb);
+        t.m = w.rows;
+        t.k = none ? 0 : p.K;
+        if constexpr (KIND == kFp8) {
+            t.SA = p.SA + w.row0 * p.ldsa;
+            t.SB = none ? p.SB : p.SB + w.group * p.stride_sb + w.n0 / kScaleBlock * p.ldsb;
+        }
+        t.C = C + (w.row0 * p.ldc + w.n0) * out;
     }
-    t.C = C + (w.row0 * p.ldc + n0) * out;
-    return true;
+    return t;
 }
+
+// The tiles of a product, BM x BN each, in an order in which neighbours share
+// operands: bands of kBand row tiles, walked column by column.
+template <Kind KIND, int BM, int BN>
+struct TileOrder {
+    const GroupedArgs &p;
+    RowTiles<BM> rows;        // (of a product with groups)
+    int tiles_n, per, total;
+
+    __device__ __forceinline__ TileOrder(const GroupedArgs &p_)
+        : p(p_), rows(KIND == kWgrad ? nullptr : p_.ends, p_.G, (int)p_.T) {
+        tiles_n = (p.N + BN - 1) / BN;
+        per = KIND == kWgrad ? (p.K + BM - 1) / BM * tiles_n : 0;
+        total = KIND == kWgrad ? p.G * per : rows.total * tiles_n;
+    }
+    __device__ __forceinline__ Place at(int id) const {
+        if constexpr (KIND == kWgrad) {
+            const int g = id / per, r = id - g * per;
+            const RowTile w = find_group(p.ends, (int)p.T, g);
+            return Place{w.group, w.row0, w.rows, r / tiles_n * BM, r % tiles_n * BN};
+        } else {
+            int im, in;
+            tile_coords(id, total, rows.total, tiles_n, kBand, 0, im, in);
+            const RowTile w = rows.find(im);
+            return Place{w.group, w.row0, w.rows, 0, in * BN};
+        }
+    }
+};
+
+// The id of this workgroup's tile, or -1 (a launch holds the most tiles there
+// can be).  Workgroups go to the 8 XCDs in turn; each XCD gets an equal run of
+// neighbouring tiles, but of a weights' gradient, whose tiles are not equally
+// long, every eighth.
+template <Kind KIND>
+__device__ __forceinline__ int tile_id(int total) {
+    const int b = (int)blockIdx.x, x = b & 7, j = b >> 3, q = total >> 3, rem = total & 7;
+    if (KIND == kWgrad) return b < total ? b : -1;
+    return j < q + (x < rem ? 1 : 0) ? x * q + (x < rem ? x : rem) + j : -1;
+}
+
+__device__ __forceinline__ float relu_if(int relu, float v) { return relu && v < 0.f ? 0.f : v; }
 
 // Writes v[0 .. 3], the columns n .. n + 3 of a row of C at `c`, of which `left` exist.
 __device__ __forceinline__ void write4(const GroupedArgs &p, unsigned char *c, int n, int left, float (&v)[4]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (p.relu && v[i] < 0.f) v[i] = 0.f;
     if (p.out_bf16) {
         __bf16 t[4];
 #pragma unroll
@@ -124,13 +145,24 @@ int64_t tile_count(const GroupedArgs &a, int bm, int bn) {
     return (KIND == kWgrad ? cdiv(a.K, bm) * a.G : row_tiles(a, bm)) * cdiv(a.N, bn);
 }
 
-// The kernels of one file each.  launch_any takes every call; launch_tile those
-// that tile_takes.
+// A compiled kernel and what a launch of it takes, in microseconds: with n tiles
+// on 256 CUs of per_cu workgroups each, every round costs `fixed` (the first
+// data's way and the results') and for each stage of k (128 bytes) `one` where
+// a CU holds one workgroup, `full` where it holds per_cu.
+struct Choice {
+    int bm, bn, per_cu;
+    float one, full, fixed;
+    bool dense_only;        // for products without groups
+    xtc_status (*launch)(const GroupedArgs &, hipStream_t);
+};
+
+// The kernels of one file each, fp32 sums of e4m3 products where `wide`.
+// launch_any takes every call, the others those that aligned_rows() takes.
 template <Kind KIND>
 xtc_status launch_any(const GroupedArgs &a, hipStream_t s);
 template <Kind KIND>
-bool tile_takes(const GroupedArgs &a);
+const Choice *tile_choices(bool wide, int *count);
 template <Kind KIND>
-xtc_status launch_tile(const GroupedArgs &a, hipStream_t s);
+const Choice *stream_choices(bool wide, int *count);
 
 }  // namespace xtc

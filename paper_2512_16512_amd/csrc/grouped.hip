@@ -13,8 +13,10 @@ __global__ void __launch_bounds__(256) grouped_any_kernel(GroupedArgs p) {
     constexpr bool FP8 = KIND == kFp8;
     constexpr int BM = 64, BN = 64, ROW = 128 + 16, E = FP8 ? 1 : 2, BK = 128 / E;
     __shared__ __attribute__((aligned(16))) unsigned char As[BM * ROW], Bs[BN * ROW];
-    Tile t;
-    if (!find_tile<KIND, BM, BN>(p, t)) return;
+    const TileOrder<KIND, BM, BN> order(p);
+    const int id = tile_id<KIND>(order.total);
+    if (id < 0) return;
+    const Tile t = make_tile<KIND>(p, order.at(id));
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int wm = (wave >> 1) * 32, wn = (wave & 1) * 32, l16 = lane & 15, g4 = lane >> 4;
 
@@ -114,7 +116,7 @@ __global__ void __launch_bounds__(256) grouped_any_kernel(GroupedArgs p) {
             if (m >= t.m) continue;
             float v[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) v[r] = acc[i][j][r];
+            for (int r = 0; r < 4; ++r) v[r] = relu_if(p.relu, acc[i][j][r]);
             write4(p, t.C + m * p.ldc * (p.out_bf16 ? 2 : 4), n, t.n - n, v);
         }
 }
@@ -130,10 +132,67 @@ xtc_status launch_any(const GroupedArgs &a, hipStream_t s) {
 }
 
 namespace {
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// 16-byte aligned rows, whole 16-byte chunks of k where they run along it, and
+// strides that keep the offsets within a tile in 31 bits.
+template <Kind KIND>
+bool aligned_rows(const GroupedArgs &a) {
+    const int64_t e = KIND == kFp8 ? 1 : 2, most = (int64_t(1) << 31) / 257;
+    if (!aligned16(a.A) || !aligned16(a.B) || a.lda * e % 16 || a.ldb * e % 16 || a.stride_b * e % 16) return false;
+    if (KIND != kWgrad && a.K * e % 16) return false;
+    return a.lda * e < most && a.ldb * e < most && a.ldsa * 4 < most && a.ldsb * 4 < most;
+}
+
+// The estimate of a launch.  How a group's rows fall into tiles only the GPU
+// knows: half a tile a group is taken to be empty.
+template <Kind KIND>
+double estimate_us(const Choice &c, const GroupedArgs &a) {
+    double rows, k;
+    if (KIND == kWgrad) {
+        rows = (double)cdiv(a.K, c.bm) * a.G;
+        k = (double)a.T / a.G;
+    } else {
+        const double each = (double)a.T / a.G / c.bm + .5;
+        rows = a.ends ? a.G * (each > 1 ? each : 1) : (double)cdiv(a.T, c.bm);
+        k = a.K;
+    }
+    const double stages = k * (KIND == kFp8 ? 1 : 2) / 128, slots = 256. * c.per_cu;
+    const int64_t n = (int64_t)(rows * cdiv(a.N, c.bn)), whole = (int64_t)(n / slots);
+    const int64_t rest = n - (int64_t)(whole * slots), held = cdiv(rest, 256);
+    double us = whole * (stages * c.full + c.fixed);
+    if (held > 0)
+        us += stages * (held > 1 ? c.one + (c.full - c.one) * (held - 1) / (c.per_cu - 1) : c.one) + c.fixed;
+    return us;
+}
+
 template <Kind KIND>
 xtc_status launch(const GroupedArgs &a, hipStream_t s) {
-    return tile_takes<KIND>(a) ? launch_tile<KIND>(a, s) : launch_any<KIND>(a, s);
+    if (!aligned_rows<KIND>(a)) return launch_any<KIND>(a, s);
+    const bool wide = KIND == kFp8 && !a.out_bf16;
+    const Choice *best = nullptr;
+    double least = 0;
+    auto look = [&](const Choice *c, int count) {
+        for (int i = 0; i < count; ++i) {
+            if (c[i].dense_only && a.ends) continue;
+            const double us = estimate_us<KIND>(c[i], a);
+            if (!best || us < least) {
+                best = &c[i];
+                least = us;
+            }
+        }
+    };
+    int count = 0;
+    const Choice *tiles = tile_choices<KIND>(wide, &count);
+    look(tiles, count);
+    if constexpr (KIND != kWgrad) {
+        const Choice *streams = stream_choices<KIND>(wide, &count);
+        look(streams, count);
+    }
+    return best->launch(a, s);
 }
+
 }  // namespace
 
 xtc_status launch_grouped_fp8(const GroupedArgs &a, hipStream_t s) { return launch<kFp8>(a, s); }

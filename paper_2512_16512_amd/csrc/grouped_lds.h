@@ -1,0 +1,138 @@
+// Operands of the grouped and 8-bit products in LDS: their copies from memory,
+// their layouts, and the fragments that the matrix instructions take.
+//
+// A stage holds 128 bytes of k (128 e4m3 or 64 bf16 values).  An operand whose
+// rows run along k lies as rows of 128 bytes, its 16-byte chunk c of row r at slot
+// c ^ (r >> 1 & 7): the fragment reads, 16 or 32 rows of one or two chunks at a
+// time, then meet every bank once.  An operand with one k a row lies as it is
+// in memory, read by the transpose reads, chunk c of row k at c ^ swz_k(k).
+//
+// A fragment is MI rows of an operand's stage, 128 bytes of k each: piece q holds
+// the 16 bytes of chunk KG q + lane / MI, KG = 64 / MI, for both operands.
+#pragma once
+
+#include "grouped.h"
+#include "lds_dma.h"
+
+namespace xtc {
+
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+// Chunk swizzle of rows of CB chunks with one k each: spreads the four rows that
+// a transpose read takes at once, and rows k and k + 8, over the banks (rows of
+// 8 chunks fill half of them, so that odd rows are apart by themselves).
+template <int CB>
+__device__ __forceinline__ int swz_k(int k) {
+    return CB == 8 ? (k & 2) | ((k >> 1) & 4) : ((k & 1) * 6) ^ ((k & 2) * 5) ^ (((k >> 3) & 1) * 2);
+}
+
+// WIDE: e4m3 operands widened to bf16 (fp32 sums; see mfma_fp8.h).
+template <Kind KIND, bool WIDE, int MI>
+struct Product {
+    static constexpr int KG = 64 / MI, PIECES = 8 / KG;
+    typedef typename Bf16Mfma<MI>::acc_t acc_t;
+    static constexpr int NACC = Bf16Mfma<MI>::NACC;
+    // registers of a fragment as the instructions take it
+    struct Frag {
+        u32x4 v[WIDE ? 2 * PIECES : PIECES];
+    };
+    static __device__ __forceinline__ Frag prepare(const u32x4 (&raw)[PIECES]) {
+        Frag f;
+#pragma unroll
+        for (int q = 0; q < PIECES; ++q) {
+            if constexpr (WIDE) {
+                f.v[2 * q] = __builtin_bit_cast(u32x4, widen_fp8(raw[q][0], raw[q][1]));
+                f.v[2 * q + 1] = __builtin_bit_cast(u32x4, widen_fp8(raw[q][2], raw[q][3]));
+            } else {
+                f.v[q] = raw[q];
+            }
+        }
+        return f;
+    }
+    static __device__ __forceinline__ acc_t mul(const Frag &a, const Frag &b, acc_t c) {
+        if constexpr (KIND == kFp8 && !WIDE) {
+#pragma unroll
+            for (int s = 0; s < PIECES / 2; ++s) {
+                const i32x8 x = __builtin_bit_cast(i32x8, __builtin_shufflevector(a.v[2 * s], a.v[2 * s + 1], 0, 1, 2, 3, 4, 5, 6, 7));
+                const i32x8 y = __builtin_bit_cast(i32x8, __builtin_shufflevector(b.v[2 * s], b.v[2 * s + 1], 0, 1, 2, 3, 4, 5, 6, 7));
+                c = Fp8Mfma<MI>::mma(x, y, c);
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < (WIDE ? 2 : 1) * PIECES; ++s)
+                c = Bf16Mfma<MI>::mma(__builtin_bit_cast(u16x8, a.v[s]), __builtin_bit_cast(u16x8, b.v[s]), c);
+        }
+        return c;
+    }
+};
+
+// One operand's copies: where this lane's 16-byte chunks lie in a stage (kOOB,
+// read as zeros, outside the operand), and the buffer of a stage.
+template <bool K_ROWS, int ROWS, int PER_WAVE>
+struct Source {
+    const unsigned char *base;   // of the stage to copy next
+    int64_t ld;                  // bytes
+    int rows;                    // rows (or columns of rows along k) that exist
+    int off[PER_WAVE];
+    int k_at[PER_WAVE];          // rows along k: the chunk's first byte of k
+
+    __device__ __forceinline__ Source(const unsigned char *p, int64_t ld_, int extent, int wave, int lane)
+        : base(p), ld(ld_), rows(extent < ROWS ? extent : ROWS) {
+#pragma unroll
+        for (int q = 0; q < PER_WAVE; ++q) {
+            const int blk = wave * PER_WAVE + q;
+            if constexpr (K_ROWS) {
+                constexpr int CB = ROWS / 8;      // chunks of a row (one k)
+                const int byte = blk * 1024 + lane * 16, k = byte / (ROWS * 2), c = (byte / 16 % CB) ^ swz_k<CB>(k);
+                off[q] = c * 8 < extent ? (int)(k * ld) + c * 16 : kOOB;
+                k_at[q] = 0;
+            } else {
+                const int row = blk * 8 + lane / 8, c = (lane & 7) ^ ((row >> 1) & 7);
+                off[q] = row < extent ? (int)(row * ld) + c * 16 : kOOB;
+                k_at[q] = c * 16;
+            }
+        }
+    }
+    // The buffer of the next stage, of which `left` values of k exist; steps
+    // `stages` on.
+    __device__ __forceinline__ i32x4 stage(int left, int elt, int stages = 1) {
+        const int bk = 128 / elt, ks = left < bk ? left : bk;
+        int bytes = 0;
+        // (whole chunks: one that holds any value of a row is mapped)
+        if (left > 0) bytes = K_ROWS ? (ks - 1) * (int)ld + ((rows * 2 + 15) & ~15) : (rows - 1) * (int)ld + ks * elt;
+        const i32x4 r = make_rsrc(base, bytes);
+        base += stages * (K_ROWS ? bk * ld : 128);
+        return r;
+    }
+    // Where this lane's chunk of copy q lies in it.
+    __device__ __forceinline__ int offset(int q, int left, int elt) const {
+        return K_ROWS || k_at[q] < left * elt ? off[q] : kOOB;
+    }
+};
+
+// Fragment of the rows (or columns) first .. first + MI - 1 from an operand's
+// stage at s, `ROWS` rows of it in all.
+template <bool K_ROWS, int ROWS, int MI>
+__device__ __forceinline__ void read_fragment(const unsigned char *s, int first, int lane, u32x4 (&raw)[MI / 8]) {
+    constexpr int KG = 64 / MI;
+    const int lrow = lane % MI, lgrp = lane / MI;
+    if constexpr (!K_ROWS) {
+        const int row = first + lrow, swz = (row >> 1) & 7;
+#pragma unroll
+        for (int q = 0; q < 8 / KG; ++q)
+            raw[q] = *reinterpret_cast<const u32x4 *>(s + row * 128 + (((KG * q + lgrp) ^ swz) << 4));
+    } else {
+        const int rsub = (lane & 15) >> 2, c = first + (lrow & ~15) + 4 * (lane & 3);
+#pragma unroll
+        for (int q = 0; q < 8 / KG; ++q) {
+            // k and k + 4: their swizzle is one
+            const int k = 8 * (KG * q + lgrp) + rsub;
+            const unsigned char *q0 = s + k * ROWS * 2 + (((c >> 3) ^ swz_k<ROWS / 8>(k)) << 4) + 8 * (lane & 1);
+            const u16x4 lo = ds_read_tr16(reinterpret_cast<const unsigned short *>(q0));
+            const u16x4 hi = ds_read_tr16(reinterpret_cast<const unsigned short *>(q0 + 4 * ROWS * 2));
+            raw[q] = __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+    }
+}
+
+}  // namespace xtc

@@ -61,33 +61,41 @@ struct RowTiles {
     }
     Step first;
 
-    __device__ __forceinline__ RowTiles(const int32_t *ends_, int G_, int T_) : ends(ends_), G(G_), T(T_) {
+    // (without ends: one group of all T rows)
+    __device__ __forceinline__ RowTiles(const int32_t *ends_, int G_, int T_) : ends(ends_), G(G_), T(T_), first{} {
+        if (!ends) {
+            total = (T + BM - 1) / BM;
+            return;
+        }
         first = step(0, 0);
-        total = __shfl(first.upto, 63, 64);
-        int prev = __shfl(first.end, 63, 64);
+        total = __builtin_amdgcn_readlane(first.upto, 63);
+        int prev = __builtin_amdgcn_readlane(first.end, 63);
         for (int g0 = 64; g0 <= G; g0 += 64) {
             const Step s = step(g0, prev);
-            total += __shfl(s.upto, 63, 64);
-            prev = __shfl(s.end, 63, 64);
+            total += __builtin_amdgcn_readlane(s.upto, 63);
+            prev = __builtin_amdgcn_readlane(s.end, 63);
         }
-        total = __builtin_amdgcn_readfirstlane(total);
     }
 
     __device__ __forceinline__ RowTile find(int index) const {
+        if (!ends) {
+            const int row0 = index * BM;
+            return RowTile{0, row0, T - row0 < BM ? T - row0 : BM};
+        }
         Step s = first;
         int before = 0;
         for (int g0 = 0;; g0 += 64) {
             const unsigned long long who = __ballot(index >= before + s.upto - s.tiles && index < before + s.upto);
             if (who) {
                 const int l = __ffsll((long long)who) - 1;
-                const int row0 = __shfl(s.start, l, 64) + (index - before - __shfl(s.upto - s.tiles, l, 64)) * BM;
-                const int left = __shfl(s.end, l, 64) - row0;
-                return RowTile{__builtin_amdgcn_readfirstlane(g0 + l), __builtin_amdgcn_readfirstlane(row0),
-                               __builtin_amdgcn_readfirstlane(left < BM ? left : BM)};
+                const int first_tile = before + __builtin_amdgcn_readlane(s.upto - s.tiles, l);
+                const int row0 = __builtin_amdgcn_readlane(s.start, l) + (index - first_tile) * BM;
+                const int left = __builtin_amdgcn_readlane(s.end, l) - row0;
+                return RowTile{g0 + l, row0, left < BM ? left : BM};
             }
             if (g0 + 64 > G) return RowTile{-1, 0, 0};
-            before += __shfl(s.upto, 63, 64);
-            s = step(g0 + 64, __shfl(s.end, 63, 64));
+            before += __builtin_amdgcn_readlane(s.upto, 63);
+            s = step(g0 + 64, __builtin_amdgcn_readlane(s.end, 63));
         }
     }
 };
@@ -102,11 +110,11 @@ __device__ __forceinline__ RowTile find_group(const int32_t *ends, int T, int g)
         v = v > T ? T : v < 0 ? 0 : v;
         const int upto = scan_max(v, lane);           // lanes past g repeat the last
         const int last = g - i0 < 63 ? g - i0 : 63;
-        const int e = __shfl(upto, last, 64), s = last > 0 ? __shfl(upto, last - 1, 64) : 0;
+        const int e = __builtin_amdgcn_readlane(upto, last), s = last > 0 ? __builtin_amdgcn_readlane(upto, last - 1) : 0;
         start = g - i0 <= 63 ? (end > s ? end : s) : 0;
         end = end > e ? end : e;
     }
-    return RowTile{g, __builtin_amdgcn_readfirstlane(start), __builtin_amdgcn_readfirstlane(end - start)};
+    return RowTile{g, start, end - start};
 }
 
 }  // namespace xtc

@@ -493,6 +493,77 @@ def test_grouped_not_finite_rows_stay_in_their_group():
     assert bool((dw[5] == 0).all())
 
 
+# Sizes at which the products take their large tiles and a workgroup computes
+# more than one of them.
+
+
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+def test_matmul_fp8_large_tiles(out):
+    M, N, K = 4099, 4000, 400
+    qa, sa, a = scaled(5, 1, M, K)
+    qb, sb, b = scaled(6, 128, N, K)
+    say("matmul_fp8", M, N, K, out)
+    got = host(x.matmul_fp8(dev8(qa), dev(sa), dev8(qb), dev(sb), dtype=out))
+    ref = a @ b.t()
+    bound = 2 * U * (K + 8) * (a.abs() @ b.abs().t())
+    if out == torch.bfloat16:
+        # no product of a group of eight exceeds the product of its operands' largest
+        eight = [v.abs().reshape(v.shape[0], K // 8, 8).amax(2) for v in (a, b)]
+        bound += BF16 * ref.abs() + 2.0 ** -10 * (eight[0] @ eight[1].t())
+    within(got, ref, bound + U * ref.abs(), "large tiles")
+
+
+LARGE_SIZES = [1500, 0, 2100, 7, 3000, 256, 900, 1, 800, -436]
+
+
+def large_groups():
+    T = sum(abs(n) for n in LARGE_SIZES)
+    sizes = [n for n in LARGE_SIZES if n >= 0]
+    return T, sizes, torch.tensor(np.cumsum(sizes), dtype=torch.int32)
+
+
+@pytest.mark.parametrize("transpose_b", [False, True])
+def test_matmul_grouped_large_tiles(transpose_b):
+    T, sizes, ends = large_groups()
+    N, K = 2088, 200
+    a, b = as_type(normal(1, T, K), "bf16"), as_type(normal(2, len(sizes), K, N), "bf16")
+    stored = b.transpose(1, 2).contiguous() if transpose_b else b
+    ref = grouped_reference(a.double(), b.double(), sizes)
+    mag = grouped_reference(a.double().abs(), b.double().abs(), sizes)
+    for out in (torch.float32, torch.bfloat16):
+        say("matmul_grouped", T, N, K, transpose_b, out)
+        got = host(x.matmul_grouped(dev(a), dev(stored), ends.cuda(), transpose_b=transpose_b, dtype=out))
+        within(got, ref, 2 * U * (K + 8) * mag + (BF16 if out == torch.bfloat16 else U) * ref.abs(), "large tiles")
+
+
+def test_matmul_grouped_fp8_large_tiles():
+    T, sizes, ends = large_groups()
+    N, K = 2100, 272
+    qa, sa, a = scaled(8, 1, T, K)
+    qb, sb, b = scaled(9, 128, len(sizes), N, K)
+    ref = grouped_reference(a, b.transpose(1, 2), sizes)
+    mag = grouped_reference(a.abs(), b.abs().transpose(1, 2), sizes)
+    eight = [v.abs().reshape(*v.shape[:-1], K // 8, 8).amax(-1) for v in (a, b)]
+    cut = 2.0 ** -10 * grouped_reference(eight[0], eight[1].transpose(1, 2), sizes)
+    say("matmul_grouped_fp8", T, N, K)
+    got = host(x.matmul_grouped_fp8(dev8(qa), dev(sa), dev8(qb), dev(sb), ends.cuda(), dtype=torch.bfloat16))
+    within(got, ref, 2 * U * (K + 8) * mag + BF16 * ref.abs() + cut, "large tiles")
+
+
+def test_matmul_grouped_wgrad_large_tiles():
+    T, sizes, ends = large_groups()
+    N, K = 1304, 1296
+    a, dy = as_type(normal(1, T, K), "bf16"), as_type(normal(2, T, N), "bf16")
+    say("matmul_grouped_wgrad", T, N, K)
+    got = host(x.matmul_grouped_wgrad(dev(a), dev(dy), ends.cuda()))
+    i = 0
+    for g, n in enumerate(sizes):
+        p, q = a[i:i + n].double(), dy[i:i + n].double()
+        ref = p.t() @ q
+        within(got[g], ref, 2 * U * (n + 8) * (p.abs().t() @ q.abs()) + U * ref.abs(), "wgrad of group %d" % g)
+        i += n
+
+
 # ------------------------------------------------------- streams, far offsets
 
 
