@@ -434,6 +434,10 @@ def rmsnorm(x, weight, residual=None, eps=1e-6, quantize=False):
     ``x`` and ``residual`` [T, D] are float32 or bfloat16 CUDA tensors with unit column stride, ``weight`` [D] is of
     the same type or float32.  ``out`` is of x's type, or with ``quantize`` float8_e4m3fn with a float32 ``scale`` for
     each 128 columns.  Enqueued on torch's current stream."""
+    if _fast is not None:
+        r = _fast.rmsnorm(x, weight, residual, eps, quantize)
+        if r is not None:
+            return RmsNorm._make(r)
     import torch
     kinds = (torch.float32, torch.bfloat16)
     _matrix(x, "x", kinds)
@@ -458,6 +462,10 @@ def rmsnorm_backward(dy, x, weight, rstd, dresidual=None):
     """``(dx, dweight)`` of ``rmsnorm``: ``x`` is the sum that was normed (its result's ``residual``), ``dresidual`` the
     gradient that reaches that sum from elsewhere.  ``dx`` (x's type) is the gradient of x and of the residual,
     ``dweight`` float32."""
+    if _fast is not None:
+        r = _fast.rmsnorm_backward(dy, x, weight, rstd, dresidual)
+        if r is not None:
+            return r
     import torch
     _matrix(x, "x", (torch.float32, torch.bfloat16))
     T, D = x.shape
@@ -481,6 +489,10 @@ def rmsnorm_backward(dy, x, weight, rstd, dresidual=None):
 def quantize_fp8(x, block_rows=1):
     """``(q, scale)``: the matrix ``x`` (float32 or bfloat16) as float8_e4m3fn with a float32 scale for each
     ``block_rows`` x 128 values; 1 for activations, 128 for weights."""
+    if _fast is not None:
+        r = _fast.quantize_fp8(x, block_rows)
+        if r is not None:
+            return r
     import torch
     _matrix(x, "x", (torch.float32, torch.bfloat16))
     if block_rows not in (1, 128):
@@ -515,6 +527,10 @@ def matmul_fp8(a, a_scale, b, b_scale, out=None, relu=False, dtype=None):
     ``b`` [N, K] with ``b_scale`` [ceil(N/128), ceil(K/128)], float8_e4m3fn and float32, as ``quantize_fp8`` gives them
     with ``block_rows`` 1 and 128.  ``out`` [M, N] is float32 or bfloat16 (``dtype``, when allocated here; float32
     unless given)."""
+    if _fast is not None:
+        r = _fast.matmul_fp8(a, a_scale, b, b_scale, out, relu, dtype)
+        if r is not None:
+            return r
     import torch
     e4m3, f32 = (torch.float8_e4m3fn,), (torch.float32,)
     _matrix(a, "a", e4m3)
@@ -538,6 +554,10 @@ def matmul_grouped(a, b, ends, transpose_b=False, out=None, relu=False, dtype=No
     ``a`` [T, K] and ``b`` [G, K, N] ([G, N, K] with ``transpose_b``) are bfloat16, ``ends`` [G] int32, ascending, on
     the same device; rows past ``ends[-1]`` are zeros in ``out`` [T, N] (float32 or bfloat16: ``dtype``).  The
     gradient of ``a`` is the same call on out's gradient with the other ``transpose_b``."""
+    if _fast is not None:
+        r = _fast.matmul_grouped(a, b, ends, transpose_b, out, relu, dtype)
+        if r is not None:
+            return r
     import torch
     bf16 = (torch.bfloat16,)
     _matrix(a, "a", bf16)
@@ -557,6 +577,10 @@ def matmul_grouped(a, b, ends, transpose_b=False, out=None, relu=False, dtype=No
 def matmul_grouped_wgrad(a, dy, ends, out=None, dtype=None):
     """The gradient of ``matmul_grouped``'s ``b`` [G, K, N] (float32 or bfloat16: ``dtype``): ``a[rows].T @ dy[rows]``
     over each group's rows, zeros for an empty group.  ``a`` [T, K] and ``dy`` [T, N] are bfloat16."""
+    if _fast is not None:
+        r = _fast.matmul_grouped_wgrad(a, dy, ends, out, dtype)
+        if r is not None:
+            return r
     import torch
     bf16 = (torch.bfloat16,)
     _matrix(a, "a", bf16)
@@ -579,6 +603,10 @@ def matmul_grouped_wgrad(a, dy, ends, out=None, dtype=None):
 def matmul_grouped_fp8(a, a_scale, b, b_scale, ends, out=None, relu=False, dtype=None):
     """``matmul_grouped`` of block-scaled operands: ``a`` [T, K] with ``a_scale`` [T, ceil(K/128)], ``b`` [G, N, K] with
     ``b_scale`` [G, ceil(N/128), ceil(K/128)] (float8_e4m3fn and float32); ``out`` [T, N]."""
+    if _fast is not None:
+        r = _fast.matmul_grouped_fp8(a, a_scale, b, b_scale, ends, out, relu, dtype)
+        if r is not None:
+            return r
     import torch
     e4m3, f32 = (torch.float8_e4m3fn,), (torch.float32,)
     _matrix(a, "a", e4m3)

@@ -20,6 +20,30 @@ __device__ __forceinline__ void narrow(float v, Bf16 *p) {
 }
 __device__ __forceinline__ void narrow(float v, float *p) { *p = v; }
 
+// Eight consecutive values as they lie in memory.
+template <typename T>
+struct Raw8 {
+    T v[8];
+    __device__ __forceinline__ float at(int i) const { return widen(v[i]); }
+};
+// Whole groups are read with 16-byte loads, which the memory pipeline takes at
+// any address; of one that ends inside, or past the row's end, zeros stand for
+// the rest.
+template <typename T>
+__device__ __forceinline__ Raw8<T> raw8(const T *p, int valid) {
+    Raw8<T> r;
+    if (valid >= 8) {
+        __builtin_memcpy(r.v, p, sizeof(r.v));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            r.v[i] = T{};
+            if (i < valid) r.v[i] = p[i];
+        }
+    }
+    return r;
+}
+
 // Values p[0 .. 7], zeros from `valid` on.  Whole groups are read with 16-byte
 // loads, which the memory pipeline takes at any address.
 template <typename T>
