@@ -79,7 +79,7 @@ def _link_binding(obj: str, verbose: bool) -> None:
     tmp = BINDING + ".tmp%d" % os.getpid()
     _run([CXX, "-shared", "-o", tmp, obj, "-L" + HERE, "-l:libxtc.so", "-Wl,-rpath,$ORIGIN",
           "-L" + os.path.join(os.path.dirname(torch.__file__), "lib"),
-          "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"], "link of _binding.so", verbose)
+          "-ltorch_python", "-ltorch_cpu", "-ltorch_hip", "-lc10", "-lc10_hip"], "link of _binding.so", verbose)
     os.replace(tmp, BINDING)
 
 

@@ -431,11 +431,15 @@ bool with_backward_team(int64_t D, F &&f) {
 
 }  // namespace
 
-// Workgroups of the gradient's kernel: two a CU leave few partial sums.
+// Workgroups of the gradient's kernel: as many as its registers let the CUs hold,
+// up to four each (8191x2048 with two 44.5 us, the rows in flight too few).
 int norm_backward_slabs(int64_t T, int64_t D) {
-    int64_t groups = T;
-    with_backward_team(D, [&](auto nt, auto) { groups = (T + RowTeam<nt()>::ROWS - 1) / RowTeam<nt()>::ROWS; });
-    return (int)(groups < 512 ? groups : 512);
+    int64_t groups = T, most = 512;
+    with_backward_team(D, [&](auto nt, auto nv) {
+        groups = (T + RowTeam<nt()>::ROWS - 1) / RowTeam<nt()>::ROWS;
+        most = nt() == 1024 ? 256 : nv() > 1 ? 768 : 1024;
+    });
+    return (int)(groups < most ? groups : most);
 }
 
 xtc_status launch_rmsnorm(const NormArgs &a, xtc_dtype dtype, bool quantize, hipStream_t s) {

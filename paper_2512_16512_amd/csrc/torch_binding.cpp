@@ -12,6 +12,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/hip/EmptyTensor.h>
 #include <ATen/ops/empty.h>
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
@@ -191,8 +192,10 @@ bool tensors(PyObject *const *args, const at::Tensor *(&out)[N], unsigned maybe 
 bool truth(PyObject *o) { return o == Py_True || o == Py_False; }
 const void *data(const at::Tensor *t) { return t ? t->data_ptr() : nullptr; }
 
+// (Straight from the GPU's allocator: the dispatcher in front of at::empty costs as
+// much again, and a norm makes four tensors.)
 at::Tensor fresh(at::IntArrayRef shape, at::ScalarType type, const at::Tensor &like) {
-    return at::empty(shape, at::TensorOptions().dtype(type).device(like.device()));
+    return at::detail::empty_cuda(shape, type, like.device(), std::nullopt);
 }
 
 // The output of a product: `given`, or a new one of the type code in `o` (0
