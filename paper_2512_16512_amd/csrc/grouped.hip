@@ -162,8 +162,11 @@ double estimate_us(const Choice &c, const GroupedArgs &a) {
     const int64_t n = (int64_t)(rows * cdiv(a.N, c.bn)), whole = (int64_t)(n / slots);
     const int64_t rest = n - (int64_t)(whole * slots), held = cdiv(rest, 256);
     double us = whole * (stages * c.full + c.fixed);
-    if (held > 0)
-        us += stages * (held > 1 ? c.one + (c.full - c.one) * (held - 1) / (c.per_cu - 1) : c.one) + c.fixed;
+    if (held > 0) {
+        const double last = stages * (held > 1 ? c.one + (c.full - c.one) * (held - 1) / (c.per_cu - 1) : c.one) + c.fixed;
+        // (where CUs hold several workgroups, those of a last, partial round begin as others end)
+        us += whole > 0 && c.per_cu > 1 ? last / 2 : last;
+    }
     return us;
 }
 

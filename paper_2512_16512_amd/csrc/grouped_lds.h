@@ -1,13 +1,14 @@
 // Operands of the grouped and 8-bit products in LDS: their copies from memory,
 // their layouts, and the fragments that the matrix instructions take.
 //
-// A stage holds 128 bytes of k (128 e4m3 or 64 bf16 values).  An operand whose
-// rows run along k lies as rows of 128 bytes, its 16-byte chunk c of row r at slot
-// c ^ (r >> 1 & 7): the fragment reads, 16 or 32 rows of one or two chunks at a
-// time, then meet every bank once.  An operand with one k a row lies as it is
-// in memory, read by the transpose reads, chunk c of row k at c ^ swz_k(k).
+// A stage holds KB = 128 or 64 bytes of k (128 e4m3 values; 64 or 32 bf16 ones).  An
+// operand whose rows run along k lies as rows of KB bytes, its 16-byte chunk c of
+// row r at slot c ^ swz_row(r): the fragment reads, 16 rows of two neighbouring
+// chunks at a time, then meet every bank once.  An operand with one k a row lies
+// as it is in memory, read by the transpose reads, chunk c of row k at
+// c ^ swz_k(k).
 //
-// A fragment is MI rows of an operand's stage, 128 bytes of k each: piece q holds
+// A fragment is MI rows of an operand's stage, KB bytes of k each: piece q holds
 // the 16 bytes of chunk KG q + lane / MI, KG = 64 / MI, for both operands.
 #pragma once
 
@@ -18,6 +19,14 @@ namespace xtc {
 
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
+// Chunk swizzle of rows of KB bytes along k.  The reads are served 16 lanes at a
+// time, rows 0-3 and 12-15 of one chunk with rows 4-11 of its neighbour: of 128
+// bytes two rows fill the banks, of 64 four.
+template <int KB>
+__device__ __forceinline__ int swz_row(int r) {
+    return KB == 128 ? (r >> 1) & 7 : (0x78 >> (2 * ((r >> 2) & 3))) & 3;   // 0, 2, 3, 1
+}
+
 // Chunk swizzle of rows of CB chunks with one k each: spreads the four rows that
 // a transpose read takes at once, and rows k and k + 8, over the banks (rows of
 // 8 chunks fill half of them, so that odd rows are apart by themselves).
@@ -27,9 +36,9 @@ __device__ __forceinline__ int swz_k(int k) {
 }
 
 // WIDE: e4m3 operands widened to bf16 (fp32 sums; see mfma_fp8.h).
-template <Kind KIND, bool WIDE, int MI>
+template <Kind KIND, bool WIDE, int MI, int KB = 128>
 struct Product {
-    static constexpr int KG = 64 / MI, PIECES = 8 / KG;
+    static constexpr int KG = 64 / MI, PIECES = KB / 16 / KG;
     typedef typename Bf16Mfma<MI>::acc_t acc_t;
     static constexpr int NACC = Bf16Mfma<MI>::NACC;
     // registers of a fragment as the instructions take it
@@ -68,7 +77,7 @@ struct Product {
 
 // One operand's copies: where this lane's 16-byte chunks lie in a stage (kOOB,
 // read as zeros, outside the operand), and the buffer of a stage.
-template <bool K_ROWS, int ROWS, int PER_WAVE>
+template <bool K_ROWS, int ROWS, int PER_WAVE, int KB = 128>
 struct Source {
     const unsigned char *base;   // of the stage to copy next
     int64_t ld;                  // bytes
@@ -87,7 +96,8 @@ struct Source {
                 off[q] = c * 8 < extent ? (int)(k * ld) + c * 16 : kOOB;
                 k_at[q] = 0;
             } else {
-                const int row = blk * 8 + lane / 8, c = (lane & 7) ^ ((row >> 1) & 7);
+                constexpr int CH = KB / 16;           // chunks of a row
+                const int row = blk * (64 / CH) + lane / CH, c = (lane % CH) ^ swz_row<KB>(row);
                 off[q] = row < extent ? (int)(row * ld) + c * 16 : kOOB;
                 k_at[q] = c * 16;
             }
@@ -96,12 +106,12 @@ struct Source {
     // The buffer of the next stage, of which `left` values of k exist; steps
     // `stages` on.
     __device__ __forceinline__ i32x4 stage(int left, int elt, int stages = 1) {
-        const int bk = 128 / elt, ks = left < bk ? left : bk;
+        const int bk = KB / elt, ks = left < bk ? left : bk;
         int bytes = 0;
         // (whole chunks: one that holds any value of a row is mapped)
         if (left > 0) bytes = K_ROWS ? (ks - 1) * (int)ld + ((rows * 2 + 15) & ~15) : (rows - 1) * (int)ld + ks * elt;
         const i32x4 r = make_rsrc(base, bytes);
-        base += stages * (K_ROWS ? bk * ld : 128);
+        base += stages * (K_ROWS ? bk * ld : KB);
         return r;
     }
     // Where this lane's chunk of copy q lies in it.
@@ -112,19 +122,19 @@ struct Source {
 
 // Fragment of the rows (or columns) first .. first + MI - 1 from an operand's
 // stage at s, `ROWS` rows of it in all.
-template <bool K_ROWS, int ROWS, int MI>
-__device__ __forceinline__ void read_fragment(const unsigned char *s, int first, int lane, u32x4 (&raw)[MI / 8]) {
+template <bool K_ROWS, int ROWS, int MI, int KB>
+__device__ __forceinline__ void read_fragment(const unsigned char *s, int first, int lane, u32x4 (&raw)[KB * MI / 1024]) {
     constexpr int KG = 64 / MI;
     const int lrow = lane % MI, lgrp = lane / MI;
     if constexpr (!K_ROWS) {
-        const int row = first + lrow, swz = (row >> 1) & 7;
+        const int row = first + lrow, swz = swz_row<KB>(row);
 #pragma unroll
-        for (int q = 0; q < 8 / KG; ++q)
-            raw[q] = *reinterpret_cast<const u32x4 *>(s + row * 128 + (((KG * q + lgrp) ^ swz) << 4));
+        for (int q = 0; q < KB / 16 / KG; ++q)
+            raw[q] = *reinterpret_cast<const u32x4 *>(s + row * KB + (((KG * q + lgrp) ^ swz) << 4));
     } else {
         const int rsub = (lane & 15) >> 2, c = first + (lrow & ~15) + 4 * (lane & 3);
 #pragma unroll
-        for (int q = 0; q < 8 / KG; ++q) {
+        for (int q = 0; q < KB / 16 / KG; ++q) {
             // k and k + 4: their swizzle is one
             const int k = 8 * (KG * q + lgrp) + rsub;
             const unsigned char *q0 = s + k * ROWS * 2 + (((c >> 3) ^ swz_k<ROWS / 8>(k)) << 4) + 8 * (lane & 1);

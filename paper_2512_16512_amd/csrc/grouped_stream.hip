@@ -69,9 +69,9 @@ __global__ void __launch_bounds__(NW * 64) grouped_stream_kernel(GroupedArgs p) 
         u32x4 ra[G::TM][P::PIECES], rb[G::TN][P::PIECES];
         float scale[G::TM];
 #pragma unroll
-        for (int i = 0; i < G::TM; ++i) read_fragment<false, BM, 16>(s, i * 16, lane, ra[i]);
+        for (int i = 0; i < G::TM; ++i) read_fragment<false, BM, 16, 128>(s, i * 16, lane, ra[i]);
 #pragma unroll
-        for (int j = 0; j < G::TN; ++j) read_fragment<G::B_K_ROWS, BN, 16>(s + G::A_BYTES, j * 16, lane, rb[j]);
+        for (int j = 0; j < G::TN; ++j) read_fragment<G::B_K_ROWS, BN, 16, 128>(s + G::A_BYTES, j * 16, lane, rb[j]);
         if constexpr (KIND == kFp8) {
             const float *c = reinterpret_cast<const float *>(s + G::A_BYTES + G::B_BYTES);
 #pragma unroll

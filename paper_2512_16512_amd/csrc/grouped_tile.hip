@@ -17,19 +17,20 @@
 namespace xtc {
 namespace {
 
-template <Kind KIND, int BM, int BN, int WM, int WN, int MI, int STAGES>
+template <Kind KIND, int BM, int BN, int WM, int WN, int MI, int STAGES, int KB>
 struct TileCfg {
-    static constexpr int E = KIND == kFp8 ? 1 : 2, BK = 128 / E;
+    static constexpr int E = KIND == kFp8 ? 1 : 2, BK = KB / E;
     static constexpr bool A_K_ROWS = KIND == kWgrad, B_K_ROWS = KIND == kWgrad || KIND == kBf16N;
     static constexpr int NWM = BM / WM, NWN = BN / WN, NWAVES = NWM * NWN, NT = NWAVES * 64;
     static constexpr int TM = WM / MI, TN = WN / MI;
-    static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128;
+    static constexpr int A_BYTES = BM * KB, B_BYTES = BN * KB;
     static constexpr int A_PER_WAVE = A_BYTES / 1024 / NWAVES, B_PER_WAVE = B_BYTES / 1024 / NWAVES;
     static constexpr int S_BYTES = KIND == kFp8 ? NWAVES * 256 : 0;   // scales: 64 values a wave
     static constexpr int STAGE_BYTES = A_BYTES + B_BYTES + S_BYTES;
     static constexpr int LOADS = A_PER_WAVE + B_PER_WAVE + (KIND == kFp8 ? 1 : 0);
     static_assert(A_PER_WAVE * NWAVES * 1024 == A_BYTES && B_PER_WAVE * NWAVES * 1024 == B_BYTES,
                   "tiles must split into whole 1 KiB blocks per wave");
+    static_assert(KIND != kFp8 || KB == 128, "a stage is a block of scales");
     static_assert(KIND != kFp8 || NWAVES > BM / 64, "a wave for B's scales");
     static_assert(128 % WN == 0, "the columns of a wave share a scale");
     static_assert(STAGES >= 2 && STAGES * STAGE_BYTES <= 160 * 1024, "LDS budget");
@@ -37,11 +38,11 @@ struct TileCfg {
     static_assert(TM % 4 == 0, "the last two rows and the next stage's first two lie in four places");
 };
 
-template <Kind KIND, bool WIDE, int BM, int BN, int WM, int WN, int MI, int STAGES>
+template <Kind KIND, bool WIDE, int BM, int BN, int WM, int WN, int MI, int STAGES, int KB>
 __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64, 2)
 grouped_tile_kernel(GroupedArgs p) {
-    typedef TileCfg<KIND, BM, BN, WM, WN, MI, STAGES> G;
-    typedef Product<KIND, WIDE, MI> P;
+    typedef TileCfg<KIND, BM, BN, WM, WN, MI, STAGES, KB> G;
+    typedef Product<KIND, WIDE, MI, KB> P;
     typedef typename P::acc_t acc_t;
     __shared__ __attribute__((aligned(1024))) unsigned char smem[STAGES * G::STAGE_BYTES];
 
@@ -54,8 +55,8 @@ grouped_tile_kernel(GroupedArgs p) {
     const unsigned smem_base = lds_address(smem);
     const int KT = (t.k + G::BK - 1) / G::BK;
 
-    Source<G::A_K_ROWS, BM, G::A_PER_WAVE> sa(t.A, t.lda, t.m, wave, lane);
-    Source<G::B_K_ROWS, BN, G::B_PER_WAVE> sb(t.B, t.ldb, t.n, wave, lane);
+    Source<G::A_K_ROWS, BM, G::A_PER_WAVE, KB> sa(t.A, t.lda, t.m, wave, lane);
+    Source<G::B_K_ROWS, BN, G::B_PER_WAVE, KB> sb(t.B, t.ldb, t.n, wave, lane);
     // this lane's scale of a stage: rows of A, then the blocks of B's columns
     int s_off = kOOB, s_bytes = 0;
     const float *s_base = t.SA;
@@ -108,12 +109,12 @@ grouped_tile_kernel(GroupedArgs p) {
     typename P::Frag b[G::TN], a[4];
     auto read_b = [&](int slot, int j) {
         u32x4 raw[P::PIECES];
-        read_fragment<G::B_K_ROWS, BN, MI>(smem + slot * G::STAGE_BYTES + G::A_BYTES, wn * WN + j * MI, lane, raw);
+        read_fragment<G::B_K_ROWS, BN, MI, KB>(smem + slot * G::STAGE_BYTES + G::A_BYTES, wn * WN + j * MI, lane, raw);
         b[j] = P::prepare(raw);
     };
     auto read_a = [&](int slot, int i) {
         u32x4 raw[P::PIECES];
-        read_fragment<G::A_K_ROWS, BM, MI>(smem + slot * G::STAGE_BYTES, wm * WM + i * MI, lane, raw);
+        read_fragment<G::A_K_ROWS, BM, MI, KB>(smem + slot * G::STAGE_BYTES, wm * WM + i * MI, lane, raw);
         a[i & 3] = P::prepare(raw);
     };
     // scales of the wave's rows in a stage, times that of its columns
@@ -225,11 +226,11 @@ grouped_tile_kernel(GroupedArgs p) {
     }
 }
 
-template <Kind KIND, bool WIDE, int BM, int BN, int WM, int WN, int MI, int STAGES>
+template <Kind KIND, bool WIDE, int BM, int BN, int WM, int WN, int MI, int STAGES, int KB>
 xtc_status launch_as(const GroupedArgs &a, hipStream_t s) {
     const int64_t tiles = tile_count<KIND>(a, BM, BN);
     if (tiles >= kMostGroups / 2) return XTC_ERR_TOO_LARGE;
-    grouped_tile_kernel<KIND, WIDE, BM, BN, WM, WN, MI, STAGES>
+    grouped_tile_kernel<KIND, WIDE, BM, BN, WM, WN, MI, STAGES, KB>
         <<<(unsigned)tiles, (BM / WM) * (BN / WN) * 64, 0, s>>>(a);
     return hip_status(hipGetLastError());
 }
@@ -242,34 +243,42 @@ template <Kind KIND>
 const Choice *tile_choices(bool wide, int *count) {
     if constexpr (KIND == kFp8) {
         static const Choice sums[] = {
-            {256, 128, 1, 1.85f, 1.95f, 5, false, launch_as<KIND, true, 256, 128, 64, 64, 16, 3>},
-            {128, 128, 2, 1.1f, 2.7f, 4, false, launch_as<KIND, true, 128, 128, 64, 32, 16, 2>},
-            {64, 128, 1, .79f, .79f, 2, false, launch_as<KIND, true, 64, 128, 64, 32, 16, 4>},
+            {256, 128, 1, 1.85f, 1.95f, 5, false, launch_as<KIND, true, 256, 128, 64, 64, 16, 3, 128>},
+            {128, 128, 2, 1.1f, 2.7f, 4, false, launch_as<KIND, true, 128, 128, 64, 32, 16, 2, 128>},
+            {64, 128, 1, .79f, .79f, 2, false, launch_as<KIND, true, 64, 128, 64, 32, 16, 4, 128>},
         };
         static const Choice rounded[] = {
-            {256, 256, 1, 1.75f, 1.75f, 9, false, launch_as<KIND, false, 256, 256, 128, 64, 16, 2>},
-            {128, 128, 2, .88f, 1.34f, 4, false, launch_as<KIND, false, 128, 128, 64, 64, 16, 2>},
-            {128, 128, 1, .75f, .75f, 4, true, launch_as<KIND, false, 128, 128, 64, 32, 16, 4>},
-            {64, 128, 3, .72f, 1.4f, 2, false, launch_as<KIND, false, 64, 128, 64, 32, 16, 2>},
+            {256, 256, 1, 1.75f, 1.75f, 9, false, launch_as<KIND, false, 256, 256, 128, 64, 16, 2, 128>},
+            {128, 128, 2, .88f, 1.34f, 4, false, launch_as<KIND, false, 128, 128, 64, 64, 16, 2, 128>},
+            {128, 128, 1, .75f, .75f, 4, true, launch_as<KIND, false, 128, 128, 64, 32, 16, 4, 128>},
+            {64, 128, 3, .72f, 1.4f, 2, false, launch_as<KIND, false, 64, 128, 64, 32, 16, 2, 128>},
         };
         *count = wide ? 3 : 4;
         return wide ? sums : rounded;
     } else if constexpr (KIND == kWgrad) {
         static const Choice all[] = {
-            {256, 256, 1, 1.5f, 1.5f, 9, false, launch_as<KIND, false, 256, 256, 128, 64, 16, 2>},
-            {128, 256, 1, .9f, .9f, 5, false, launch_as<KIND, false, 128, 256, 64, 64, 16, 3>},
-            {128, 128, 2, .7f, 1.75f, 4, false, launch_as<KIND, false, 128, 128, 64, 64, 16, 2>},
+            // (four stages of 64 bytes: 102 us for 16384 rows over 16 groups, 1024 x 2048
+            // each; two of 128 116)
+            {256, 256, 1, 1.45f, 1.45f, 8, false, launch_as<KIND, false, 256, 256, 128, 64, 16, 4, 64>},
+            {128, 256, 1, .9f, .9f, 5, false, launch_as<KIND, false, 128, 256, 64, 64, 16, 3, 128>},
+            {128, 128, 2, .7f, 1.75f, 4, false, launch_as<KIND, false, 128, 128, 64, 64, 16, 2, 128>},
         };
         *count = 3;
         return all;
     } else {
         static const Choice all[] = {
-            {256, 256, 1, 1.5f, 1.5f, 8, false, launch_as<KIND, false, 256, 256, 128, 64, 16, 2>},
-            {128, 256, 1, .9f, .9f, 5, false, launch_as<KIND, false, 128, 256, 64, 64, 16, 3>},
-            {128, 128, 2, .7f, 1.7f, 3, false, launch_as<KIND, false, 128, 128, 64, 64, 16, 2>},
-            {64, 128, 3, .6f, 1.5f, 2, false, launch_as<KIND, false, 64, 128, 64, 32, 16, 2>},
+            {256, 256, 1, 1.5f, 1.5f, 8, false, launch_as<KIND, false, 256, 256, 128, 64, 16, 2, 128>},
+            // Stages of 64 bytes let a CU hold two workgroups of four 64x128 waves, one of
+            // which computes while the other begins or stores (16384 rows over 16 groups,
+            // 1024 -> 2048: 87 us, the other tiles 103); rows along k then move half a
+            // line at a time, so B's other layout gains less (96 us, 100).
+            {128, 256, 2, KIND == kBf16N ? 1.2f : 1.3f, KIND == kBf16N ? 2.f : 2.4f, KIND == kBf16N ? 6.f : 4.f, false,
+             launch_as<KIND, false, 128, 256, 64, 128, 16, 3, 64>},
+            {128, 256, 1, .9f, .9f, 5, false, launch_as<KIND, false, 128, 256, 64, 64, 16, 3, 128>},
+            {128, 128, 2, .7f, 1.7f, 3, false, launch_as<KIND, false, 128, 128, 64, 64, 16, 2, 128>},
+            {64, 128, 3, .6f, 1.5f, 2, false, launch_as<KIND, false, 64, 128, 64, 32, 16, 2, 128>},
         };
-        *count = 4;
+        *count = 5;
         return all;
     }
 }
