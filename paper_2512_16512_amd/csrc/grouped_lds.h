@@ -120,6 +120,92 @@ struct Source {
     }
 };
 
+// The same for rows at any address, through registers: fetch() starts the loads
+// of the next stage, store() writes them where the copies would have.
+template <bool K_ROWS, int ROWS, int PER_WAVE, int KB>
+struct Carried {
+    const unsigned char *base;
+    int64_t ld;
+    int extent, rows;
+    u32x4 r[PER_WAVE];
+
+    __device__ __forceinline__ Carried(const unsigned char *p, int64_t ld_, int extent_)
+        : base(p), ld(ld_), extent(extent_), rows(extent_ < ROWS ? extent_ : ROWS) {}
+
+    // 16 bytes at p of which the first `valid` exist (whole elements of ELT bytes).
+    template <int ELT>
+    static __device__ __forceinline__ u32x4 cut(const unsigned char *p, int valid) {
+        u32x4 v = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 16; i += ELT)
+            if (i < valid) v[i / 4] |= (unsigned)(ELT == 2 ? *reinterpret_cast<const unsigned short *>(p + i) : p[i]) << (8 * (i % 4));
+        return v;
+    }
+    // v shifted down by `bytes`, 0 to 15.
+    static __device__ __forceinline__ u32x4 shifted(const u32x4 &v, int bytes) {
+        // by 8 and by 4 bytes as asked (bitwise selects), then within a dword
+        const unsigned m8 = bytes & 8 ? ~0u : 0u, m4 = bytes & 4 ? ~0u : 0u;
+        const unsigned a0 = v[0] ^ ((v[0] ^ v[2]) & m8), a1 = v[1] ^ ((v[1] ^ v[3]) & m8), a2 = v[2] & ~m8, a3 = v[3] & ~m8;
+        const unsigned b0 = a0 ^ ((a0 ^ a1) & m4), b1 = a1 ^ ((a1 ^ a2) & m4), b2 = a2 ^ ((a2 ^ a3) & m4), b3 = a3 & ~m4;
+        const unsigned s = (unsigned)(bytes & 3);
+        return u32x4{(unsigned)__builtin_amdgcn_alignbyte(b1, b0, s), (unsigned)__builtin_amdgcn_alignbyte(b2, b1, s),
+                     (unsigned)__builtin_amdgcn_alignbyte(b3, b2, s), (unsigned)__builtin_amdgcn_alignbyte(0, b3, s)};
+    }
+    // `wide`: the operand's rows hold 16 bytes at least.  A chunk that ends past its
+    // row (or the last of k) is then read from 16 bytes before that end and
+    // shifted; of narrower rows byte by byte.
+    template <int ELT>
+    __device__ __forceinline__ void fetch(int left, bool wide, int wave, int lane) {
+        constexpr int BK = KB / ELT;
+        const bool whole = left >= BK && (!K_ROWS || extent >= ROWS);
+        const unsigned char *row_at[PER_WAVE];
+        int at[PER_WAVE], end[PER_WAVE];       // bytes of the row: the chunk's first, and one past the last
+#pragma unroll
+        for (int q = 0; q < PER_WAVE; ++q) {
+            const int blk = wave * PER_WAVE + q;
+            if constexpr (K_ROWS) {
+                constexpr int CB = ROWS / 8;
+                const int byte = blk * 1024 + lane * 16, k = byte / (ROWS * 2);
+                at[q] = ((byte / 16 % CB) ^ swz_k<CB>(k)) * 16;
+                end[q] = k < left ? extent * 2 : 0;
+                row_at[q] = base + (k < left ? k : 0) * ld;
+            } else {
+                constexpr int CH = KB / 16;
+                // (rows past the last one repeat it: nothing of theirs is kept)
+                const int row = blk * (64 / CH) + lane / CH;
+                at[q] = ((lane % CH) ^ swz_row<KB>(row)) * 16;
+                end[q] = left * ELT;
+                row_at[q] = base + (row < rows ? row : rows - 1) * ld;
+            }
+        }
+        if (whole) {
+#pragma unroll
+            for (int q = 0; q < PER_WAVE; ++q) __builtin_memcpy(&r[q], row_at[q] + at[q], 16);
+        } else if (left > 0 && wide) {
+            u32x4 v[PER_WAVE];
+#pragma unroll
+            for (int q = 0; q < PER_WAVE; ++q) {
+                // (of a row of k past the last one, whose end is 0, the first row's)
+                const int last = (K_ROWS ? extent * 2 : end[q]) - 16;
+                __builtin_memcpy(&v[q], row_at[q] + (at[q] < last ? at[q] : last), 16);
+            }
+#pragma unroll
+            for (int q = 0; q < PER_WAVE; ++q) {
+                const int over = at[q] - (end[q] - 16);
+                const u32x4 none = {0, 0, 0, 0};
+                r[q] = over <= 0 ? v[q] : over < 16 ? shifted(v[q], over) : none;
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < PER_WAVE; ++q) r[q] = cut<ELT>(row_at[q] + at[q], left > 0 ? end[q] - at[q] : 0);
+        }
+        base += K_ROWS ? BK * ld : KB;
+    }
+    __device__ __forceinline__ void store(unsigned char *lds, int q, int lane) const {
+        *reinterpret_cast<u32x4 *>(lds + q * 1024 + lane * 16) = r[q];
+    }
+};
+
 // Fragment of the rows (or columns) first .. first + MI - 1 from an operand's
 // stage at s, `ROWS` rows of it in all.
 template <bool K_ROWS, int ROWS, int MI, int KB>

@@ -2,6 +2,9 @@
 // from memory into LDS (dma16), two stages of 128 bytes of k (128 e4m3 or 64 bf16
 // values) in a ring.
 //
+// Rows at any address (ANY) go through registers instead, one stage further
+// ahead.
+//
 // Loop.  A wave keeps the fragments of its columns (B) of a stage in registers
 // and walks through its rows (A), two fragments ahead.  Before the products of
 // the last two row fragments every read of the stage has returned: there
@@ -38,7 +41,7 @@ struct TileCfg {
     static_assert(TM % 4 == 0, "the last two rows and the next stage's first two lie in four places");
 };
 
-template <Kind KIND, bool WIDE, int BM, int BN, int WM, int WN, int MI, int STAGES, int KB>
+template <Kind KIND, bool WIDE, int BM, int BN, int WM, int WN, int MI, int STAGES, int KB, bool ANY>
 __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64, 2)
 grouped_tile_kernel(GroupedArgs p) {
     typedef TileCfg<KIND, BM, BN, WM, WN, MI, STAGES, KB> G;
@@ -55,19 +58,29 @@ grouped_tile_kernel(GroupedArgs p) {
     const unsigned smem_base = lds_address(smem);
     const int KT = (t.k + G::BK - 1) / G::BK;
 
-    Source<G::A_K_ROWS, BM, G::A_PER_WAVE, KB> sa(t.A, t.lda, t.m, wave, lane);
-    Source<G::B_K_ROWS, BN, G::B_PER_WAVE, KB> sb(t.B, t.ldb, t.n, wave, lane);
+    typedef std::conditional_t<ANY, Carried<G::A_K_ROWS, BM, G::A_PER_WAVE, KB>, Source<G::A_K_ROWS, BM, G::A_PER_WAVE, KB>> FromA;
+    typedef std::conditional_t<ANY, Carried<G::B_K_ROWS, BN, G::B_PER_WAVE, KB>, Source<G::B_K_ROWS, BN, G::B_PER_WAVE, KB>> FromB;
+    FromA sa = [&]() __attribute__((always_inline)) {
+        if constexpr (ANY) return FromA(t.A, t.lda, t.m);
+        else return FromA(t.A, t.lda, t.m, wave, lane);
+    }();
+    FromB sb = [&]() __attribute__((always_inline)) {
+        if constexpr (ANY) return FromB(t.B, t.ldb, t.n);
+        else return FromB(t.B, t.ldb, t.n, wave, lane);
+    }();
     // this lane's scale of a stage: rows of A, then the blocks of B's columns
-    int s_off = kOOB, s_bytes = 0;
     const float *s_base = t.SA;
+    int64_t s_off = -1;          // in values; none: -1
+    int s_bytes = 0;
+    float s_value = 0.f;
     if constexpr (KIND == kFp8) {
         const int r = wave * 64 + lane;
         if (wave < BM / 64) {
-            s_off = r < sa.rows ? r * (int)p.ldsa * 4 : kOOB;
+            if (r < sa.rows) s_off = r * p.ldsa;
             s_bytes = ((sa.rows - 1) * (int)p.ldsa + KT) * 4;
         } else {
             const int nb = r - BM;
-            s_off = nb * 128 < sb.rows ? nb * (int)p.ldsb * 4 : kOOB;
+            if (nb * 128 < sb.rows) s_off = nb * p.ldsb;
             s_base = t.SB;
             s_bytes = ((sb.rows - 1) / 128 * (int)p.ldsb + KT) * 4;
         }
@@ -75,27 +88,49 @@ grouped_tile_kernel(GroupedArgs p) {
 
     // The copies of stage kt into a slot: LOADS a wave, past the end of k too (they
     // write zeros), so that one count of copies in flight holds throughout.
-    // begin() settles the stage, piece(q) issues one of them.
+    // begin() settles the stage, piece(q) issues one of them.  Of rows at any
+    // address (ANY) the stage's values are on their way to registers since
+    // fetch(), and piece(q) writes them.
     i32x4 ra, rb;
     int left = 0, next = 0;      // of k from stage `next` on
     unsigned at = 0;
-    auto begin = [&](int kt, int slot) {
-        at = smem_base + slot * G::STAGE_BYTES;
-        left = t.k - kt * G::BK;
-        next = kt;
-        ra = sa.stage(left, G::E);
-        rb = sb.stage(left, G::E);
+    unsigned char *to = smem;
+    auto fetch = [&](int kt) __attribute__((always_inline)) {
+        if constexpr (ANY) {
+            left = t.k - kt * G::BK;
+            sa.template fetch<G::E>(left, (KIND == kWgrad ? p.K : t.k) * G::E >= 16, wave, lane);
+            sb.template fetch<G::E>(left, (G::B_K_ROWS ? p.N : t.k) * G::E >= 16, wave, lane);
+            if constexpr (KIND == kFp8) s_value = left > 0 && s_off >= 0 ? s_base[s_off + kt] : 0.f;
+        }
     };
-    auto piece = [&](auto Q) {
+    auto begin = [&](int kt, int slot) __attribute__((always_inline)) {
+        if constexpr (ANY) {
+            to = smem + slot * G::STAGE_BYTES;
+        } else {
+            at = smem_base + slot * G::STAGE_BYTES;
+            left = t.k - kt * G::BK;
+            next = kt;
+            ra = sa.stage(left, G::E);
+            rb = sb.stage(left, G::E);
+        }
+    };
+    auto piece = [&](auto Q) __attribute__((always_inline)) {
         constexpr int q = Q;
-        if constexpr (q < G::A_PER_WAVE)
-            dma16(ra, at + (wave * G::A_PER_WAVE + q) * 1024, sa.offset(q, left, G::E));
-        else if constexpr (q < G::A_PER_WAVE + G::B_PER_WAVE)
-            dma16(rb, at + G::A_BYTES + (wave * G::B_PER_WAVE + q - G::A_PER_WAVE) * 1024,
-                  sb.offset(q - G::A_PER_WAVE, left, G::E));
-        else
-            dma4(make_rsrc(s_base, s_bytes), at + G::A_BYTES + G::B_BYTES + wave * 256,
-                 left > 0 && s_off != kOOB ? s_off + next * 4 : kOOB);
+        constexpr bool of_a = q < G::A_PER_WAVE, of_b = !of_a && q < G::A_PER_WAVE + G::B_PER_WAVE;
+        constexpr int qb = q - G::A_PER_WAVE;
+        if constexpr (ANY) {
+            if constexpr (of_a) sa.store(to + wave * G::A_PER_WAVE * 1024, q, lane);
+            else if constexpr (of_b) sb.store(to + G::A_BYTES + wave * G::B_PER_WAVE * 1024, qb, lane);
+            else reinterpret_cast<float *>(to + G::A_BYTES + G::B_BYTES)[wave * 64 + lane] = s_value;
+        } else {
+            if constexpr (of_a)
+                dma16(ra, at + (wave * G::A_PER_WAVE + q) * 1024, sa.offset(q, left, G::E));
+            else if constexpr (of_b)
+                dma16(rb, at + G::A_BYTES + (wave * G::B_PER_WAVE + qb) * 1024, sb.offset(qb, left, G::E));
+            else
+                dma4(make_rsrc(s_base, s_bytes), at + G::A_BYTES + G::B_BYTES + wave * 256,
+                     left > 0 && s_off >= 0 ? ((int)s_off + next) * 4 : kOOB);
+        }
     };
 
     acc_t acc[G::TM][G::TN];
@@ -107,19 +142,19 @@ grouped_tile_kernel(GroupedArgs p) {
             for (int r = 0; r < P::NACC; ++r) acc[i][j][r] = 0.f;
 
     typename P::Frag b[G::TN], a[4];
-    auto read_b = [&](int slot, int j) {
+    auto read_b = [&](int slot, int j) __attribute__((always_inline)) {
         u32x4 raw[P::PIECES];
         read_fragment<G::B_K_ROWS, BN, MI, KB>(smem + slot * G::STAGE_BYTES + G::A_BYTES, wn * WN + j * MI, lane, raw);
         b[j] = P::prepare(raw);
     };
-    auto read_a = [&](int slot, int i) {
+    auto read_a = [&](int slot, int i) __attribute__((always_inline)) {
         u32x4 raw[P::PIECES];
         read_fragment<G::A_K_ROWS, BM, MI, KB>(smem + slot * G::STAGE_BYTES, wm * WM + i * MI, lane, raw);
         a[i & 3] = P::prepare(raw);
     };
     // scales of the wave's rows in a stage, times that of its columns
     float scale[2][KIND == kFp8 ? G::TM : 1];
-    auto read_scales = [&](int slot, int set) {
+    auto read_scales = [&](int slot, int set) __attribute__((always_inline)) {
         if constexpr (KIND == kFp8) {
             const float *s = reinterpret_cast<const float *>(smem + slot * G::STAGE_BYTES + G::A_BYTES + G::B_BYTES);
             const float c = s[BM + wn * WN / 128];
@@ -134,7 +169,7 @@ grouped_tile_kernel(GroupedArgs p) {
     acc_t part[LAG + 1];         // e4m3: sums of a block of k, not yet scaled
     auto row_of = [](int n) { return n < HEAD ? n / G::TN : G::TM - 2 + (n - HEAD) % 2; };
     auto column_of = [](int n) { return n < HEAD ? n % G::TN : (n - HEAD) / 2; };
-    auto product = [&](auto N) {
+    auto product = [&](auto N) __attribute__((always_inline)) {
         constexpr int n = N, i = row_of(n), j = column_of(n);
         if constexpr (KIND == kFp8) {
             acc_t z;
@@ -145,18 +180,23 @@ grouped_tile_kernel(GroupedArgs p) {
             acc[i][j] = P::mul(b[j], a[i & 3], acc[i][j]);
         }
     };
-    auto add_scaled = [&](auto N) {
+    auto add_scaled = [&](auto N) __attribute__((always_inline)) {
         constexpr int n = N, i = row_of(n), j = column_of(n);
 #pragma unroll
         for (int r = 0; r < P::NACC; ++r) acc[i][j][r] += part[n % (LAG + 1)][r] * scale[0][i];
     };
 
-    each_index([&](auto S) {
+    each_index([&](auto S) __attribute__((always_inline)) {
+        fetch(S);
         begin(S, S);
-        each_index([&](auto Q) { piece(Q); }, std::make_integer_sequence<int, G::LOADS>());
+        each_index([&](auto Q) __attribute__((always_inline)) { piece(Q); }, std::make_integer_sequence<int, G::LOADS>());
     }, std::make_integer_sequence<int, STAGES>());
-    wait_vmcnt<(STAGES - 1) * G::LOADS>();
-    __builtin_amdgcn_s_barrier();
+    if constexpr (ANY) {
+        __syncthreads();
+    } else {
+        wait_vmcnt<(STAGES - 1) * G::LOADS>();
+        __builtin_amdgcn_s_barrier();
+    }
     asm volatile("" ::: "memory");
     read_scales(0, 0);
 #pragma unroll
@@ -165,7 +205,8 @@ grouped_tile_kernel(GroupedArgs p) {
     read_a(0, 1);
     int slot = 0;
     for (int kt = 0; kt < KT; ++kt) {
-        each_index([&](auto N) {
+        fetch(kt + STAGES);
+        each_index([&](auto N) __attribute__((always_inline)) {
             constexpr int n = N;
             if constexpr (n % G::TN == 0) read_a(slot, n / G::TN + 2);
             product(N);
@@ -174,7 +215,8 @@ grouped_tile_kernel(GroupedArgs p) {
         }, std::make_integer_sequence<int, HEAD>());
         // every read of the slot has returned, and stage kt + 1 has landed
         asm volatile("" ::: "memory");
-        wait_vmcnt_and_lds<(STAGES - 2) * G::LOADS>();
+        if constexpr (ANY) __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): also what this wave wrote for stage kt + 1
+        else wait_vmcnt_and_lds<(STAGES - 2) * G::LOADS>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         const int after = slot + 1 < STAGES ? slot + 1 : 0;
@@ -183,24 +225,24 @@ grouped_tile_kernel(GroupedArgs p) {
         read_a(after, 0);
         read_a(after, 1);
         __builtin_amdgcn_sched_barrier(0);
-        each_index([&](auto M) {
+        each_index([&](auto M) __attribute__((always_inline)) {
             constexpr int m = M, n = HEAD + m, q0 = m * G::LOADS / (2 * G::TN), q1 = (m + 1) * G::LOADS / (2 * G::TN);
             product(std::integral_constant<int, n>());
             if constexpr (KIND == kFp8 && n >= LAG) add_scaled(std::integral_constant<int, n - LAG>());
             if constexpr (m % 2 == 1) read_b(after, m / 2);
-            each_index([&](auto Q) { piece(std::integral_constant<int, q0 + Q>()); },
+            each_index([&](auto Q) __attribute__((always_inline)) { piece(std::integral_constant<int, q0 + Q>()); },
                        std::make_integer_sequence<int, q1 - q0>());
             __builtin_amdgcn_sched_barrier(0);
         }, std::make_integer_sequence<int, 2 * G::TN>());
         if constexpr (KIND == kFp8) {
-            each_index([&](auto N) { add_scaled(std::integral_constant<int, STEPS - LAG + N>()); },
+            each_index([&](auto N) __attribute__((always_inline)) { add_scaled(std::integral_constant<int, STEPS - LAG + N>()); },
                        std::make_integer_sequence<int, LAG>());
 #pragma unroll
             for (int i = 0; i < G::TM; ++i) scale[0][i] = scale[1][i];
         }
         slot = after;
     }
-    wait_vmcnt<0>();   // no copy may still be writing LDS when the workgroup ends
+    if constexpr (!ANY) wait_vmcnt<0>();   // no copy may still be writing LDS when the workgroup ends
 
     if (p.relu) {
 #pragma unroll
@@ -226,11 +268,11 @@ grouped_tile_kernel(GroupedArgs p) {
     }
 }
 
-template <Kind KIND, bool WIDE, int BM, int BN, int WM, int WN, int MI, int STAGES, int KB>
+template <Kind KIND, bool WIDE, int BM, int BN, int WM, int WN, int MI, int STAGES, int KB, bool ANY = false>
 xtc_status launch_as(const GroupedArgs &a, hipStream_t s) {
     const int64_t tiles = tile_count<KIND>(a, BM, BN);
     if (tiles >= kMostGroups / 2) return XTC_ERR_TOO_LARGE;
-    grouped_tile_kernel<KIND, WIDE, BM, BN, WM, WN, MI, STAGES, KB>
+    grouped_tile_kernel<KIND, WIDE, BM, BN, WM, WN, MI, STAGES, KB, ANY>
         <<<(unsigned)tiles, (BM / WM) * (BN / WN) * 64, 0, s>>>(a);
     return hip_status(hipGetLastError());
 }
@@ -283,6 +325,28 @@ const Choice *tile_choices(bool wide, int *count) {
     }
 }
 
+template <Kind KIND>
+xtc_status launch_any(const GroupedArgs &a, hipStream_t s) {
+    // 64 rows for few of them (KIND wgrad: 128 throughout)
+    const bool few = KIND != kWgrad && (a.ends ? a.T / a.G : a.T) <= 64;
+    if constexpr (KIND == kFp8) {
+        if (!a.out_bf16)
+            return few ? launch_as<KIND, true, 64, 128, 64, 32, 16, 2, 128, true>(a, s)
+                       : launch_as<KIND, true, 128, 128, 64, 32, 16, 2, 128, true>(a, s);
+        return few ? launch_as<KIND, false, 64, 128, 64, 32, 16, 2, 128, true>(a, s)
+                   : launch_as<KIND, false, 128, 128, 64, 64, 16, 2, 128, true>(a, s);
+    } else if constexpr (KIND == kWgrad) {
+        return launch_as<KIND, false, 128, 128, 64, 64, 16, 2, 128, true>(a, s);
+    } else {
+        return few ? launch_as<KIND, false, 64, 128, 64, 32, 16, 2, 128, true>(a, s)
+                   : launch_as<KIND, false, 128, 128, 64, 64, 16, 2, 128, true>(a, s);
+    }
+}
+
+template xtc_status launch_any<kFp8>(const GroupedArgs &, hipStream_t);
+template xtc_status launch_any<kBf16N>(const GroupedArgs &, hipStream_t);
+template xtc_status launch_any<kBf16T>(const GroupedArgs &, hipStream_t);
+template xtc_status launch_any<kWgrad>(const GroupedArgs &, hipStream_t);
 template const Choice *tile_choices<kFp8>(bool, int *);
 template const Choice *tile_choices<kBf16N>(bool, int *);
 template const Choice *tile_choices<kBf16T>(bool, int *);

@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(RowTeam<NT>::THREADS) rmsnorm_kernel(NormArgs 
         }
         if constexpr (QUANT) {
             const float s = fp8_scale(lanes_max<16>(amax));
-            store_fp8(static_cast<uint8_t *>(p.Y) + t * p.ldy + c, valid, to_fp8(y, 1.f / s));
+            store_fp8(static_cast<uint8_t *>(p.Y) + t * p.ldy + c, valid, to_fp8(y, s));
             if ((tid & 15) == 0 && valid > 0) p.S[t * p.lds + c / kScaleBlock] = s;
         } else {
             store8(static_cast<T *>(p.Y) + t * p.ldy + c, valid, y);
@@ -166,7 +166,7 @@ __global__ void __launch_bounds__(kThreads) rmsnorm_loop_kernel(NormArgs p) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) amax = fmaxf(amax, finite_abs(y[i]));
                 const float s = fp8_scale(lanes_max<16>(amax));
-                store_fp8(static_cast<uint8_t *>(p.Y) + t * p.ldy + c, valid, to_fp8(y, 1.f / s));
+                store_fp8(static_cast<uint8_t *>(p.Y) + t * p.ldy + c, valid, to_fp8(y, s));
                 if ((tid & 15) == 0 && valid > 0) p.S[t * p.lds + c / kScaleBlock] = s;
             } else {
                 store8(static_cast<T *>(p.Y) + t * p.ldy + c, valid, y);
@@ -349,7 +349,7 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(QuantArgs p) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) amax = fmaxf(amax, finite_abs(v[i]));
         const float s = fp8_scale(lanes_max<16>(amax));
-        store_fp8(p.Q + m * p.ldq + k, valid, to_fp8(v, 1.f / s));
+        store_fp8(p.Q + m * p.ldq + k, valid, to_fp8(v, s));
         if (sub == 0) p.S[m * p.lds + (b - m * kb)] = s;
     }
 }
@@ -387,13 +387,13 @@ __global__ void __launch_bounds__(kThreads) quantize_blocks_kernel(QuantArgs p) 
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kThreads / 64; ++i) amax = fmaxf(amax, scratch[i]);
-    const float s = fp8_scale(amax), inv = 1.f / s;
+    const float s = fp8_scale(amax);
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = r[q].at(i);
-        if (whole || q < rows) store_fp8(q8 + 16 * q * p.ldq, whole ? 8 : cols, to_fp8(v, inv));
+        if (whole || q < rows) store_fp8(q8 + 16 * q * p.ldq, whole ? 8 : cols, to_fp8(v, s));
     }
     if (threadIdx.x == 0) p.S[mb * p.lds + b] = s;
 }

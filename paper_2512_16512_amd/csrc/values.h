@@ -88,14 +88,19 @@ __device__ __forceinline__ float fp8_scale(float amax) {
     return s > kFp8Tiny ? s : kFp8Tiny;
 }
 
-// Eight e4m3 values v * inv in memory order (round to nearest even; what is not finite becomes NaN).
-// |v| * inv is at most 448 up to three roundings, far below 464, from where it would no longer
-// round to 448.
-__device__ __forceinline__ uint2 to_fp8(const float (&v)[8], float inv) {
+// Eight e4m3 values v / scale in memory order (round to nearest even; what is not finite becomes NaN).
+// The quotient is the true one: a product with 1/scale, corrected by its remainder, since bf16 values
+// meet ties between e4m3 values often (by the product alone one value in a hundred went the other way).
+// |v| / scale is at most 448 up to a rounding, far below 464, from where it would no longer round to 448.
+__device__ __forceinline__ uint2 to_fp8(const float (&v)[8], float scale) {
+    const float inv = 1.f / scale;
     float t[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        t[i] = __builtin_fabsf(v[i]) < __builtin_inff() ? v[i] * inv : __builtin_nanf("");
+    for (int i = 0; i < 8; ++i) {
+        const float q = v[i] * inv;
+        const float exact = __builtin_fmaf(__builtin_fmaf(-q, scale, v[i]), inv, q);
+        t[i] = __builtin_fabsf(v[i]) < __builtin_inff() ? exact : __builtin_nanf("");
+    }
     int lo = __builtin_amdgcn_cvt_pk_fp8_f32(t[0], t[1], 0, false);
     lo = __builtin_amdgcn_cvt_pk_fp8_f32(t[2], t[3], lo, true);
     int hi = __builtin_amdgcn_cvt_pk_fp8_f32(t[4], t[5], 0, false);
