@@ -1,0 +1,76 @@
+"""The mixture-of-experts block that runs the norm, 8-bit and grouped operators
+together, against the same block in 64 bits.
+
+Tolerances, as relative Frobenius errors: a value rounded to e4m3 is off by
+2.6 % in the mean (3 bits after the point), and a served result passes four such
+roundings (the normed rows, both weights, the hidden rows): 2 x 2.6 % x sqrt(4)
+allows it twice that.  A value rounded to bfloat16 is off by 0.17 %; eight
+roundings lie on the longest way of the training step."""
+import pytest
+
+from _helpers import say
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def moe():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU visible")
+    from paper_2512_16512_amd import moe as mod
+    return mod
+
+
+def block(x, r, norm, w1, w2, token, ends, p, T, on=None):
+    """The block in 64 bits for a given routing, differentiable.  ``on``: which hidden values the step had above zero
+    (a value that rounding takes over zero turns its whole gradient on or off, which no tolerance on roundings
+    describes); else those above zero in 64 bits."""
+    h = x + r
+    y = norm * h / torch.sqrt(h.square().mean(1, keepdim=True) + 1e-6)
+    rows, parts, i = y[token], [], 0
+    for e, j in enumerate(ends.tolist()):
+        h = rows[i:j] @ w1[e]
+        parts.append((torch.relu(h) if on is None else h * on[i:j]) @ w2[e])
+        i = j
+    return torch.zeros(T, x.shape[1], dtype=torch.float64).index_add(0, token, torch.cat(parts) * p[:, None])
+
+
+def rel(got, want):
+    return ((got.double().cpu() - want).norm() / want.norm()).item()
+
+
+@pytest.mark.parametrize("tokens", [1, 7, 200])
+def test_served_step(moe, tokens):
+    D, F, E = 256, 384, 6
+    norm, router, w1, w2 = moe.weights(E, D, F)
+    g = torch.Generator().manual_seed(tokens)
+    x, r = (torch.randn(tokens, D, generator=g).bfloat16().cuda() for _ in range(2))
+    served = moe.Served(norm, router, w1, w2)
+    say("served step", tokens)
+    out, total = served.step(x, r)
+    # the routing that the step took
+    n = moe.rmsnorm(x, norm, r, quantize=True)
+    token, ends, p, _ = moe.route(moe.matmul_fp8(n.out, n.scale, *served.router), 2)
+    want = block(*(t.double().cpu() for t in (x, r, norm, w1, w2)), token.cpu(), ends.cpu(), p.double().cpu(), tokens)
+    assert rel(out, want) < 4 * 0.026
+    assert rel(total, (x.double() + r.double()).cpu()) < 2 ** -8
+
+
+def test_train_step(moe):
+    T, D, F, E = 300, 192, 320, 5
+    norm, router, w1, w2 = moe.weights(E, D, F)
+    g = torch.Generator().manual_seed(3)
+    x, r, dout = (torch.randn(T, D, generator=g).bfloat16().cuda() for _ in range(3))
+    say("train step")
+    out, *grads = moe.train_step(x, r, norm, router, w1, w2, dout)
+    n = moe.rmsnorm(x, norm, r)
+    token, ends, p, _ = moe.route(n.out.float() @ router.float().t(), 2)
+    on = (moe.matmul_grouped(n.out[token], w1, ends, relu=True, dtype=torch.bfloat16) > 0).double().cpu()
+    leaf = [t.double().cpu().requires_grad_() for t in (x, norm, w1, w2)]
+    want = block(leaf[0], r.double().cpu(), leaf[1], leaf[2], leaf[3], token.cpu(), ends.cpu(), p.double().cpu(), T, on)
+    want.backward(dout.double().cpu())
+    assert rel(out, want.detach()) < 8 * 0.0017
+    for name, got, t in zip(("x", "norm", "w1", "w2"), grads, leaf):
+        assert rel(got, t.grad) < 8 * 0.0017, name

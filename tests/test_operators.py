@@ -625,3 +625,68 @@ def test_rows_and_matrices_past_32_bit_offsets():
     n = x.rmsnorm(a, torch.ones(K, dtype=torch.bfloat16, device="cuda"))
     _, _, y = norm_reference(rows, torch.ones(K), None, 1e-6)
     within(host(n.out[-40:]), y, (BF16 + 2 * (K + 16) * U) * y.abs(), "last rows normed")
+
+
+# ------------------------------------------------------ the native entries
+
+
+def test_native_and_python_paths_of_the_operators_agree(monkeypatch):
+    """The plain calls go through the native module; without it the same library is called from Python."""
+    v = normal(1, 40, 264).bfloat16().cuda()
+    w = torch.ones(264, dtype=torch.bfloat16, device="cuda")
+    wq, ws = x.quantize_fp8(normal(2, 130, 264).float().cuda(), block_rows=128)
+    fam = normal(3, 3, 264, 72).bfloat16().cuda()
+    famq = wq.view(torch.uint8).expand(3, 130, 264).contiguous().view(torch.float8_e4m3fn)
+    fams = ws.expand(3, *ws.shape).contiguous()
+    ends = torch.tensor([7, 30, 38], dtype=torch.int32, device="cuda")
+    out = torch.empty(40, 130, dtype=torch.bfloat16, device="cuda")
+
+    def calls():
+        n = x.rmsnorm(v, w, v, eps=1e-5, quantize=True)
+        m = x.rmsnorm(v, w.float())
+        assert type(n) is x.RmsNorm and m.scale is None and m.residual is v
+        yield from (n.out.float(), n.scale, n.residual, n.rstd, m.out, m.rstd)
+        yield from x.rmsnorm_backward(v, n.residual, w, n.rstd, v)
+        q, s = x.quantize_fp8(v)
+        yield from (q.float(), s, x.matmul_fp8(q, s, wq, ws), x.matmul_fp8(q, s, wq, ws, relu=True, dtype=torch.bfloat16))
+        assert x.matmul_fp8(q, s, wq, ws, out=out) is out
+        yield out.clone()
+        yield x.matmul_grouped(v, fam, ends, relu=True)
+        yield x.matmul_grouped(v, fam.transpose(1, 2).contiguous(), ends, transpose_b=True, dtype=torch.bfloat16)
+        yield x.matmul_grouped_wgrad(v, v[:, :80].contiguous(), ends, dtype=torch.bfloat16)
+        yield x.matmul_grouped_fp8(q, s, famq, fams, ends)
+
+    assert x._fast is not None
+    native = [t.clone() for t in calls()]
+    monkeypatch.setattr(x, "_fast", None)
+    for a, b in zip(native, calls()):
+        assert a.dtype == b.dtype and torch.equal(a, b)
+
+
+def test_captured_in_a_graph():
+    """Replays give what eager calls give, with new values in the same tensors."""
+    v = normal(1, 33, 512).bfloat16().cuda()
+    w = torch.ones(512, dtype=torch.bfloat16, device="cuda")
+    wq, ws = x.quantize_fp8(normal(2, 200, 512).float().cuda(), block_rows=128)
+    fam = normal(3, 4, 512, 96).bfloat16().cuda()
+    ends = torch.tensor([3, 9, 9, 33], dtype=torch.int32, device="cuda")
+
+    def chain():
+        n = x.rmsnorm(v, w, v, quantize=True)
+        dx, dw = x.rmsnorm_backward(v, n.residual, w, n.rstd)
+        return [x.matmul_fp8(n.out, n.scale, wq, ws), x.matmul_grouped(n.residual, fam, ends),
+                x.matmul_grouped_wgrad(v, n.residual, ends), dx, dw]
+
+    chain()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = chain()
+    for seed in range(4):
+        v.copy_(normal(10 + seed, 33, 512).bfloat16())
+        ends.copy_(torch.tensor([[3, 9, 9, 33], [0, 0, 33, 33], [8, 16, 24, 30], [33, 33, 33, 33]][seed], dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = chain()
+        for a, b in zip(captured, want):
+            assert torch.equal(a, b)

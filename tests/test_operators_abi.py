@@ -37,7 +37,7 @@ BACK = dict(T=4, D=200, DY=BAD, lddy=200, X=BAD, ldx=200, W=BAD, rstd=BAD, DR=BA
 
 
 @pytest.mark.parametrize("change,status", [
-    (dict(dtype=2), 4), (dict(w_dtype=1), 4), (dict(T=-1), 2), (dict(D=-1), 2), (dict(workspace_bytes=3199), 2),
+    (dict(dtype=2), 4), (dict(w_dtype=1), 4), (dict(T=-1), 2), (dict(D=-1), 2), (dict(workspace_bytes=x.xtc_rmsnorm_backward_workspace(4, 200) - 1), 2),
     (dict(lddy=199), 3), (dict(ldx=199), 3), (dict(lddr=199), 3), (dict(lddx=199), 3),
     (dict(DY=0), 1), (dict(X=0), 1), (dict(W=0), 1), (dict(rstd=0), 1), (dict(DX=0), 1), (dict(DW=0), 1),
     (dict(workspace=0), 1), (dict(DX=BAD + 2), 9), (dict(workspace=BAD + 4), 9), (dict(T=BIG), 7), (dict(lddx=BIG), 7),
@@ -154,6 +154,18 @@ E4M3 = torch.float8_e4m3fn
 def test_conveniences_refuse(fn, args, error, match):
     with pytest.raises(error, match=match):
         fn(*args)
+
+
+def test_the_native_entries_leave_other_tensors_to_python():
+    a, i = t(4, 8), torch.zeros(2, dtype=torch.int32)
+    q = t(4, 8, dtype=E4M3)
+    for name, args in (("rmsnorm", (a, t(8), None, 1e-6, False)), ("rmsnorm_backward", (a, a, t(8), t(4), None)),
+                       ("quantize_fp8", (a, 1)), ("matmul_fp8", (q, t(4, 1), q, t(1, 1), None, False, None)),
+                       ("matmul_grouped", (a, t(2, 8, 4), i, False, None, False, None)),
+                       ("matmul_grouped_wgrad", (a, a, i, None, None)),
+                       ("matmul_grouped_fp8", (q, t(4, 1), t(2, 4, 8, dtype=E4M3), t(2, 1, 1), i, None, False, None))):
+        fast = getattr(x._fast, name)
+        assert fast(*args) is None and fast() is None and fast(*([None] * len(args))) is None
 
 
 @pytest.mark.gpu
