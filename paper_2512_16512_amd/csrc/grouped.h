@@ -134,6 +134,22 @@ __device__ __forceinline__ void write4(const GroupedArgs &p, unsigned char *c, i
     }
 }
 
+// 16 bytes of results to p, of which the first `left` exist.
+template <typename T, int N>
+__device__ __forceinline__ void store_past_caches(T *p, const T (&v)[N], int left) {
+    static_assert(N * sizeof(T) == 16, "16 bytes");
+    typedef unsigned u32x4s __attribute__((ext_vector_type(4), aligned(2)));
+    if (left >= N) {
+        u32x4s q;
+        __builtin_memcpy(&q, v, 16);
+        __builtin_nontemporal_store(q, reinterpret_cast<u32x4s *>(p));
+    } else {
+#pragma unroll
+        for (int i = 0; i < N - 1; ++i)
+            if (i < left) p[i] = v[i];
+    }
+}
+
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Tiles of bm rows that a launch has to hold for whatever groups the GPU finds.
