@@ -164,10 +164,11 @@ int64_t tile_count(const GroupedArgs &a, int bm, int bn) {
 // A compiled kernel and what a launch of it takes, in microseconds: with n tiles
 // on 256 CUs of per_cu workgroups each, every round costs `fixed` (the first
 // data's way and the results') and for each stage of k (128 bytes) `one` where
-// a CU holds one workgroup, `full` where it holds per_cu.
+// a CU holds one workgroup (`cold` with weights that come from memory), `full`
+// where it holds per_cu.
 struct Choice {
     int bm, bn, per_cu;
-    float one, full, fixed;
+    float one, cold, full, fixed;
     bool dense_only;        // for products without groups
     xtc_status (*launch)(const GroupedArgs &, hipStream_t);
 };

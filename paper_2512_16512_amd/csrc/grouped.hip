@@ -34,9 +34,14 @@ double estimate_us(const Choice &c, const GroupedArgs &a) {
     const double stages = k * (KIND == kFp8 ? 1 : 2) / 128, slots = 256. * c.per_cu;
     const int64_t n = (int64_t)(rows * cdiv(a.N, c.bn)), whole = (int64_t)(n / slots);
     const int64_t rest = n - (int64_t)(whole * slots), held = cdiv(rest, 256);
-    double us = whole * (stages * c.full + c.fixed);
+    // Weights above 64 MB are taken to come from memory in every call (100 rows over
+    // 32 groups, bf16, 2048 to 1024: tiles of 64x128 34 us, 32x64 27; their stages at
+    // the rate of cached weights would have been 21 and 23).
+    const bool from_memory = KIND != kWgrad && (double)a.G * a.N * a.K * (KIND == kFp8 ? 1 : 2) > 64e6;
+    const double one = from_memory ? c.cold : c.one, full = c.per_cu > 1 ? c.full : one;
+    double us = whole * (stages * full + c.fixed);
     if (held > 0) {
-        const double last = stages * (held > 1 ? c.one + (c.full - c.one) * (held - 1) / (c.per_cu - 1) : c.one) + c.fixed;
+        const double last = stages * (held > 1 ? one + (full - one) * (held - 1) / (c.per_cu - 1) : one) + c.fixed;
         // (where CUs hold several workgroups, those of a last, partial round begin as others end)
         us += whole > 0 && c.per_cu > 1 ? last / 2 : last;
     }

@@ -327,40 +327,43 @@ template <Kind KIND>
 const Choice *tile_choices(bool wide, int *count) {
     if constexpr (KIND == kFp8) {
         static const Choice sums[] = {
-            {256, 128, 1, 1.85f, 1.95f, 5, false, launch_as<KIND, true, 256, 128, 64, 64, 16, 3, 128>},
-            {128, 128, 2, 1.1f, 2.7f, 4, false, launch_as<KIND, true, 128, 128, 64, 32, 16, 2, 128>},
-            {64, 128, 1, .79f, .79f, 2, false, launch_as<KIND, true, 64, 128, 64, 32, 16, 4, 128>},
+            // Widening costs about what the products do: the squarer the waves' parts, the
+            // less of it (4096 x 4096 x 4096: parts of 64x64 138 us, 64x32 178; tiles of
+            // 256x128 of the first 137, but 1531 x 2000 x 4096 58 for 38).
+            {128, 128, 2, 1.07f, 1.3f, 2.f, 4, false, launch_as<KIND, true, 128, 128, 64, 64, 16, 2, 128>},
+            // (4138 x 944 x 896: 13.5 us, the tile above 19; 571 x 1264 x 768: 8.2 and 11)
+            {128, 64, 2, .73f, .8f, 1.2f, 4, false, launch_as<KIND, true, 128, 64, 64, 32, 16, 3, 128>},
         };
         static const Choice rounded[] = {
-            {256, 256, 1, 1.75f, 1.75f, 9, false, launch_as<KIND, false, 256, 256, 128, 64, 16, 2, 128>},
-            {128, 128, 2, .88f, 1.34f, 4, false, launch_as<KIND, false, 128, 128, 64, 64, 16, 2, 128>},
-            {128, 128, 1, .75f, .75f, 4, true, launch_as<KIND, false, 128, 128, 64, 32, 16, 4, 128>},
-            {64, 128, 3, .72f, 1.4f, 2, false, launch_as<KIND, false, 64, 128, 64, 32, 16, 2, 128>},
+            {256, 256, 1, 1.75f, 1.75f, 1.75f, 9, false, launch_as<KIND, false, 256, 256, 128, 64, 16, 2, 128>},
+            {128, 128, 2, .88f, 1.1f, 1.34f, 4, false, launch_as<KIND, false, 128, 128, 64, 64, 16, 2, 128>},
+            {128, 128, 1, .75f, .75f, .75f, 4, true, launch_as<KIND, false, 128, 128, 64, 32, 16, 4, 128>},
+            {64, 128, 3, .72f, 1.1f, 1.4f, 2, false, launch_as<KIND, false, 64, 128, 64, 32, 16, 2, 128>},
         };
-        *count = wide ? 3 : 4;
+        *count = wide ? 2 : 4;
         return wide ? sums : rounded;
     } else if constexpr (KIND == kWgrad) {
         static const Choice all[] = {
             // (four stages of 64 bytes: 102 us for 16384 rows over 16 groups, 1024 x 2048
             // each; two of 128 116)
-            {256, 256, 1, 1.45f, 1.45f, 8, false, launch_as<KIND, false, 256, 256, 128, 64, 16, 4, 64>},
-            {128, 256, 1, .9f, .9f, 5, false, launch_as<KIND, false, 128, 256, 64, 64, 16, 3, 128>},
-            {128, 128, 2, .7f, 1.75f, 4, false, launch_as<KIND, false, 128, 128, 64, 64, 16, 2, 128>},
+            {256, 256, 1, 1.45f, 1.45f, 1.45f, 8, false, launch_as<KIND, false, 256, 256, 128, 64, 16, 4, 64>},
+            {128, 256, 1, .9f, .9f, .9f, 5, false, launch_as<KIND, false, 128, 256, 64, 64, 16, 3, 128>},
+            {128, 128, 2, .7f, .7f, 1.75f, 4, false, launch_as<KIND, false, 128, 128, 64, 64, 16, 2, 128>},
         };
         *count = 3;
         return all;
     } else {
         static const Choice all[] = {
-            {256, 256, 1, 1.5f, 1.5f, 8, false, launch_as<KIND, false, 256, 256, 128, 64, 16, 2, 128>},
+            {256, 256, 1, 1.5f, 1.5f, 1.5f, 8, false, launch_as<KIND, false, 256, 256, 128, 64, 16, 2, 128>},
             // Stages of 64 bytes let a CU hold two workgroups of four 64x128 waves, one of
             // which computes while the other begins or stores (16384 rows over 16 groups,
             // 1024 -> 2048: 87 us, the other tiles 103); rows along k then move half a
             // line at a time, so B's other layout gains less (96 us, 100).
-            {128, 256, 2, KIND == kBf16N ? 1.2f : 1.3f, KIND == kBf16N ? 2.f : 2.4f, KIND == kBf16N ? 6.f : 4.f, false,
+            {128, 256, 2, KIND == kBf16N ? 1.2f : 1.3f, KIND == kBf16N ? 1.2f : 1.3f, KIND == kBf16N ? 2.f : 2.4f, KIND == kBf16N ? 6.f : 4.f, false,
              launch_as<KIND, false, 128, 256, 64, 128, 16, 3, 64>},
-            {128, 256, 1, .9f, .9f, 5, false, launch_as<KIND, false, 128, 256, 64, 64, 16, 3, 128>},
-            {128, 128, 2, .7f, 1.7f, 3, false, launch_as<KIND, false, 128, 128, 64, 64, 16, 2, 128>},
-            {64, 128, 3, .6f, 1.5f, 2, false, launch_as<KIND, false, 64, 128, 64, 32, 16, 2, 128>},
+            {128, 256, 1, .9f, .9f, .9f, 5, false, launch_as<KIND, false, 128, 256, 64, 64, 16, 3, 128>},
+            {128, 128, 2, .7f, 1.05f, 1.7f, 3, false, launch_as<KIND, false, 128, 128, 64, 64, 16, 2, 128>},
+            {64, 128, 3, .6f, 1.f, 1.5f, 2, false, launch_as<KIND, false, 64, 128, 64, 32, 16, 2, 128>},
         };
         *count = 5;
         return all;
@@ -369,7 +372,8 @@ const Choice *tile_choices(bool wide, int *count) {
 
 template <Kind KIND>
 xtc_status launch_any(const GroupedArgs &a, hipStream_t s) {
-    // 64 rows for few of them (KIND wgrad: 128 throughout)
+    // 64 rows for few of them (KIND wgrad: 128 throughout).  (Widened parts of 64x64
+    // would not fit the registers beside the values on their way.)
     const bool few = KIND != kWgrad && (a.ends ? a.T / a.G : a.T) <= 64;
     if constexpr (KIND == kFp8) {
         if (!a.out_bf16)
