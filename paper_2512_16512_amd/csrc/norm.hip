@@ -359,7 +359,11 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(QuantArgs p) {
 template <typename T>
 __global__ void __launch_bounds__(kThreads) quantize_blocks_kernel(QuantArgs p) {
     __shared__ float scratch[kThreads / 64];
-    const int64_t kb = (p.K + kScaleBlock - 1) / kScaleBlock, mb = blockIdx.x / kb, b = blockIdx.x - mb * kb;
+    // Workgroups go to the 8 XCDs in turn; each XCD gets a run of neighbouring blocks,
+    // which share lines where rows do not begin on one (8192x3001: 22 us without, 17.6).
+    const int xcd = (int)blockIdx.x & 7, each = (int)gridDim.x >> 3, rem = (int)gridDim.x & 7;
+    const int64_t id = xcd * each + (xcd < rem ? xcd : rem) + ((int)blockIdx.x >> 3);
+    const int64_t kb = (p.K + kScaleBlock - 1) / kScaleBlock, mb = id / kb, b = id - mb * kb;
     const int64_t k = b * kScaleBlock + (threadIdx.x & 15) * 8, m = mb * 128 + (threadIdx.x >> 4);
     const T *x = static_cast<const T *>(p.X) + m * p.ldx + k;
     uint8_t *q8 = p.Q + m * p.ldq + k;
