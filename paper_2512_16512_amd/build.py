@@ -21,8 +21,8 @@ LIB = os.path.join(HERE, "libxtc.so")
 BINDING = os.path.join(HERE, "_binding.so")
 OBJDIR = os.path.join(HERE, "_build")
 
-SOURCES = ["gemm_f32.hip", "gemm_bf16.hip", "conv2d_f32.hip", "conv2d_bf16.hip", "norm.hip", "grouped.hip", "grouped_tile.hip", "grouped_stream.hip",
-           "xtc_api.cpp", "operators_api.cpp"]
+SOURCES = ["gemm_f32.hip", "gemm_bf16.hip", "conv2d_f32.hip", "conv2d_bf16.hip", "norm.hip",
+           "grouped.hip", "grouped_tile.hip", "grouped_stream.hip", "xtc_api.cpp", "operators_api.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

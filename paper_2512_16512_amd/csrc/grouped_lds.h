@@ -19,6 +19,8 @@ namespace xtc {
 
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
+constexpr int MI = 16;   // rows (or columns) of a fragment
+
 // Chunk swizzle of rows of KB bytes along k.  The reads are served 16 lanes at a
 // time, rows 0-3 and 12-15 of one chunk with rows 4-11 of its neighbour: of 128
 // bytes two rows fill the banks, of 64 four.
@@ -36,11 +38,9 @@ __device__ __forceinline__ int swz_k(int k) {
 }
 
 // WIDE: e4m3 operands widened to bf16 (fp32 sums; see mfma_fp8.h).
-template <Kind KIND, bool WIDE, int MI, int KB = 128>
+template <Kind KIND, bool WIDE, int KB = 128>
 struct Product {
-    static constexpr int KG = 64 / MI, PIECES = KB / 16 / KG;
-    typedef typename Bf16Mfma<MI>::acc_t acc_t;
-    static constexpr int NACC = Bf16Mfma<MI>::NACC;
+    static constexpr int PIECES = KB / 16 / (64 / MI);
     // registers of a fragment as the instructions take it
     struct Frag {
         u32x4 v[WIDE ? 2 * PIECES : PIECES];
@@ -58,13 +58,13 @@ struct Product {
         }
         return f;
     }
-    static __device__ __forceinline__ acc_t mul(const Frag &a, const Frag &b, acc_t c) {
+    static __device__ __forceinline__ f32x4 mul(const Frag &a, const Frag &b, f32x4 c) {
         if constexpr (KIND == kFp8 && !WIDE) {
 #pragma unroll
             for (int s = 0; s < PIECES / 2; ++s) {
                 const i32x8 x = __builtin_bit_cast(i32x8, __builtin_shufflevector(a.v[2 * s], a.v[2 * s + 1], 0, 1, 2, 3, 4, 5, 6, 7));
                 const i32x8 y = __builtin_bit_cast(i32x8, __builtin_shufflevector(b.v[2 * s], b.v[2 * s + 1], 0, 1, 2, 3, 4, 5, 6, 7));
-                c = Fp8Mfma<MI>::mma(x, y, c);
+                c = mma_fp8(x, y, c);
             }
         } else {
 #pragma unroll
@@ -208,7 +208,7 @@ struct Carried {
 
 // Fragment of the rows (or columns) first .. first + MI - 1 from an operand's
 // stage at s, `ROWS` rows of it in all.
-template <bool K_ROWS, int ROWS, int MI, int KB>
+template <bool K_ROWS, int ROWS, int KB>
 __device__ __forceinline__ void read_fragment(const unsigned char *s, int first, int lane, u32x4 (&raw)[KB * MI / 1024]) {
     constexpr int KG = 64 / MI;
     const int lrow = lane % MI, lgrp = lane / MI;

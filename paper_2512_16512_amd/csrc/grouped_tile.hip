@@ -1,9 +1,15 @@
 // The grouped and 8-bit products on LDS-staged tiles: operands copied straight
-// from memory into LDS (dma16), two stages of 128 bytes of k (128 e4m3 or 64 bf16
-// values) in a ring.
+// from memory into LDS (dma16), two to four stages of 128 or 64 bytes of k (128
+// e4m3 values; 64 or 32 bf16 ones) in a ring.
 //
 // Rows at any address (ANY) go through registers instead, one stage further
 // ahead.
+//
+// What bounds it.  Large products the matrix cores: the loop of a 256x256 tile
+// runs at 1583 TFLOP/s in bf16 and 2562 in e4m3, with the first data's way and the
+// results' (12 to 16 us a tile) 8192 x 8192 x 8192 in e4m3 at 2200.  Grouped ones the
+// CUs' shares: 16384 rows over 16 uneven groups are a few rounds of tiles of
+// which the last is partly empty (1024 to 2048: 84 us, 813 TFLOP/s).
 //
 // Loop.  A wave keeps the fragments of its columns (B) of a stage in registers
 // and walks through its rows (A), two fragments ahead.  Before the products of
@@ -20,7 +26,7 @@
 namespace xtc {
 namespace {
 
-template <Kind KIND, int BM, int BN, int WM, int WN, int MI, int STAGES, int KB>
+template <Kind KIND, int BM, int BN, int WM, int WN, int STAGES, int KB>
 struct TileCfg {
     static constexpr int E = KIND == kFp8 ? 1 : 2, BK = KB / E;
     static constexpr bool A_K_ROWS = KIND == kWgrad, B_K_ROWS = KIND == kWgrad || KIND == kBf16N;
@@ -41,20 +47,20 @@ struct TileCfg {
     static_assert(TM % 4 == 0, "the last two rows and the next stage's first two lie in four places");
 };
 
-template <Kind KIND, bool WIDE, int BM, int BN, int WM, int WN, int MI, int STAGES, int KB, bool ANY>
+template <Kind KIND, bool WIDE, int BM, int BN, int WM, int WN, int STAGES, int KB, bool ANY>
 __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64, 2)
 grouped_tile_kernel(GroupedArgs p) {
-    typedef TileCfg<KIND, BM, BN, WM, WN, MI, STAGES, KB> G;
-    typedef Product<KIND, WIDE, MI, KB> P;
-    typedef typename P::acc_t acc_t;
+    typedef TileCfg<KIND, BM, BN, WM, WN, STAGES, KB> G;
+    typedef Product<KIND, WIDE, KB> P;
     __shared__ __attribute__((aligned(1024))) unsigned char smem[STAGES * G::STAGE_BYTES];
 
     const TileOrder<KIND, BM, BN> order(p);
     const int id = tile_id<KIND>(order.total);
-    if (id < 0) return;                  const Tile t = make_tile<KIND>(p, order.at(id));
+    if (id < 0) return;
+    const Tile t = make_tile<KIND>(p, order.at(id));
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / G::NWN, wn = wave % G::NWN;
-    const int lrow = lane % MI;
+    const int lrow = lane % MI, lcol = lane / MI * 4;   // of a fragment's results: the row, the first of four columns
     const unsigned smem_base = lds_address(smem);
     const int KT = (t.k + G::BK - 1) / G::BK;
 
@@ -133,23 +139,17 @@ grouped_tile_kernel(GroupedArgs p) {
         }
     };
 
-    acc_t acc[G::TM][G::TN];
-#pragma unroll
-    for (int i = 0; i < G::TM; ++i)
-#pragma unroll
-        for (int j = 0; j < G::TN; ++j)
-#pragma unroll
-            for (int r = 0; r < P::NACC; ++r) acc[i][j][r] = 0.f;
+    f32x4 acc[G::TM][G::TN] = {};
 
     typename P::Frag b[G::TN], a[4];
     auto read_b = [&](int slot, int j) __attribute__((always_inline)) {
         u32x4 raw[P::PIECES];
-        read_fragment<G::B_K_ROWS, BN, MI, KB>(smem + slot * G::STAGE_BYTES + G::A_BYTES, wn * WN + j * MI, lane, raw);
+        read_fragment<G::B_K_ROWS, BN, KB>(smem + slot * G::STAGE_BYTES + G::A_BYTES, wn * WN + j * MI, lane, raw);
         b[j] = P::prepare(raw);
     };
     auto read_a = [&](int slot, int i) __attribute__((always_inline)) {
         u32x4 raw[P::PIECES];
-        read_fragment<G::A_K_ROWS, BM, MI, KB>(smem + slot * G::STAGE_BYTES, wm * WM + i * MI, lane, raw);
+        read_fragment<G::A_K_ROWS, BM, KB>(smem + slot * G::STAGE_BYTES, wm * WM + i * MI, lane, raw);
         a[i & 3] = P::prepare(raw);
     };
     // scales of the wave's rows in a stage, times that of its columns
@@ -165,16 +165,14 @@ grouped_tile_kernel(GroupedArgs p) {
     // Step n of a stage's products: rows of fragments one after the other, the
     // last two column by column.
     constexpr int STEPS = G::TM * G::TN, HEAD = STEPS - 2 * G::TN;
-    constexpr int LAG = KIND == kFp8 ? (MI == 16 ? 4 : 2) : 0;
-    acc_t part[LAG + 1];         // e4m3: sums of a block of k, not yet scaled
+    constexpr int LAG = KIND == kFp8 ? 4 : 0;
+    f32x4 part[LAG + 1];         // e4m3: sums of a block of k, not yet scaled
     auto row_of = [](int n) { return n < HEAD ? n / G::TN : G::TM - 2 + (n - HEAD) % 2; };
     auto column_of = [](int n) { return n < HEAD ? n % G::TN : (n - HEAD) / 2; };
     auto product = [&](auto N) __attribute__((always_inline)) {
         constexpr int n = N, i = row_of(n), j = column_of(n);
         if constexpr (KIND == kFp8) {
-            acc_t z;
-#pragma unroll
-            for (int r = 0; r < P::NACC; ++r) z[r] = 0.f;
+            const f32x4 z = {0.f, 0.f, 0.f, 0.f};
             part[n % (LAG + 1)] = P::mul(b[j], a[i & 3], z);
         } else {
             acc[i][j] = P::mul(b[j], a[i & 3], acc[i][j]);
@@ -183,7 +181,7 @@ grouped_tile_kernel(GroupedArgs p) {
     auto add_scaled = [&](auto N) __attribute__((always_inline)) {
         constexpr int n = N, i = row_of(n), j = column_of(n);
 #pragma unroll
-        for (int r = 0; r < P::NACC; ++r) acc[i][j][r] += part[n % (LAG + 1)][r] * scale[0][i];
+        for (int r = 0; r < 4; ++r) acc[i][j][r] += part[n % (LAG + 1)][r] * scale[0][i];
     };
 
     each_index([&](auto S) __attribute__((always_inline)) {
@@ -250,7 +248,7 @@ grouped_tile_kernel(GroupedArgs p) {
 #pragma unroll
             for (int j = 0; j < G::TN; ++j)
 #pragma unroll
-                for (int r = 0; r < P::NACC; ++r) acc[i][j][r] = acc[i][j][r] < 0.f ? 0.f : acc[i][j][r];
+                for (int r = 0; r < 4; ++r) acc[i][j][r] = acc[i][j][r] < 0.f ? 0.f : acc[i][j][r];
     }
     // Results leave as whole lines past the caches, which the operands then keep:
     // fp32 ones as they lie, four columns a lane (the weights' gradient of 16384
@@ -266,13 +264,11 @@ grouped_tile_kernel(GroupedArgs p) {
             if (m >= t.m) continue;
             float *c = reinterpret_cast<float *>(t.C) + m * p.ldc;
 #pragma unroll
-            for (int j = 0; j < G::TN; ++j)
-#pragma unroll
-                for (int r = 0; r < P::NACC; r += 4) {
-                    const int n = wn * WN + j * MI + Bf16Mfma<MI>::row(lane, r);
-                    const float v[4] = {acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]};
-                    store_past_caches(c + n, v, t.n - n);
-                }
+            for (int j = 0; j < G::TN; ++j) {
+                const int n = wn * WN + j * MI + lcol;
+                const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+                store_past_caches(c + n, v, t.n - n);
+            }
         }
         return;
     }
@@ -287,15 +283,12 @@ grouped_tile_kernel(GroupedArgs p) {
         each_index([&](auto I) __attribute__((always_inline)) {
             constexpr int i = i0 + I;
 #pragma unroll
-            for (int j = 0; j < G::TN; ++j)
+            for (int j = 0; j < G::TN; ++j) {
+                __bf16 v[4];
 #pragma unroll
-                for (int r = 0; r < P::NACC; r += 4) {
-                    __bf16 v[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = (__bf16)acc[i][j][r + e];
-                    __builtin_memcpy(__builtin_assume_aligned(own + (I * MI + lrow) * PITCH +
-                                                              (j * MI + Bf16Mfma<MI>::row(lane, r)) * 2, 8), v, 8);
-                }
+                for (int e = 0; e < 4; ++e) v[e] = (__bf16)acc[i][j][e];
+                __builtin_memcpy(__builtin_assume_aligned(own + (I * MI + lrow) * PITCH + (j * MI + lcol) * 2, 8), v, 8);
+            }
         }, std::make_integer_sequence<int, i1 - i0>());
         asm volatile("" ::: "memory");
         const int n = wn * WN + lane % LANES * 8;
@@ -310,11 +303,11 @@ grouped_tile_kernel(GroupedArgs p) {
     }, std::make_integer_sequence<int, (G::TM + PASS - 1) / PASS>());
 }
 
-template <Kind KIND, bool WIDE, int BM, int BN, int WM, int WN, int MI, int STAGES, int KB, bool ANY = false>
+template <Kind KIND, bool WIDE, int BM, int BN, int WM, int WN, int STAGES, int KB, bool ANY = false>
 xtc_status launch_as(const GroupedArgs &a, hipStream_t s) {
     const int64_t tiles = tile_count<KIND>(a, BM, BN);
     if (tiles >= kMostGroups / 2) return XTC_ERR_TOO_LARGE;
-    grouped_tile_kernel<KIND, WIDE, BM, BN, WM, WN, MI, STAGES, KB, ANY>
+    grouped_tile_kernel<KIND, WIDE, BM, BN, WM, WN, STAGES, KB, ANY>
         <<<(unsigned)tiles, (BM / WM) * (BN / WN) * 64, 0, s>>>(a);
     return hip_status(hipGetLastError());
 }
@@ -330,15 +323,15 @@ const Choice *tile_choices(bool wide, int *count) {
             // Widening costs about what the products do: the squarer the waves' parts, the
             // less of it (4096 x 4096 x 4096: parts of 64x64 138 us, 64x32 178; tiles of
             // 256x128 of the first 137, but 1531 x 2000 x 4096 58 for 38).
-            {128, 128, 2, 1.07f, 1.3f, 2.f, 4, false, launch_as<KIND, true, 128, 128, 64, 64, 16, 2, 128>},
+            {128, 128, 2, 1.07f, 1.3f, 2.f, 4, false, launch_as<KIND, true, 128, 128, 64, 64, 2, 128>},
             // (4138 x 944 x 896: 13.5 us, the tile above 19; 571 x 1264 x 768: 8.2 and 11)
-            {128, 64, 2, .73f, .8f, 1.2f, 4, false, launch_as<KIND, true, 128, 64, 64, 32, 16, 3, 128>},
+            {128, 64, 2, .73f, .8f, 1.2f, 4, false, launch_as<KIND, true, 128, 64, 64, 32, 3, 128>},
         };
         static const Choice rounded[] = {
-            {256, 256, 1, 1.75f, 1.75f, 1.75f, 9, false, launch_as<KIND, false, 256, 256, 128, 64, 16, 2, 128>},
-            {128, 128, 2, .88f, 1.1f, 1.34f, 4, false, launch_as<KIND, false, 128, 128, 64, 64, 16, 2, 128>},
-            {128, 128, 1, .75f, .75f, .75f, 4, true, launch_as<KIND, false, 128, 128, 64, 32, 16, 4, 128>},
-            {64, 128, 3, .72f, 1.1f, 1.4f, 2, false, launch_as<KIND, false, 64, 128, 64, 32, 16, 2, 128>},
+            {256, 256, 1, 1.75f, 1.75f, 1.75f, 9, false, launch_as<KIND, false, 256, 256, 128, 64, 2, 128>},
+            {128, 128, 2, .88f, 1.1f, 1.34f, 4, false, launch_as<KIND, false, 128, 128, 64, 64, 2, 128>},
+            {128, 128, 1, .75f, .75f, .75f, 4, true, launch_as<KIND, false, 128, 128, 64, 32, 4, 128>},
+            {64, 128, 3, .72f, 1.1f, 1.4f, 2, false, launch_as<KIND, false, 64, 128, 64, 32, 2, 128>},
         };
         *count = wide ? 2 : 4;
         return wide ? sums : rounded;
@@ -346,24 +339,24 @@ const Choice *tile_choices(bool wide, int *count) {
         static const Choice all[] = {
             // (four stages of 64 bytes: 102 us for 16384 rows over 16 groups, 1024 x 2048
             // each; two of 128 116)
-            {256, 256, 1, 1.45f, 1.45f, 1.45f, 8, false, launch_as<KIND, false, 256, 256, 128, 64, 16, 4, 64>},
-            {128, 256, 1, .9f, .9f, .9f, 5, false, launch_as<KIND, false, 128, 256, 64, 64, 16, 3, 128>},
-            {128, 128, 2, .7f, .7f, 1.75f, 4, false, launch_as<KIND, false, 128, 128, 64, 64, 16, 2, 128>},
+            {256, 256, 1, 1.45f, 1.45f, 1.45f, 8, false, launch_as<KIND, false, 256, 256, 128, 64, 4, 64>},
+            {128, 256, 1, .9f, .9f, .9f, 5, false, launch_as<KIND, false, 128, 256, 64, 64, 3, 128>},
+            {128, 128, 2, .7f, .7f, 1.75f, 4, false, launch_as<KIND, false, 128, 128, 64, 64, 2, 128>},
         };
         *count = 3;
         return all;
     } else {
         static const Choice all[] = {
-            {256, 256, 1, 1.5f, 1.5f, 1.5f, 8, false, launch_as<KIND, false, 256, 256, 128, 64, 16, 2, 128>},
+            {256, 256, 1, 1.5f, 1.5f, 1.5f, 8, false, launch_as<KIND, false, 256, 256, 128, 64, 2, 128>},
             // Stages of 64 bytes let a CU hold two workgroups of four 64x128 waves, one of
             // which computes while the other begins or stores (16384 rows over 16 groups,
             // 1024 -> 2048: 87 us, the other tiles 103); rows along k then move half a
             // line at a time, so B's other layout gains less (96 us, 100).
             {128, 256, 2, KIND == kBf16N ? 1.2f : 1.3f, KIND == kBf16N ? 1.2f : 1.3f, KIND == kBf16N ? 2.f : 2.4f, KIND == kBf16N ? 6.f : 4.f, false,
-             launch_as<KIND, false, 128, 256, 64, 128, 16, 3, 64>},
-            {128, 256, 1, .9f, .9f, .9f, 5, false, launch_as<KIND, false, 128, 256, 64, 64, 16, 3, 128>},
-            {128, 128, 2, .7f, 1.05f, 1.7f, 3, false, launch_as<KIND, false, 128, 128, 64, 64, 16, 2, 128>},
-            {64, 128, 3, .6f, 1.f, 1.5f, 2, false, launch_as<KIND, false, 64, 128, 64, 32, 16, 2, 128>},
+             launch_as<KIND, false, 128, 256, 64, 128, 3, 64>},
+            {128, 256, 1, .9f, .9f, .9f, 5, false, launch_as<KIND, false, 128, 256, 64, 64, 3, 128>},
+            {128, 128, 2, .7f, 1.05f, 1.7f, 3, false, launch_as<KIND, false, 128, 128, 64, 64, 2, 128>},
+            {64, 128, 3, .6f, 1.f, 1.5f, 2, false, launch_as<KIND, false, 64, 128, 64, 32, 2, 128>},
         };
         *count = 5;
         return all;
@@ -377,15 +370,15 @@ xtc_status launch_any(const GroupedArgs &a, hipStream_t s) {
     const bool few = KIND != kWgrad && (a.ends ? a.T / a.G : a.T) <= 64;
     if constexpr (KIND == kFp8) {
         if (!a.out_bf16)
-            return few ? launch_as<KIND, true, 64, 128, 64, 32, 16, 2, 128, true>(a, s)
-                       : launch_as<KIND, true, 128, 128, 64, 32, 16, 2, 128, true>(a, s);
-        return few ? launch_as<KIND, false, 64, 128, 64, 32, 16, 2, 128, true>(a, s)
-                   : launch_as<KIND, false, 128, 128, 64, 64, 16, 2, 128, true>(a, s);
+            return few ? launch_as<KIND, true, 64, 128, 64, 32, 2, 128, true>(a, s)
+                       : launch_as<KIND, true, 128, 128, 64, 32, 2, 128, true>(a, s);
+        return few ? launch_as<KIND, false, 64, 128, 64, 32, 2, 128, true>(a, s)
+                   : launch_as<KIND, false, 128, 128, 64, 64, 2, 128, true>(a, s);
     } else if constexpr (KIND == kWgrad) {
-        return launch_as<KIND, false, 128, 128, 64, 64, 16, 2, 128, true>(a, s);
+        return launch_as<KIND, false, 128, 128, 64, 64, 2, 128, true>(a, s);
     } else {
-        return few ? launch_as<KIND, false, 64, 128, 64, 32, 16, 2, 128, true>(a, s)
-                   : launch_as<KIND, false, 128, 128, 64, 64, 16, 2, 128, true>(a, s);
+        return few ? launch_as<KIND, false, 64, 128, 64, 32, 2, 128, true>(a, s)
+                   : launch_as<KIND, false, 128, 128, 64, 64, 2, 128, true>(a, s);
     }
 }
 

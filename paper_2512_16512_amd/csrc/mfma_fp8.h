@@ -1,8 +1,8 @@
-// e4m3 matrix-core instructions with unit scales.  A lane gives 32 values of
-// one row (of the first operand) or column (of the second), lane % MI; which 32
+// The e4m3 matrix-core instruction with unit scales.  A lane gives 32 values of
+// one row (of the first operand) or column (of the second), lane % 16; which 32
 // of the instruction's k is the same for both operands, so any assignment of
 // a tile's k to lane groups and bytes that both share computes the same sum.
-// Accumulators lie as those of the bf16 instructions of the same shape.
+// Accumulators lie as those of the bf16 instruction of the same shape.
 //
 // Precision, measured on gfx950 with one large and one small product: among the
 // eight products of eight consecutive bytes of a lane, what lies more than 13
@@ -23,13 +23,6 @@ namespace xtc {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-// 16 bytes at p and 16 at p + second, both on 16-byte boundaries.
-__device__ __forceinline__ i32x8 read_32_bytes(const unsigned char *p, int second) {
-    typedef int i32x4v __attribute__((ext_vector_type(4)));
-    const i32x4v lo = *reinterpret_cast<const i32x4v *>(p), hi = *reinterpret_cast<const i32x4v *>(p + second);
-    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-}
-
 // Eight e4m3 values (two registers) as bf16, exactly.
 __device__ __forceinline__ u16x8 widen_fp8(unsigned lo, unsigned hi) {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -40,25 +33,9 @@ __device__ __forceinline__ u16x8 widen_fp8(unsigned lo, unsigned hi) {
     return __builtin_bit_cast(u16x8, v);
 }
 
-template <int MI>
-struct Fp8Mfma;
-
-template <>
-struct Fp8Mfma<32> {
-    typedef f32x16 acc_t;
-    static constexpr int NACC = 16, K = 64;
-    static __device__ __forceinline__ acc_t mma(const i32x8 &a, const i32x8 &b, const acc_t &c) {
-        return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, 0, 0, 0);
-    }
-};
-
-template <>
-struct Fp8Mfma<16> {
-    typedef f32x4 acc_t;
-    static constexpr int NACC = 4, K = 128;
-    static __device__ __forceinline__ acc_t mma(const i32x8 &a, const i32x8 &b, const acc_t &c) {
-        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, 0, 0, 0);
-    }
-};
+// 16x16 products over 128 values of k.
+__device__ __forceinline__ f32x4 mma_fp8(const i32x8 &a, const i32x8 &b, const f32x4 &c) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, 0, 0, 0);
+}
 
 }  // namespace xtc

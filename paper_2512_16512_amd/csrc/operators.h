@@ -1,6 +1,6 @@
 // Internal interface between the host side of the 8-bit, grouped and
-// normalisation operators (operators_api.cpp) and their kernels (norm.hip,
-// grouped.hip).  Not installed.
+// normalisation operators (operators_api.cpp) and their kernels (norm.hip and
+// grouped.hip, grouped_tile.hip, grouped_stream.hip).  Not installed.
 #pragma once
 
 #include <hip/hip_runtime.h>
