@@ -564,6 +564,75 @@ def test_matmul_grouped_wgrad_large_tiles():
         i += n
 
 
+# Sizes at which each of the other kernels is taken.
+
+
+@pytest.mark.parametrize("quantize", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,D", [(5, 2048), (6, 1501)])
+def test_rmsnorm_of_other_widths(T, D, dtype, quantize):
+    test_rmsnorm(T, D, dtype, quantize)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,D", [(40, 2048), (9, 8192), (270, 5001)])
+def test_rmsnorm_backward_of_other_widths(T, D, dtype):
+    test_rmsnorm_backward(T, D, dtype)
+
+
+@pytest.mark.parametrize("M,N,K,out", [(1947, 8119, 400, torch.bfloat16), (11035, 132, 880, torch.bfloat16),
+                                       (4232, 102, 160, torch.float32), (8248, 105, 160, torch.float32)])
+def test_matmul_fp8_other_tiles(M, N, K, out):
+    qa, sa, a = scaled(15, 1, M, K)
+    qb, sb, b = scaled(16, 128, N, K)
+    say("matmul_fp8", M, N, K, out)
+    got = host(x.matmul_fp8(dev8(qa), dev(sa), dev8(qb), dev(sb), dtype=out))
+    ref = a @ b.t()
+    bound = 2 * U * (K + 8) * (a.abs() @ b.abs().t()) + U * ref.abs()
+    if out == torch.bfloat16:
+        eight = [v.abs().reshape(v.shape[0], K // 8, 8).amax(2) for v in (a, b)]
+        bound += BF16 * ref.abs() + 2.0 ** -10 * (eight[0] @ eight[1].t())
+    within(got, ref, bound, "other tiles")
+
+
+def uneven_groups(T, G):
+    """T rows in G groups of very different sizes, some empty, some rows past the last."""
+    share = normal(T, G + 1).exp().square()
+    share[::5] = 0
+    share[-1] = share.sum() / 50
+    sizes = (share / share.sum() * T).floor().long().tolist()
+    return sizes[:G], torch.tensor(np.cumsum(sizes[:G]), dtype=torch.int32)
+
+
+@pytest.mark.parametrize("T,N,K,G,transpose_b", [(10588, 392, 160, 56, False), (6836, 136, 208, 48, False),
+                                                 (15549, 139, 320, 40, True), (8221, 136, 192, 2, True),
+                                                 (18996, 585, 288, 22, True)])
+def test_matmul_grouped_other_tiles(T, N, K, G, transpose_b):
+    sizes, ends = uneven_groups(T, G)
+    a, b = as_type(normal(21, T, K), "bf16"), as_type(normal(22, G, K, N), "bf16")
+    stored = b.transpose(1, 2).contiguous() if transpose_b else b
+    ref = grouped_reference(a.double(), b.double(), sizes)
+    mag = grouped_reference(a.double().abs(), b.double().abs(), sizes)
+    for out in (torch.float32, torch.bfloat16):
+        say("matmul_grouped", T, N, K, G, transpose_b, out)
+        got = host(x.matmul_grouped(dev(a), dev(stored), ends.cuda(), transpose_b=transpose_b, dtype=out))
+        within(got, ref, 2 * U * (K + 8) * mag + (BF16 if out == torch.bfloat16 else U) * ref.abs(), "other tiles")
+
+
+def test_matmul_grouped_wgrad_other_tiles():
+    T, N, K, G = 205, 136, 1952, 32
+    sizes, ends = uneven_groups(T, G)
+    a, dy = as_type(normal(23, T, K), "bf16"), as_type(normal(24, T, N), "bf16")
+    say("matmul_grouped_wgrad", T, N, K, G)
+    got = host(x.matmul_grouped_wgrad(dev(a), dev(dy), ends.cuda()))
+    i = 0
+    for g, n in enumerate(sizes):
+        p, q = a[i:i + n].double(), dy[i:i + n].double()
+        ref = p.t() @ q
+        within(got[g], ref, 2 * U * (n + 8) * (p.abs().t() @ q.abs()) + U * ref.abs(), "wgrad of group %d" % g)
+        i += n
+
+
 # ------------------------------------------------------- streams, far offsets
 
 
