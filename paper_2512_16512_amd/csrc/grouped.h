@@ -84,7 +84,7 @@ struct TileOrder {
     __device__ __forceinline__ Place at(int id) const {
         if constexpr (KIND == kWgrad) {
             const int g = id / per, r = id - g * per;
-            const RowTile w = find_group(p.ends, (int)p.T, g);
+            const RowTile w = find_by_length(p.ends, p.G, (int)p.T, g);
             return Place{w.group, w.row0, w.rows, r / tiles_n * BM, r % tiles_n * BN};
         } else {
             int im, in;
@@ -98,7 +98,8 @@ struct TileOrder {
 // The id of this workgroup's tile, or -1 (a launch holds the most tiles there
 // can be).  Workgroups go to the 8 XCDs in turn; each XCD gets an equal run of
 // neighbouring tiles, but of a weights' gradient, whose tiles are not equally
-// long, every eighth.
+// long, every eighth, the longest groups' first (16384 rows over 16 uneven groups,
+// 1024 x 2048 each, tiles of 128x256: in the groups' order 111 to 122 us, so 100 to 110).
 template <Kind KIND>
 __device__ __forceinline__ int tile_id(int total) {
     const int b = (int)blockIdx.x, x = b & 7, j = b >> 3, q = total >> 3, rem = total & 7;

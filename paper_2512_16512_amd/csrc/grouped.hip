@@ -45,6 +45,13 @@ double estimate_us(const Choice &c, const GroupedArgs &a) {
         // (where CUs hold several workgroups, those of a last, partial round begin as others end)
         us += whole > 0 && c.per_cu > 1 ? last / 2 : last;
     }
+    if (KIND == kWgrad) {
+        // The tiles of the longest group take that long in any case; it is taken to hold
+        // up to three times its share (16384 rows over 16 uneven groups, 1024 x 2048 each:
+        // tiles of 256x256 95 to 129 us, 128x256 100 to 110; over equal ones 100 and 103).
+        const double longest = stages * c.one * (a.G < 5 ? (1 + a.G) / 2. : 3.) + c.fixed;
+        us = us > longest ? us : longest;
+    }
     return us;
 }
 

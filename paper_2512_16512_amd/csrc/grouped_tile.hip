@@ -337,11 +337,10 @@ const Choice *tile_choices(bool wide, int *count) {
         return wide ? sums : rounded;
     } else if constexpr (KIND == kWgrad) {
         static const Choice all[] = {
-            // (four stages of 64 bytes: 102 us for 16384 rows over 16 groups, 1024 x 2048
-            // each; two of 128 116)
-            {256, 256, 1, 1.45f, 1.45f, 1.45f, 8, false, launch_as<KIND, false, 256, 256, 128, 64, 4, 64>},
-            {128, 256, 1, .9f, .9f, .9f, 5, false, launch_as<KIND, false, 128, 256, 64, 64, 3, 128>},
-            {128, 128, 2, .7f, .7f, 1.75f, 4, false, launch_as<KIND, false, 128, 128, 64, 64, 2, 128>},
+            // Four stages of 64 bytes, of the same LDS as two of 128, wait less for memory.
+            {256, 256, 1, 1.75f, 1.75f, 1.75f, 17, false, launch_as<KIND, false, 256, 256, 128, 64, 4, 64>},
+            {128, 256, 1, 1.05f, 1.05f, 1.05f, 8.4f, false, launch_as<KIND, false, 128, 256, 64, 64, 3, 128>},
+            {128, 128, 2, .9f, .9f, 1.4f, 8, false, launch_as<KIND, false, 128, 128, 64, 64, 2, 128>},
         };
         *count = 3;
         return all;

@@ -100,21 +100,36 @@ struct RowTiles {
     }
 };
 
-// The rows of group g (g < G).
-__device__ __forceinline__ RowTile find_group(const int32_t *ends, int T, int g) {
+// Of each 64 groups the one that is `index` % 64 th in length, the longest first
+// (index < G; every lane of a wave calls it with the same arguments).
+__device__ __forceinline__ RowTile find_by_length(const int32_t *ends, int G, int T, int index) {
     const int lane = threadIdx.x & 63;
-    int start = 0, end = 0;
-    for (int i0 = 0; i0 <= g; i0 += 64) {
-        const int i = i0 + lane;
-        int v = i <= g ? ends[i] : 0;
-        v = v > T ? T : v < 0 ? 0 : v;
-        const int upto = scan_max(v, lane);           // lanes past g repeat the last
-        const int last = g - i0 < 63 ? g - i0 : 63;
-        const int e = __builtin_amdgcn_readlane(upto, last), s = last > 0 ? __builtin_amdgcn_readlane(upto, last - 1) : 0;
-        start = g - i0 <= 63 ? (end > s ? end : s) : 0;
-        end = end > e ? end : e;
+    int prev = 0;
+    for (int g0 = 0;; g0 += 64) {
+        const int g = g0 + lane;
+        const int v = g < G ? ends[g] : 0;
+        int end = scan_max(v > T ? T : v, lane);
+        end = end > prev ? end : prev;
+        if (index - g0 >= 64) {
+            prev = __builtin_amdgcn_readlane(end, 63);
+            continue;
+        }
+        int start = __shfl_up(end, 1, 64);
+        if (lane == 0) start = prev;
+        const int rows = g < G ? end - start : -1;
+        int longer = 0;
+        const int n = G - g0 < 64 ? G - g0 : 64;
+        for (int i0 = 0; i0 < n; i0 += 8) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) longer += __builtin_amdgcn_readlane(rows, i0 + i) > rows ? 1 : 0;
+        }
+        // equally long ones in their order
+        const int at = index - g0, same = __builtin_amdgcn_readlane(scan_max(longer <= at ? longer : 0, lane), 63);
+        const unsigned long long those = __ballot(longer == same);
+        const int before = __builtin_amdgcn_mbcnt_hi((unsigned)(those >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)those, 0));
+        const int l = __ffsll((long long)__ballot(longer == same && before == at - same)) - 1;
+        return RowTile{g0 + l, __builtin_amdgcn_readlane(start, l), __builtin_amdgcn_readlane(rows, l)};
     }
-    return RowTile{g, start, end - start};
 }
 
 }  // namespace xtc
