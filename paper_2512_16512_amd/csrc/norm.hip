@@ -55,8 +55,9 @@ __device__ __forceinline__ Raw8<float> raw_weight(const void *w, int w_f32, cons
 // NT threads share a row and hold it in registers, NV groups of eight columns
 // each, between the sum of squares and the outputs: every row is read once.
 // A workgroup has 256 threads or NT.  8192 x 4096 bf16 with a residual to 8
-// bits, bound by memory: the loop kernel below, which reads a row twice, took
-// 67 us.
+// bits, bound by memory: 52 us, 4.5 TB/s of its 236 MB where a copy reaches 5.3
+// (the loop kernel below, which reads a row twice, 67).  One row of 4096 columns
+// takes 3.9 us, the time of a launch and two trips to memory.
 template <int NT>
 struct RowTeam {
     static constexpr int THREADS = NT > 256 ? NT : 256, ROWS = THREADS / NT;
@@ -178,6 +179,8 @@ __global__ void __launch_bounds__(kThreads) rmsnorm_loop_kernel(NormArgs p) {
 // The gradient in one pass: team by team, rows t, t + teams, ...; a thread keeps
 // the sums over its rows of its columns' part of DW, and the workgroup leaves
 // one row of partial sums.  The next row is on its way while one is computed.
+// 8191 x 2048 bf16, bound by memory: 28.6 us, 4.7 TB/s; DX and DW by kernels of
+// their own, which read the rows twice, took 151 us.
 template <typename T, int NT, int NV>
 __global__ void __launch_bounds__(RowTeam<NT>::THREADS) rmsnorm_backward_kernel(NormBackwardArgs p) {
     typedef RowTeam<NT> Team;
@@ -313,7 +316,8 @@ __global__ void __launch_bounds__(kThreads) rmsnorm_dw_kernel(NormBackwardArgs p
 }
 
 // Column sums of the slabs: sixteen columns a workgroup, 64 runs of slabs, each
-// in its order, joined by halves.
+// in its order, joined by halves (1024 rows of 2048 sums: 5 us, a few trips to
+// memory and as many barriers).
 constexpr int kJoinColumns = 16, kJoinThreads = 1024;
 __global__ void __launch_bounds__(kJoinThreads) rmsnorm_dw_join_kernel(const float *partial, int slabs, int D, float *DW) {
     __shared__ float s[kJoinThreads];
@@ -333,7 +337,8 @@ __global__ void __launch_bounds__(kJoinThreads) rmsnorm_dw_join_kernel(const flo
     if (run == 0 && c < D) DW[c] = s[threadIdx.x];
 }
 
-// e4m3 with a scale per 1 x 128 block: sixteen lanes a block.
+// e4m3 with a scale per 1 x 128 block: sixteen lanes a block.  Bound by memory:
+// 4096 x 4096 bf16 in 11.2 us, 4.5 TB/s.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(QuantArgs p) {
     const int64_t kb = (p.K + kScaleBlock - 1) / kScaleBlock, blocks = p.M * kb;
@@ -355,7 +360,8 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(QuantArgs p) {
 }
 
 // e4m3 with a scale per 128 x 128 block: a workgroup a block, which stays in
-// registers between its maximum and its rounding.
+// registers between its maximum and its rounding.  Bound by memory: 8192 x 3001
+// bf16, whose rows begin at odd addresses, in 17.6 us, 4.2 TB/s.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) quantize_blocks_kernel(QuantArgs p) {
     __shared__ float scratch[kThreads / 64];
