@@ -45,17 +45,19 @@ struct Product {
     struct Frag {
         u32x4 v[WIDE ? 2 * PIECES : PIECES];
     };
+    // piece q of them, from the 16 bytes read
+    static __device__ __forceinline__ void prepare(Frag &f, const u32x4 (&raw)[PIECES], int q) {
+        if constexpr (WIDE) {
+            f.v[2 * q] = __builtin_bit_cast(u32x4, widen_fp8(raw[q][0], raw[q][1]));
+            f.v[2 * q + 1] = __builtin_bit_cast(u32x4, widen_fp8(raw[q][2], raw[q][3]));
+        } else {
+            f.v[q] = raw[q];
+        }
+    }
     static __device__ __forceinline__ Frag prepare(const u32x4 (&raw)[PIECES]) {
         Frag f;
 #pragma unroll
-        for (int q = 0; q < PIECES; ++q) {
-            if constexpr (WIDE) {
-                f.v[2 * q] = __builtin_bit_cast(u32x4, widen_fp8(raw[q][0], raw[q][1]));
-                f.v[2 * q + 1] = __builtin_bit_cast(u32x4, widen_fp8(raw[q][2], raw[q][3]));
-            } else {
-                f.v[q] = raw[q];
-            }
-        }
+        for (int q = 0; q < PIECES; ++q) prepare(f, raw, q);
         return f;
     }
     static __device__ __forceinline__ f32x4 mul(const Frag &a, const Frag &b, f32x4 c) {
