@@ -143,8 +143,9 @@ grouped_tile_kernel(GroupedArgs p) {
 
     // Fragments: of A four rows as read and, where they have to be widened first, two
     // widened; of B all columns, and two as read.  What is read is widened some
-    // products later, so that no product waits for either (widened as soon as read:
-    // 1531 x 2000 x 4096 38 us, LATER_FIGURE).
+    // products later, so that no product waits for either (818 x 3552 x 4608 widened as
+    // soon as read 43 us, so 39; vector instructions set singly between the matrix
+    // ones, or two products' chains in turn, gave nothing more).
     typename P::Frag b[G::TN], wide[2];
     u32x4 a[4][P::PIECES], b_read[2][P::PIECES];
     auto read_b = [&](int slot, int j) __attribute__((always_inline)) {
@@ -352,7 +353,7 @@ const Choice *tile_choices(bool wide, int *count) {
             // Widening costs about what the products do: the squarer the waves' parts, the
             // less of it (4096 x 4096 x 4096: parts of 64x64 138 us, 64x32 178; tiles of
             // 256x128 of the first 137, but 1531 x 2000 x 4096 58 for 38).
-            {128, 128, 2, 1.07f, 1.3f, 2.f, 4, false, launch_as<KIND, true, 128, 128, 64, 64, 2, 128>},
+            {128, 128, 2, 1.f, 1.3f, 2.f, 4, false, launch_as<KIND, true, 128, 128, 64, 64, 2, 128>},
             // (4138 x 944 x 896: 13.5 us, the tile above 19; 571 x 1264 x 768: 8.2 and 11)
             {128, 64, 2, .73f, .8f, 1.2f, 4, false, launch_as<KIND, true, 128, 64, 64, 32, 3, 128>},
         };
