@@ -99,7 +99,7 @@ struct TileOrder {
 // can be).  Workgroups go to the 8 XCDs in turn; each XCD gets an equal run of
 // neighbouring tiles, but of a weights' gradient, whose tiles are not equally
 // long, every eighth, the longest groups' first (16384 rows over 16 uneven groups,
-// 1024 x 2048 each, tiles of 128x256: in the groups' order 111 to 122 us, so 100 to 110).
+// 1024 x 2048 each, tiles of 128x256: in the groups' order a tenth longer).
 template <Kind KIND>
 __device__ __forceinline__ int tile_id(int total) {
     const int b = (int)blockIdx.x, x = b & 7, j = b >> 3, q = total >> 3, rem = total & 7;

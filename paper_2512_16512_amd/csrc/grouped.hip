@@ -48,7 +48,7 @@ double estimate_us(const Choice &c, const GroupedArgs &a) {
     if (KIND == kWgrad) {
         // The tiles of the longest group take that long in any case; it is taken to hold
         // up to three times its share (16384 rows over 16 uneven groups, 1024 x 2048 each:
-        // tiles of 256x256 95 to 129 us, 128x256 100 to 110; over equal ones 100 and 103).
+        // tiles of 256x256 101 to 120 us, 128x256 95 to 96; over equal ones 90 and 95).
         const double longest = stages * c.one * (a.G < 5 ? (1 + a.G) / 2. : 3.) + c.fixed;
         us = us > longest ? us : longest;
     }

@@ -280,57 +280,49 @@ grouped_tile_kernel(GroupedArgs p) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) acc[i][j][r] = acc[i][j][r] < 0.f ? 0.f : acc[i][j][r];
     }
-    // Results leave as whole lines past the caches, which the operands then keep:
-    // fp32 ones as they lie, four columns a lane (the weights' gradient of 16384
-    // rows over 16 groups, 1024 x 2048 each: 117 us with ordinary stores, 93); bf16
-    // ones, eight columns a lane, by way of a part of LDS of the wave's own (16384
-    // rows over 16 groups, 1024 to 2048: 98 us with ordinary stores of four columns
-    // a lane, 104 with those past the caches, half lines each, and 85 this way;
-    // e4m3 8192 x 8192 x 8192: 526 and 504).
-    if (!p.out_bf16) {
-#pragma unroll
-        for (int i = 0; i < G::TM; ++i) {
-            const int m = wm * WM + i * MI + lrow;
-            if (m >= t.m) continue;
-            float *c = reinterpret_cast<float *>(t.C) + m * p.ldc;
-#pragma unroll
-            for (int j = 0; j < G::TN; ++j) {
-                const int n = wn * WN + j * MI + lcol;
-                const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-                store_past_caches(c + n, v, t.n - n);
-            }
-        }
-        return;
-    }
+    // Results leave as whole lines past the caches, which the operands then keep, by way
+    // of a part of LDS of the wave's own.  16384 rows over 16 groups, 1024 to 2048, bf16:
+    // 98 us with ordinary stores of four columns a lane, 104 with those past the caches,
+    // half lines each, and 85 this way; e4m3 8192 x 8192 x 8192: 526 and 504.  fp32 results
+    // straight from the registers are half lines too, of which 1.4 times the bytes reach
+    // memory: weights' gradients of the same rows 105 us, so 95; of 64 groups of 64 rows,
+    // 1024 x 1024, 80 and 58.
     __syncthreads();
-    constexpr int PART = STAGES * G::STAGE_BYTES / G::NWAVES / 16 * 16, PITCH = WN * 2 + 16;   // (rows a few banks apart)
-    constexpr int FIT = PART / PITCH / MI, PASS = FIT < G::TM ? FIT : G::TM;                   // fragments' rows at once
-    static_assert(PASS > 0, "a fragment's rows fit");
-    constexpr int LANES = WN / 8;                                                              // lanes a row
-    unsigned char *own = smem + wave * PART;
-    each_index([&](auto I0) __attribute__((always_inline)) {
-        constexpr int i0 = I0 * PASS, i1 = i0 + PASS < G::TM ? i0 + PASS : G::TM;
-        each_index([&](auto I) __attribute__((always_inline)) {
-            constexpr int i = i0 + I;
+    auto store = [&](auto ZERO) __attribute__((always_inline)) {
+        typedef decltype(ZERO) T;
+        constexpr int PART = STAGES * G::STAGE_BYTES / G::NWAVES / 16 * 16;
+        constexpr int PITCH = WN * (int)sizeof(T) + 16;                             // (rows a few banks apart)
+        constexpr int FIT = PART / PITCH / MI, PASS = FIT < G::TM ? FIT : G::TM;    // fragments' rows at once
+        static_assert(PASS > 0, "a fragment's rows fit");
+        constexpr int EACH = 16 / (int)sizeof(T), LANES = WN / EACH;                // columns a lane, lanes a row
+        unsigned char *own = smem + wave * PART;
+        each_index([&](auto I0) __attribute__((always_inline)) {
+            constexpr int i0 = I0 * PASS, i1 = i0 + PASS < G::TM ? i0 + PASS : G::TM;
+            each_index([&](auto I) __attribute__((always_inline)) {
+                constexpr int i = i0 + I;
 #pragma unroll
-            for (int j = 0; j < G::TN; ++j) {
-                __bf16 v[4];
+                for (int j = 0; j < G::TN; ++j) {
+                    T v[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = (__bf16)acc[i][j][e];
-                __builtin_memcpy(__builtin_assume_aligned(own + (I * MI + lrow) * PITCH + (j * MI + lcol) * 2, 8), v, 8);
+                    for (int e = 0; e < 4; ++e) v[e] = (T)acc[i][j][e];
+                    void *to = own + (I * MI + lrow) * PITCH + (j * MI + lcol) * (int)sizeof(T);
+                    __builtin_memcpy(__builtin_assume_aligned(to, sizeof(v)), v, sizeof(v));
+                }
+            }, std::make_integer_sequence<int, i1 - i0>());
+            asm volatile("" ::: "memory");
+            const int n = wn * WN + lane % LANES * EACH;
+#pragma unroll
+            for (int q = 0; q < (i1 - i0) * MI * LANES / 64; ++q) {
+                const int row = q * (64 / LANES) + lane / LANES, m = wm * WM + i0 * MI + row;
+                T v[EACH];
+                __builtin_memcpy(v, __builtin_assume_aligned(own + row * PITCH + lane % LANES * 16, 16), 16);
+                if (m < t.m) store_past_caches(reinterpret_cast<T *>(t.C) + m * p.ldc + n, v, t.n - n);
             }
-        }, std::make_integer_sequence<int, i1 - i0>());
-        asm volatile("" ::: "memory");
-        const int n = wn * WN + lane % LANES * 8;
-#pragma unroll
-        for (int q = 0; q < (i1 - i0) * MI * LANES / 64; ++q) {
-            const int row = q * (64 / LANES) + lane / LANES, m = wm * WM + i0 * MI + row;
-            __bf16 v[8];
-            __builtin_memcpy(v, __builtin_assume_aligned(own + row * PITCH + lane % LANES * 16, 16), 16);
-            if (m < t.m) store_past_caches(reinterpret_cast<__bf16 *>(t.C) + m * p.ldc + n, v, t.n - n);
-        }
-        asm volatile("" ::: "memory");
-    }, std::make_integer_sequence<int, (G::TM + PASS - 1) / PASS>());
+            asm volatile("" ::: "memory");
+        }, std::make_integer_sequence<int, (G::TM + PASS - 1) / PASS>());
+    };
+    if (p.out_bf16) store(__bf16());
+    else store(0.f);
 }
 
 template <Kind KIND, bool WIDE, int BM, int BN, int WM, int WN, int STAGES, int KB, bool ANY = false>
@@ -368,9 +360,9 @@ const Choice *tile_choices(bool wide, int *count) {
     } else if constexpr (KIND == kWgrad) {
         static const Choice all[] = {
             // Four stages of 64 bytes, of the same LDS as two of 128, wait less for memory.
-            {256, 256, 1, 1.75f, 1.75f, 1.75f, 17, false, launch_as<KIND, false, 256, 256, 128, 64, 4, 64>},
-            {128, 256, 1, 1.05f, 1.05f, 1.05f, 8.4f, false, launch_as<KIND, false, 128, 256, 64, 64, 3, 128>},
-            {128, 128, 2, .9f, .9f, 1.4f, 8, false, launch_as<KIND, false, 128, 128, 64, 64, 2, 128>},
+            {256, 256, 1, 1.9f, 1.9f, 1.9f, 12.7f, false, launch_as<KIND, false, 256, 256, 128, 64, 4, 64>},
+            {128, 256, 1, 1.02f, 1.02f, 1.02f, 7.1f, false, launch_as<KIND, false, 128, 256, 64, 64, 3, 128>},
+            {128, 128, 2, .9f, .9f, 1.22f, 6.5f, false, launch_as<KIND, false, 128, 128, 64, 64, 2, 128>},
         };
         *count = 3;
         return all;
