@@ -33,24 +33,27 @@ double estimate_us(const Choice &c, const GroupedArgs &a) {
     }
     const double stages = k * (KIND == kFp8 ? 1 : 2) / 128, slots = 256. * c.per_cu;
     const int64_t n = (int64_t)(rows * cdiv(a.N, c.bn)), whole = (int64_t)(n / slots);
+    if (KIND == kWgrad) {
+        // Tiles of different lengths fill the ends of each other's rounds; those of the
+        // longest group, taken to hold up to 4.5 times its share, last that long in any
+        // case (16384 rows over 16 uneven groups, 1024 x 2048 each: tiles of 256x256 101 to
+        // 120 us, 128x256 95 to 96; over equal ones 90 and 95).
+        const double rounds = n / slots, second = n > 256 && c.per_cu > 1 ? (n - 256) / (slots - 256) : 0;
+        const double us = rounds >= 1 ? rounds * (stages * c.full + c.fixed) : stages * (c.one + (c.full - c.one) * second) + c.fixed;
+        const double longest = stages * c.one * (a.G < 8 ? (1 + a.G) / 2. : 4.5) + c.fixed;
+        return us > longest ? us : longest;
+    }
     const int64_t rest = n - (int64_t)(whole * slots), held = cdiv(rest, 256);
     // Weights above 64 MB are taken to come from memory in every call (100 rows over
     // 32 groups, bf16, 2048 to 1024: tiles of 64x128 34 us, 32x64 27; their stages at
     // the rate of cached weights would have been 21 and 23).
-    const bool from_memory = KIND != kWgrad && (double)a.G * a.N * a.K * (KIND == kFp8 ? 1 : 2) > 64e6;
+    const bool from_memory = (double)a.G * a.N * a.K * (KIND == kFp8 ? 1 : 2) > 64e6;
     const double one = from_memory ? c.cold : c.one, full = c.per_cu > 1 ? c.full : one;
     double us = whole * (stages * full + c.fixed);
     if (held > 0) {
         const double last = stages * (held > 1 ? one + (full - one) * (held - 1) / (c.per_cu - 1) : one) + c.fixed;
         // (where CUs hold several workgroups, those of a last, partial round begin as others end)
         us += whole > 0 && c.per_cu > 1 ? last / 2 : last;
-    }
-    if (KIND == kWgrad) {
-        // The tiles of the longest group take that long in any case; it is taken to hold
-        // up to three times its share (16384 rows over 16 uneven groups, 1024 x 2048 each:
-        // tiles of 256x256 101 to 120 us, 128x256 95 to 96; over equal ones 90 and 95).
-        const double longest = stages * c.one * (a.G < 5 ? (1 + a.G) / 2. : 3.) + c.fixed;
-        us = us > longest ? us : longest;
     }
     return us;
 }

@@ -360,9 +360,9 @@ const Choice *tile_choices(bool wide, int *count) {
     } else if constexpr (KIND == kWgrad) {
         static const Choice all[] = {
             // Four stages of 64 bytes, of the same LDS as two of 128, wait less for memory.
-            {256, 256, 1, 1.9f, 1.9f, 1.9f, 12.7f, false, launch_as<KIND, false, 256, 256, 128, 64, 4, 64>},
-            {128, 256, 1, 1.02f, 1.02f, 1.02f, 7.1f, false, launch_as<KIND, false, 128, 256, 64, 64, 3, 128>},
-            {128, 128, 2, .9f, .9f, 1.22f, 6.5f, false, launch_as<KIND, false, 128, 128, 64, 64, 2, 128>},
+            {256, 256, 1, 1.1f, 1.1f, 1.1f, 12, false, launch_as<KIND, false, 256, 256, 128, 64, 4, 64>},
+            {128, 256, 1, .81f, .81f, .81f, 7.9f, false, launch_as<KIND, false, 128, 256, 64, 64, 3, 128>},
+            {128, 128, 2, .7f, .7f, 1.18f, 7.1f, false, launch_as<KIND, false, 128, 128, 64, 64, 2, 128>},
         };
         *count = 3;
         return all;

@@ -633,6 +633,20 @@ def test_matmul_grouped_wgrad_other_tiles():
         i += n
 
 
+@pytest.mark.parametrize("T,N,K,G", [(216, 136, 920, 57), (143, 3824, 2056, 1)])
+def test_matmul_grouped_wgrad_tall_and_wide(T, N, K, G):
+    sizes, ends = uneven_groups(T, G) if G > 1 else ([T], torch.tensor([T], dtype=torch.int32))
+    a, dy = as_type(normal(25, T, K), "bf16"), as_type(normal(26, T, N), "bf16")
+    say("matmul_grouped_wgrad", T, N, K, G)
+    got = host(x.matmul_grouped_wgrad(dev(a), dev(dy), ends.cuda()))
+    i = 0
+    for g, n in enumerate(sizes):
+        p, q = a[i:i + n].double(), dy[i:i + n].double()
+        ref = p.t() @ q
+        within(got[g], ref, 2 * U * (n + 8) * (p.abs().t() @ q.abs()) + U * ref.abs(), "wgrad of group %d" % g)
+        i += n
+
+
 # ------------------------------------------------------- streams, far offsets
 
 
