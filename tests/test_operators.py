@@ -647,6 +647,25 @@ def test_matmul_grouped_wgrad_tall_and_wide(T, N, K, G):
         i += n
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("M,N", [(300, 261), (1947, 2111)])
+def test_tiles_write_their_own_columns_only(M, N, dtype):
+    """Results of tiles in rows that begin at odd addresses, beside columns that stay."""
+    K = 400
+    qa, sa, a = scaled(31, 1, M, K)
+    qb, sb, b = scaled(32, 128, N, K)
+    wide = torch.full((M, N + 10), 5.0, device="cuda", dtype=dtype)
+    say("matmul_fp8", M, N, K, dtype)
+    got = x.matmul_fp8(dev8(qa), dev(sa), dev8(qb), dev(sb), dtype=dtype, out=wide[:, 3:N + 3])
+    ref = a @ b.t()
+    bound = 2 * U * (K + 8) * (a.abs() @ b.abs().t()) + U * ref.abs()
+    if dtype == torch.bfloat16:
+        eight = [v.abs().reshape(v.shape[0], K // 8, 8).amax(2) for v in (a, b)]
+        bound += BF16 * ref.abs() + 2.0 ** -10 * (eight[0] @ eight[1].t())
+    within(host(got), ref, bound, "out")
+    assert bool((wide[:, :3] == 5).all()) and bool((wide[:, N + 3:] == 5).all())
+
+
 # ------------------------------------------------------- streams, far offsets
 
 
