@@ -298,7 +298,8 @@ xtc_status xtc_conv2d_nchw_relu(int64_t N, int64_t C, int64_t H, int64_t W,
  *   h = X + R (fp32), rstd = 1 / sqrt(sum_j h_j^2 / D + eps),
  *   Y_j = W_j * h_j * rstd, rounded once.
  *
- *  T, D       rows and columns, >= 0; either 0 is a no-op.
+ *  T, D       rows and columns, >= 0; either 0 is a no-op (with D 0, whose
+ *             means are 0/0, rstd is left as it is).
  *  X, R       device, dtype (XTC_F32 or XTC_BF16), row strides ldx, ldr.  R NULL:
  *             nothing is added.
  *  W          device, D values of w_dtype: dtype or XTC_F32.

@@ -433,7 +433,7 @@ def rmsnorm(x, weight, residual=None, eps=1e-6, quantize=False):
 
     ``x`` and ``residual`` [T, D] are float32 or bfloat16 CUDA tensors with unit column stride, ``weight`` [D] is of
     the same type or float32.  ``out`` is of x's type, or with ``quantize`` float8_e4m3fn with a float32 ``scale`` for
-    each 128 columns.  Enqueued on torch's current stream."""
+    each 128 columns.  ``rstd`` of rows without columns is NaN.  Enqueued on torch's current stream."""
     if _fast is not None:
         r = _fast.rmsnorm(x, weight, residual, eps, quantize)
         if r is not None:
@@ -449,6 +449,8 @@ def rmsnorm(x, weight, residual=None, eps=1e-6, quantize=False):
     scale = torch.empty((T, _blocks_of(D)), dtype=torch.float32, device=x.device) if quantize else None
     total = x if residual is None else torch.empty((T, D), dtype=x.dtype, device=x.device)
     rstd = torch.empty(T, dtype=torch.float32, device=x.device)
+    if D == 0:
+        rstd.fill_(float("nan"))     # the mean of nothing, 0/0 (the library's call does nothing)
     code = _dtype_code(torch, x)
     _check(xtc_rmsnorm(T, D, x.data_ptr(), _ld(x), _ptr(residual), 0 if residual is None else _ld(residual),
                        weight.data_ptr(), eps, out.data_ptr(), max(D, 1), _ptr(scale), _blocks_of(D),

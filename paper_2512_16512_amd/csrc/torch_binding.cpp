@@ -241,7 +241,8 @@ PyObject *rmsnorm(PyObject *, PyObject *const *args, Py_ssize_t n) {
     const at::Tensor &x = *t[0], &w = *t[1];
     if (!row_major(x) || !dtype_code(x, &dt)) Py_RETURN_NONE;
     const int64_t T = x.size(0), D = x.size(1);
-    if (!dtype_code(w, &dtw) || (dtw != dt && dtw != XTC_F32) || !vector_of(w, w.scalar_type(), D, x) ||
+    // (of no columns the library's call writes nothing, but there is an rstd to fill)
+    if (D == 0 || !dtype_code(w, &dtw) || (dtw != dt && dtw != XTC_F32) || !vector_of(w, w.scalar_type(), D, x) ||
         (t[2] && !matrix(*t[2], x.scalar_type(), T, D, x)))
         Py_RETURN_NONE;
     try {

@@ -792,3 +792,18 @@ def test_captured_in_a_graph():
         want = chain()
         for a, b in zip(captured, want):
             assert torch.equal(a, b)
+
+
+def test_rmsnorm_of_rows_without_columns():
+    """The mean of nothing is 0/0: rstd is NaN, whatever its memory held before."""
+    for dtype in ("f32", "bf16"):
+        for quantize in (False, True):
+            xs, w = (as_type(torch.zeros(*s), dtype).cuda() for s in ((50, 0), (0,)))
+            for value in (3.0, 7.0):
+                junk = torch.full((50,), value, device="cuda")
+                del junk
+                n = x.rmsnorm(xs, w, xs, quantize=quantize)
+                assert n.out.shape == n.residual.shape == (50, 0) and n.rstd.shape == (50,)
+                assert bool(torch.isnan(n.rstd).all())
+                dx, dw = x.rmsnorm_backward(xs, xs, w, n.rstd)
+                assert dx.shape == (50, 0) and dw.shape == (0,)
