@@ -26,7 +26,8 @@ def route(scores, top):
     p, expert = torch.topk(scores.float(), top)
     p = torch.softmax(p, 1)
     expert, which = torch.sort(expert.flatten(), stable=True)
-    ends = torch.cumsum(torch.bincount(expert, minlength=scores.shape[1]), 0).to(torch.int32)
+    # (a count of each expert's rows would be a call that waits for the GPU)
+    ends = torch.searchsorted(expert, torch.arange(scores.shape[1], device=expert.device), right=True, out_int32=True)
     return which // top, ends, p.flatten()[which], which
 
 

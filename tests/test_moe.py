@@ -74,3 +74,36 @@ def test_train_step(moe):
     assert rel(out, want.detach()) < 8 * 0.0017
     for name, got, t in zip(("x", "norm", "w1", "w2"), grads, leaf):
         assert rel(got, t.grad) < 8 * 0.0017, name
+
+
+def block_inputs(moe, T, D=256, F=384, E=6):
+    norm, router, w1, w2 = moe.weights(E, D, F)
+    g = torch.Generator().manual_seed(11)
+    x, r, dout = (torch.randn(T, D, generator=g).bfloat16().cuda() for _ in range(3))
+    return norm, router, w1, w2, x, r, dout
+
+
+def test_steps_do_not_wait_for_the_gpu(moe):
+    """The groups' ends stay on the device: nothing of a step is read back to the host."""
+    norm, router, w1, w2, x, r, dout = block_inputs(moe, 200)
+    served = moe.Served(norm, router, w1, w2)
+    torch.cuda.synchronize()
+    torch.cuda.set_sync_debug_mode("error")
+    try:
+        served.step(x, r)
+        moe.train_step(x, r, norm, router, w1, w2, dout)
+    finally:
+        torch.cuda.set_sync_debug_mode("default")
+
+
+def test_route_sorts_rows_by_expert(moe):
+    """Also where experts at either end or in between get no row."""
+    scores = torch.full((5, 7), -9.0)
+    scores[:, [1, 4]] = torch.tensor([[3.0, 1], [0, 2], [5, 4], [1, 1.5], [2, 6]])
+    token, ends, p, which = moe.route(scores.cuda(), 2)
+    assert ends.dtype == torch.int32 and ends.tolist() == [0, 5, 5, 5, 10, 10, 10]
+    assert token.tolist() == [0, 1, 2, 3, 4] * 2 and sorted(which.tolist()) == list(range(10))
+    want = torch.softmax(scores[:, [1, 4]].double(), 1).t().flatten()
+    assert torch.allclose(p.cpu().double(), want, rtol=1e-6, atol=0)
+    _, ends, _, _ = moe.route(scores[:0].cuda(), 2)
+    assert ends.tolist() == [0] * 7
