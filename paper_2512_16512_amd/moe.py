@@ -31,10 +31,12 @@ def route(scores, top):
     return which // top, ends, p.flatten()[which], which
 
 
-def combine(rows, token, p, T):
-    """The weighted sum of each token's rows, in float32."""
-    out = torch.zeros(T, rows.shape[1], dtype=torch.float32, device=rows.device)
-    return out.index_add_(0, token, rows.float() * p[:, None])
+def sum_experts(rows, which, T):
+    """The sum of each token's rows, which go to the places ``which`` of [T, top]: in the order of its experts whatever
+    the run (sums by atomics would give a token of three experts or more other bits from call to call)."""
+    placed = torch.empty_like(rows)
+    placed[which] = rows
+    return placed.view(T, rows.shape[0] // max(T, 1), rows.shape[1]).sum(1)
 
 
 def quantize_family(w):
@@ -55,11 +57,11 @@ class Served:
     def step(self, x, residual):
         """(out [T, D] float32, the sum that was normed): any number of tokens, one among them."""
         n = rmsnorm(x, self.norm, residual, quantize=True)
-        token, ends, p, _ = route(matmul_fp8(n.out, n.scale, *self.router), self.top)
+        token, ends, p, which = route(matmul_fp8(n.out, n.scale, *self.router), self.top)
         rows = n.out.view(torch.uint8)[token].view(torch.float8_e4m3fn)
         h = matmul_grouped_fp8(rows, n.scale[token], *self.w1, ends, relu=True, dtype=torch.bfloat16)
         y = matmul_grouped_fp8(*quantize_fp8(h), *self.w2, ends, dtype=torch.bfloat16)
-        return combine(y, token, p, x.shape[0]), n.residual
+        return sum_experts(y.float() * p[:, None], which, x.shape[0]), n.residual
 
 
 def train_step(x, residual, norm, router, w1, w2, dout, top=2):
@@ -67,11 +69,11 @@ def train_step(x, residual, norm, router, w1, w2, dout, top=2):
     residual's is the same), norm, w1, w2); the routing is taken as given."""
     n = rmsnorm(x, norm, residual)
     T = x.shape[0]
-    token, ends, p, _ = route(n.out.float() @ router.float().t(), top)
+    token, ends, p, which = route(n.out.float() @ router.float().t(), top)
     rows = n.out[token]
     h = matmul_grouped(rows, w1, ends, relu=True, dtype=torch.bfloat16)
     y = matmul_grouped(h, w2, ends, dtype=torch.bfloat16)
-    out = combine(y, token, p, T)
+    out = sum_experts(y.float() * p[:, None], which, T)
 
     dy = (dout.float()[token] * p[:, None]).bfloat16()
     dw2 = matmul_grouped_wgrad(h, dy, ends)
@@ -79,7 +81,7 @@ def train_step(x, residual, norm, router, w1, w2, dout, top=2):
     dh = torch.where(h > 0, dh, torch.zeros_like(dh))
     dw1 = matmul_grouped_wgrad(rows, dh, ends)
     drows = matmul_grouped(dh, w1, ends, transpose_b=True)
-    dn = torch.zeros(T, x.shape[1], device=x.device).index_add_(0, token, drows).to(x.dtype)
+    dn = sum_experts(drows, which, T).to(x.dtype)
     dx, dnorm = rmsnorm_backward(dn, n.residual, norm, n.rstd)
     return out, dx, dnorm, dw1, dw2
 

@@ -107,3 +107,23 @@ def test_route_sorts_rows_by_expert(moe):
     assert torch.allclose(p.cpu().double(), want, rtol=1e-6, atol=0)
     _, ends, _, _ = moe.route(scores[:0].cuda(), 2)
     assert ends.tolist() == [0] * 7
+
+
+def test_steps_give_the_same_bits_again(moe):
+    """A token's experts are summed in their order, however many it has."""
+    norm, router, w1, w2, x, r, dout = block_inputs(moe, 3000, 512, 128, 16)
+    served = moe.Served(norm, router, w1, w2, top=8)
+    first = served.step(x, r)
+    train = moe.train_step(x, r, norm, router, w1, w2, dout, top=8)
+    for _ in range(4):
+        assert all(torch.equal(a, b) for a, b in zip(first, served.step(x, r)))
+        assert all(torch.equal(a, b) for a, b in zip(train, moe.train_step(x, r, norm, router, w1, w2, dout, top=8)))
+
+
+def test_steps_of_no_tokens(moe):
+    norm, router, w1, w2, x, r, dout = block_inputs(moe, 0)
+    out, total = moe.Served(norm, router, w1, w2).step(x, r)
+    assert out.shape == total.shape == (0, 256) and out.dtype == torch.float32
+    out, dx, dnorm, dw1, dw2 = moe.train_step(x, r, norm, router, w1, w2, dout)
+    assert out.shape == dx.shape == (0, 256) and dw1.shape == w1.shape and dw2.shape == w2.shape
+    assert not any(bool(t.any()) for t in (dnorm, dw1, dw2))
