@@ -58,18 +58,21 @@ double estimate_us(const Choice &c, const GroupedArgs &a) {
     return us;
 }
 
+// The kernel of the least estimate among those for aligned rows, and its place:
+// tiles first, then streams.
 template <Kind KIND>
-xtc_status launch(const GroupedArgs &a, hipStream_t s) {
-    if (!aligned_rows<KIND>(a)) return launch_any<KIND>(a, s);
+const Choice *choose(const GroupedArgs &a, int *place) {
     const bool wide = KIND == kFp8 && !a.out_bf16;
     const Choice *best = nullptr;
     double least = 0;
+    int seen = 0;
     auto look = [&](const Choice *c, int count) {
-        for (int i = 0; i < count; ++i) {
+        for (int i = 0; i < count; ++i, ++seen) {
             if (c[i].dense_only && a.ends) continue;
             const double us = estimate_us<KIND>(c[i], a);
             if (!best || us < least) {
                 best = &c[i];
+                *place = seen;
                 least = us;
             }
         }
@@ -81,7 +84,28 @@ xtc_status launch(const GroupedArgs &a, hipStream_t s) {
         const Choice *streams = stream_choices<KIND>(wide, &count);
         look(streams, count);
     }
-    return best->launch(a, s);
+    return best;
+}
+
+template <Kind KIND>
+xtc_status launch(const GroupedArgs &a, hipStream_t s) {
+    int place;
+    if (!aligned_rows<KIND>(a)) return launch_any<KIND>(a, s);
+    return choose<KIND>(a, &place)->launch(a, s);
+}
+
+template <Kind KIND>
+int kernel_place(const GroupedArgs &a, int *kernels) {
+    const bool wide = KIND == kFp8 && !a.out_bf16;
+    int count = 0, place = -1;
+    tile_choices<KIND>(wide, &count);
+    *kernels = count;
+    if constexpr (KIND != kWgrad) {
+        stream_choices<KIND>(wide, &count);
+        *kernels += count;
+    }
+    if (aligned_rows<KIND>(a)) choose<KIND>(a, &place);
+    return place;
 }
 
 }  // namespace
@@ -91,5 +115,14 @@ xtc_status launch_grouped_bf16(const GroupedArgs &a, bool b_rows_n, hipStream_t 
     return b_rows_n ? launch<kBf16T>(a, s) : launch<kBf16N>(a, s);
 }
 xtc_status launch_grouped_wgrad(const GroupedArgs &a, hipStream_t s) { return launch<kWgrad>(a, s); }
+
+int grouped_kernel(const GroupedArgs &a, int kind, int *kernels) {
+    switch (kind) {
+        case kFp8: return kernel_place<kFp8>(a, kernels);
+        case kBf16N: return kernel_place<kBf16N>(a, kernels);
+        case kBf16T: return kernel_place<kBf16T>(a, kernels);
+        default: return kernel_place<kWgrad>(a, kernels);
+    }
+}
 
 }  // namespace xtc

@@ -101,4 +101,9 @@ xtc_status launch_grouped_bf16(const GroupedArgs &a, bool b_rows_n, hipStream_t 
 // bf16 A [T, K] and B [T, N]: C of group g [K, N] = A_g^T B_g
 xtc_status launch_grouped_wgrad(const GroupedArgs &a, hipStream_t s);
 
+// Which of the kernels for aligned rows a product takes (-1: the one for rows at
+// any address), and how many there are.  kind: 0 e4m3, 1 bf16 with B [K, N], 2 with
+// B [N, K], 3 a weights' gradient.
+int grouped_kernel(const GroupedArgs &a, int kind, int *kernels);
+
 }  // namespace xtc

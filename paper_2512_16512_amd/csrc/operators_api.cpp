@@ -193,4 +193,21 @@ xtc_status xtc_matmul_grouped_wgrad(int64_t G, int64_t T, int64_t N, int64_t K, 
     return launch_grouped_wgrad(a, static_cast<hipStream_t>(stream));
 }
 
+// Not part of the ABI: the kernel of a product of contiguous, 16-byte aligned
+// operands (`grouped`: with ends), as grouped_kernel() numbers them, so that the tests
+// can see that their sizes reach every one.  Pure host function.
+int32_t xtc_test_product_kernel(int32_t kind, int32_t grouped, int64_t G, int64_t T, int64_t N, int64_t K,
+                                int32_t out_bf16, int32_t *kernels) {
+    static const int32_t ends = 0;
+    GroupedArgs a = {};
+    a.T = T; a.N = (int)N; a.K = (int)K;
+    a.lda = K; a.ldb = kind == 1 || kind == 3 ? N : K;
+    a.stride_b = kind == 3 ? 0 : N * K;
+    a.ldsa = a.ldsb = scale_blocks(K); a.stride_sb = scale_blocks(N) * a.ldsb;
+    a.ldc = N; a.stride_c = N * K;
+    a.ends = grouped ? &ends : nullptr; a.G = (int)G;
+    a.out_bf16 = out_bf16;
+    return grouped_kernel(a, kind, kernels);
+}
+
 }  // extern "C"
