@@ -666,6 +666,52 @@ def test_tiles_write_their_own_columns_only(M, N, dtype):
     assert bool((wide[:, :3] == 5).all()) and bool((wide[:, N + 3:] == 5).all())
 
 
+# Rows beyond what a launch holds at once: each workgroup of the gradient takes
+# several, and the last trip is a partial one.
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,D", [(9001, 40), (7001, 600), (2501, 1100), (2301, 2100), (601, 5001), (1201, 8200)])
+def test_rmsnorm_backward_of_many_rows(T, D, dtype):
+    test_rmsnorm_backward(T, D, dtype)
+
+
+@pytest.mark.parametrize("quantize", [False, True])
+def test_rmsnorm_of_more_rows_than_one_launch(quantize):
+    """A launch holds 2^21 workgroups of four rows: the rows behind it are normed by another."""
+    T, D, first = (1 << 23) + 7, 3, (1 << 23) - 6
+    v = torch.zeros(T, D, device="cuda")
+    r = torch.zeros(T, D, device="cuda")
+    xs, w, res = norm_case(T - first, D, "f32", True, 9)
+    v[first:], r[first:] = xs.cuda(), res.cuda()
+    say("rmsnorm", T, D, quantize)
+    n = x.rmsnorm(v, dev(w), r, eps=1e-5, quantize=quantize)
+    h, rstd, y = norm_reference(xs, w, res, 1e-5)
+    rel = (D + 16) * U
+    within(host(n.rstd[first:]), rstd, rel * rstd, "rstd")
+    within(host(n.residual[first:]), h, U * h.abs() + U * (xs.double().abs() + res.double().abs()), "sum")
+    if quantize:
+        check_e4m3(n.out[first:], n.scale[first:], y, 1, rel, "last rows")
+        assert bool((n.out[:first].view(torch.uint8) == 0).all()) and bool((n.scale[:first] == 2.0 ** -126).all())
+    else:
+        within(host(n.out[first:]), y, (U + 2 * rel) * y.abs(), "last rows")
+        assert bool((n.out[:first] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [1, 128])
+def test_quantize_divides_as_the_definition_does(rows, dtype):
+    """Scales and values are the bits of fp32 divisions, amax / 448 and x / scale, the latter rounded to nearest even."""
+    M, K = 384, 1280
+    v = as_type(normal(77, M, K) * torch.exp(2 * normal(78, K)), dtype)
+    q, s = x.quantize_fp8(dev(v), block_rows=rows)
+    cut = v.float().reshape(M // rows, rows, K // 128, 128)
+    scale = cut.abs().amax((1, 3)) / torch.full((), 448.0)
+    assert torch.equal(s.cpu(), scale)
+    want = (cut / scale[:, None, :, None]).reshape(M, K).to(torch.float8_e4m3fn)
+    assert torch.equal(q.cpu().view(torch.uint8), want.view(torch.uint8))
+
+
 # ------------------------------------------------------- streams, far offsets
 
 

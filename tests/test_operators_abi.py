@@ -53,6 +53,13 @@ def test_rmsnorm_backward_workspace():
     assert x.xtc_rmsnorm_backward_workspace(4, 200) >= 4 * 200
 
 
+@pytest.mark.parametrize("T,D,slabs", [(0, 100, 0), (4, 200, 1), (5, 200, 2), (8191, 500, 1024), (8191, 1000, 768),
+                                       (8191, 2048, 1024), (8191, 4096, 768), (8191, 8192, 256), (300, 9000, 300),
+                                       (8191, 9000, 512)])
+def test_rmsnorm_backward_workspace_holds_a_row_of_sums_for_each_workgroup(T, D, slabs):
+    assert x.xtc_rmsnorm_backward_workspace(T, D) == 4 * slabs * D
+
+
 QUANT = dict(M=4, K=200, X=BAD, ldx=200, block_rows=1, Q=BAD, ldq=200, S=BAD, lds=2, dtype=0)
 
 
