@@ -11,7 +11,9 @@ current stream, nothing else); the plain calls among theirs go through
 ``_binding.so`` (csrc/torch_binding.cpp), which saves the interpreter's share
 of a call.  ``rmsnorm``, ``rmsnorm_backward``, ``quantize_fp8``, ``matmul_fp8``,
 ``matmul_grouped``, ``matmul_grouped_wgrad`` and ``matmul_grouped_fp8`` likewise
-stand for the entry points of those names.
+stand for the entry points of those names.  None of them records an autograd
+graph: a result does not require a gradient whatever its operands do, and the
+gradients are calls of their own.
 
 If the library has not been built, importing this package raises
 ``ImportError``: there is no fallback implementation.  Without the native
@@ -528,7 +530,9 @@ def matmul_fp8(a, a_scale, b, b_scale, out=None, relu=False, dtype=None):
     """``out = A @ B.T`` (``relu`` fused) of block-scaled operands: ``a`` [M, K] with ``a_scale`` [M, ceil(K/128)] and
     ``b`` [N, K] with ``b_scale`` [ceil(N/128), ceil(K/128)], float8_e4m3fn and float32, as ``quantize_fp8`` gives them
     with ``block_rows`` 1 and 128.  ``out`` [M, N] is float32 or bfloat16 (``dtype``, when allocated here; float32
-    unless given)."""
+    unless given).  A float32 result has float32 sums.  For a bfloat16 one each eight consecutive products lose what lies
+    more than 13 binary places below their largest: far below the result's rounding, but for sums that cancel, where
+    the error can be 2^-10 of the largest product of each eight."""
     if _fast is not None:
         r = _fast.matmul_fp8(a, a_scale, b, b_scale, out, relu, dtype)
         if r is not None:
@@ -604,7 +608,7 @@ def matmul_grouped_wgrad(a, dy, ends, out=None, dtype=None):
 
 def matmul_grouped_fp8(a, a_scale, b, b_scale, ends, out=None, relu=False, dtype=None):
     """``matmul_grouped`` of block-scaled operands: ``a`` [T, K] with ``a_scale`` [T, ceil(K/128)], ``b`` [G, N, K] with
-    ``b_scale`` [G, ceil(N/128), ceil(K/128)] (float8_e4m3fn and float32); ``out`` [T, N]."""
+    ``b_scale`` [G, ceil(N/128), ceil(K/128)] (float8_e4m3fn and float32); ``out`` [T, N], its sums as ``matmul_fp8``'s."""
     if _fast is not None:
         r = _fast.matmul_grouped_fp8(a, a_scale, b, b_scale, ends, out, relu, dtype)
         if r is not None:

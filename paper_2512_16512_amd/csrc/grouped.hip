@@ -37,7 +37,9 @@ double estimate_us(const Choice &c, const GroupedArgs &a) {
         // Tiles of different lengths fill the ends of each other's rounds; those of the
         // longest group, taken to hold up to 4.5 times its share, last that long in any
         // case (16384 rows over 16 uneven groups, 1024 x 2048 each: tiles of 256x256 101 to
-        // 120 us, 128x256 95 to 96; over equal ones 90 and 95).
+        // 120 us, 128x256 95 to 96; over equal ones 90 and 95).  With few groups the guess can
+        // be wrong: 11424 rows over 4, 1472 x 1088, 85 us where 128x256 takes 70, the most
+        // of 26 problems.
         const double rounds = n / slots, second = n > 256 && c.per_cu > 1 ? (n - 256) / (slots - 256) : 0;
         const double us = rounds >= 1 ? rounds * (stages * c.full + c.fixed) : stages * (c.one + (c.full - c.one) * second) + c.fixed;
         const double longest = stages * c.one * (a.G < 8 ? (1 + a.G) / 2. : 4.5) + c.fixed;
