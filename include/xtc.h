@@ -367,7 +367,9 @@ xtc_status xtc_quantize_fp8(int64_t M, int64_t K, const void *X, int64_t ldx, in
  * products, what lies more than 13 binary places below the largest is cut off,
  * 1.5e-5 of a typical result, a hundredth of its rounding.  Where large products
  * cancel it can be 2^-10 of the largest of each eight, whatever is left: sums that
- * may cancel are for XTC_F32.
+ * may cancel are for XTC_F32.  A block's two scales are multiplied first, in
+ * fp32: where that product is no normal number (below 2^-126, or an overflow), so
+ * is the result less exact, or not finite.
  *
  *  A   e4m3 M x K, row stride lda; SA its scales, one per row and 128 k, row
  *      stride ldsa.
