@@ -348,6 +348,38 @@ xtc_status xtc_rmsnorm_backward(int64_t T, int64_t D, const void *DY, int64_t ld
 int64_t xtc_rmsnorm_backward_workspace(int64_t T, int64_t D);
 
 /*
+ * xtc_layernorm -- layer norm of each row of X + R:
+ *   h = X + R (fp32), mean = sum_j h_j / D, rstd = 1 / sqrt(sum_j (h_j - mean)^2 / D + eps),
+ *   Y_j = W_j * (h_j - mean) * rstd + B_j, rounded once.
+ * B (device, D values of w_dtype) may be NULL: nothing is added.  mean and rstd are
+ * device, T fp32 values each for the gradient, or NULL.  All else, 8-bit outputs
+ * and errors among it, as for xtc_rmsnorm; sums are fp32.
+ */
+xtc_status xtc_layernorm(int64_t T, int64_t D, const void *X, int64_t ldx,
+                         const void *R, int64_t ldr, const void *W, const void *B, float eps,
+                         void *Y, int64_t ldy, float *S, int64_t lds,
+                         void *H, int64_t ldh, float *mean, float *rstd,
+                         xtc_dtype dtype, xtc_dtype w_dtype, xtc_dtype out_dtype, void *stream);
+
+/*
+ * xtc_layernorm_backward -- the layer norm's gradient.  X is what was normalised and
+ * mean, rstd what xtc_layernorm kept; with xh = (X - mean) * rstd and g = DY * W,
+ *   DX = rstd * (g - sum_j g_j / D - xh * sum_j(g_j xh_j) / D) + DR,
+ *   DW_j = sum_t DY_tj xh_tj,  DB_j = sum_t DY_tj.
+ * DB: device, D fp32 values, like DW.  All else as for xtc_rmsnorm_backward, with
+ * xtc_layernorm_backward_workspace(T, D).
+ */
+xtc_status xtc_layernorm_backward(int64_t T, int64_t D, const void *DY, int64_t lddy,
+                                  const void *X, int64_t ldx, const void *W,
+                                  const float *mean, const float *rstd,
+                                  const void *DR, int64_t lddr, void *DX, int64_t lddx,
+                                  float *DW, float *DB, void *workspace, int64_t workspace_bytes,
+                                  xtc_dtype dtype, xtc_dtype w_dtype, void *stream);
+
+/* Bytes of workspace for T rows of D columns; -1 for extents outside the limits.  Pure host function. */
+int64_t xtc_layernorm_backward_workspace(int64_t T, int64_t D);
+
+/*
  * xtc_quantize_fp8 -- X [M, K] (dtype, row stride ldx) as e4m3 values Q (row
  * stride ldq) and scales S (row stride lds): one for each block_rows x 128
  * values, block_rows 1 (activations) or 128 (weights), else XTC_ERR_BAD_SHAPE.

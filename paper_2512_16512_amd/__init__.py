@@ -113,6 +113,14 @@ def _load():
     lib.xtc_rmsnorm_backward.restype = i32
     lib.xtc_rmsnorm_backward_workspace.argtypes = [i64, i64]
     lib.xtc_rmsnorm_backward_workspace.restype = i64
+    lib.xtc_layernorm.argtypes = [i64, i64, vp, i64, vp, i64, vp, vp, f32, vp, i64, vp, i64, vp, i64, vp, vp, i32, i32,
+                                  i32, vp]
+    lib.xtc_layernorm.restype = i32
+    lib.xtc_layernorm_backward.argtypes = [i64, i64, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp, i64, i32,
+                                           i32, vp]
+    lib.xtc_layernorm_backward.restype = i32
+    lib.xtc_layernorm_backward_workspace.argtypes = [i64, i64]
+    lib.xtc_layernorm_backward_workspace.restype = i64
     lib.xtc_quantize_fp8.argtypes = [i64, i64, vp, i64, i64, vp, i64, vp, i64, i32, vp]
     lib.xtc_quantize_fp8.restype = i32
     lib.xtc_matmul_fp8.argtypes = [i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, i32, i32, vp]
@@ -166,7 +174,8 @@ _fast = _load_binding()
 
 # Every symbol include/xtc.h declares.
 EXPORTS = ("xtc_matmul", "xtc_conv2d_nchw", "xtc_matmul_relu", "xtc_conv2d_nchw_relu",
-           "xtc_rmsnorm", "xtc_rmsnorm_backward", "xtc_rmsnorm_backward_workspace", "xtc_quantize_fp8",
+           "xtc_rmsnorm", "xtc_rmsnorm_backward", "xtc_rmsnorm_backward_workspace", "xtc_layernorm",
+           "xtc_layernorm_backward", "xtc_layernorm_backward_workspace", "xtc_quantize_fp8",
            "xtc_matmul_fp8", "xtc_matmul_grouped", "xtc_matmul_grouped_wgrad", "xtc_matmul_grouped_fp8",
            "xtc_default_schedule", "xtc_sched_occupancy", "xtc_sched_check",
            "xtc_sched_list", "xtc_status_str", "xtc_last_hip_error", "xtc_conv_max_k",
@@ -213,6 +222,22 @@ def xtc_rmsnorm_backward(T, D, DY, lddy, X, ldx, W, rstd, DR, lddr, DX, lddx, DW
 
 def xtc_rmsnorm_backward_workspace(T, D) -> int:
     return _lib.xtc_rmsnorm_backward_workspace(T, D)
+
+
+def xtc_layernorm(T, D, X, ldx, R, ldr, W, B, eps, Y, ldy, S, lds, H, ldh, mean, rstd, dtype, w_dtype, out_dtype,
+                  stream=0) -> int:
+    return _lib.xtc_layernorm(T, D, X, ldx, R, ldr, W, B, eps, Y, ldy, S, lds, H, ldh, mean, rstd, dtype, w_dtype,
+                              out_dtype, stream)
+
+
+def xtc_layernorm_backward(T, D, DY, lddy, X, ldx, W, mean, rstd, DR, lddr, DX, lddx, DW, DB, workspace,
+                           workspace_bytes, dtype, w_dtype, stream=0) -> int:
+    return _lib.xtc_layernorm_backward(T, D, DY, lddy, X, ldx, W, mean, rstd, DR, lddr, DX, lddx, DW, DB, workspace,
+                                       workspace_bytes, dtype, w_dtype, stream)
+
+
+def xtc_layernorm_backward_workspace(T, D) -> int:
+    return _lib.xtc_layernorm_backward_workspace(T, D)
 
 
 def xtc_quantize_fp8(M, K, X, ldx, block_rows, Q, ldq, S, lds, dtype, stream=0) -> int:
@@ -379,6 +404,9 @@ def conv2d_nchw(x, w, stride=1, pad=0, out=None, sched=None, relu=False):
 # --------------------------------------- norms, 8-bit and grouped products
 
 
+#: What ``layernorm`` returns: as ``RmsNorm``, and each row's ``mean`` (float32).
+LayerNorm = namedtuple("LayerNorm", "out scale residual mean rstd")
+
 #: What ``rmsnorm`` returns.  ``out``: the normed rows, in x's type or as
 #: float8_e4m3fn with ``scale`` (else None); ``residual``: x plus the residual
 #: (x itself when there was none); ``rstd``: one float32 a row, for the gradient.
@@ -423,6 +451,11 @@ def _ptr(t):
 
 def _blocks_of(n):
     return -(-n // 128)
+
+
+def _on(torch, device):
+    """The context in which launches go to ``device``."""
+    return torch.cuda.device(device)
 
 
 def _check(st, where):
@@ -488,6 +521,72 @@ def rmsnorm_backward(dy, x, weight, rstd, dresidual=None):
                                 _dtype_code(torch, x), _dtype_code(torch, weight), _stream(torch, x.device)),
            "xtc_rmsnorm_backward")
     return dx, dweight
+
+
+def layernorm(x, weight, bias=None, residual=None, eps=1e-5, quantize=False):
+    """Layer norm of each row of ``x`` (plus ``residual``): ``LayerNorm(out, scale, residual, mean, rstd)``.
+
+    Operands and results as for ``rmsnorm``; ``bias`` [D] is of the weight's type.  ``mean`` and ``rstd`` of rows
+    without columns are NaN.  Enqueued on torch's current stream."""
+    if _fast is not None:
+        r = _fast.layernorm(x, weight, bias, residual, eps, quantize)
+        if r is not None:
+            return LayerNorm._make(r)
+    import torch
+    kinds = (torch.float32, torch.bfloat16)
+    _matrix(x, "x", kinds)
+    T, D = x.shape
+    _vector(weight, "weight", (torch.float32, x.dtype), D, x.device)
+    if bias is not None:
+        _vector(bias, "bias", (weight.dtype,), D, x.device)
+    if residual is not None:
+        _matrix(residual, "residual", (x.dtype,), (T, D), x.device)
+    out = torch.empty((T, D), dtype=torch.float8_e4m3fn if quantize else x.dtype, device=x.device)
+    scale = torch.empty((T, _blocks_of(D)), dtype=torch.float32, device=x.device) if quantize else None
+    total = x if residual is None else torch.empty((T, D), dtype=x.dtype, device=x.device)
+    mean, rstd = (torch.empty(T, dtype=torch.float32, device=x.device) for _ in range(2))
+    if D == 0:
+        mean.fill_(float("nan"))     # the means of nothing, 0/0 (the library's call does nothing)
+        rstd.fill_(float("nan"))
+    code = _dtype_code(torch, x)
+    with _on(torch, x.device):
+        _check(xtc_layernorm(T, D, x.data_ptr(), _ld(x), _ptr(residual), 0 if residual is None else _ld(residual),
+                             weight.data_ptr(), _ptr(bias), eps, out.data_ptr(), max(D, 1), _ptr(scale), _blocks_of(D),
+                             None if residual is None else total.data_ptr(), D, mean.data_ptr(), rstd.data_ptr(), code,
+                             _dtype_code(torch, weight), XTC_FP8 if quantize else code, _stream(torch, x.device)),
+               "xtc_layernorm")
+    return LayerNorm(out, scale, total, mean, rstd)
+
+
+def layernorm_backward(dy, x, weight, mean, rstd, dresidual=None):
+    """``(dx, dweight, dbias)`` of ``layernorm``: ``x`` is the sum that was normed (its result's ``residual``),
+    ``dresidual`` the gradient that reaches that sum from elsewhere.  ``dx`` (x's type) is the gradient of x and of the
+    residual, ``dweight`` and ``dbias`` are float32."""
+    if _fast is not None:
+        r = _fast.layernorm_backward(dy, x, weight, mean, rstd, dresidual)
+        if r is not None:
+            return r
+    import torch
+    _matrix(x, "x", (torch.float32, torch.bfloat16))
+    T, D = x.shape
+    _matrix(dy, "dy", (x.dtype,), (T, D), x.device)
+    _vector(weight, "weight", (torch.float32, x.dtype), D, x.device)
+    _vector(mean, "mean", (torch.float32,), T, x.device)
+    _vector(rstd, "rstd", (torch.float32,), T, x.device)
+    if dresidual is not None:
+        _matrix(dresidual, "dresidual", (x.dtype,), (T, D), x.device)
+    dx = torch.empty((T, D), dtype=x.dtype, device=x.device)
+    dweight, dbias = (torch.empty(D, dtype=torch.float32, device=x.device) for _ in range(2))
+    size = xtc_layernorm_backward_workspace(T, D)
+    work = torch.empty(max(size, 0), dtype=torch.uint8, device=x.device)
+    with _on(torch, x.device):
+        _check(xtc_layernorm_backward(T, D, dy.data_ptr(), _ld(dy), x.data_ptr(), _ld(x), weight.data_ptr(),
+                                      mean.data_ptr(), rstd.data_ptr(), _ptr(dresidual),
+                                      0 if dresidual is None else _ld(dresidual), dx.data_ptr(), max(D, 1),
+                                      dweight.data_ptr(), dbias.data_ptr(), work.data_ptr(), size,
+                                      _dtype_code(torch, x), _dtype_code(torch, weight), _stream(torch, x.device)),
+               "xtc_layernorm_backward")
+    return dx, dweight, dbias
 
 
 def quantize_fp8(x, block_rows=1):

@@ -1,13 +1,18 @@
-// Root-mean-square norm with the residual's addition, its gradient, and the
-// conversion of rows and blocks to e4m3 with a scale.
+// Root-mean-square norm and layer norm (CENTER) with the residual's addition, their
+// gradients, and the conversion of rows and blocks to e4m3 with a scale.
 //
 //   h = x + r, rstd = 1 / sqrt(mean_j h_j^2 + eps), y_j = w_j h_j rstd
+//   centred: d = h - mean_j h_j, rstd = 1 / sqrt(mean_j d_j^2 + eps), y_j = w_j d_j rstd + b_j
 //
 // with h and every sum in fp32.  In 8 bits the 128 values of a block share
 // s = max(amax / 448, 2^-126) and are rounded from y / s.
 //
-// The gradient, with xh = h rstd and g = dy w:
+// The gradient, with xh = h rstd (centred: d rstd) and g = dy w:
 //   dx = rstd (g - xh mean_j(g_j xh_j)) + dr,   dw_j = sum_t dy_tj xh_tj
+//   centred: dx = rstd (g - mean_j g_j - xh mean_j(g_j xh_j)) + dr,   db_j = sum_t dy_tj
+//
+// The centred sum of squares is taken from the differences, in a second pass over
+// registers: mean(h^2) - mean(h)^2 loses what a large mean leaves of 24 bits.
 #include <type_traits>
 
 #include "operators.h"
@@ -76,8 +81,8 @@ struct RowTeam {
     }
 };
 
-template <typename T, bool QUANT, int NT, int NV>
-__global__ void __launch_bounds__(RowTeam<NT>::THREADS) rmsnorm_kernel(NormArgs p) {
+template <typename T, bool QUANT, bool CENTER, int NT, int NV>
+__global__ void __launch_bounds__(RowTeam<NT>::THREADS) norm_kernel(NormArgs p) {
     typedef RowTeam<NT> Team;
     __shared__ float scratch[NT / 64];
     const int tid = threadIdx.x % NT, D = p.D;
@@ -99,9 +104,23 @@ __global__ void __launch_bounds__(RowTeam<NT>::THREADS) rmsnorm_kernel(NormArgs 
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             h[v][i] = r ? rx[v].at(i) + rr[v].at(i) : rx[v].at(i);
-            sum += h[v][i] * h[v][i];
+            sum += CENTER ? h[v][i] : h[v][i] * h[v][i];
         }
     sum = Team::sum(sum, scratch);
+    float mean = 0.f;
+    if constexpr (CENTER) {
+        mean = sum / (float)D;
+        sum = 0.f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float d = (v * NT + tid) * 8 + i < D ? h[v][i] - mean : 0.f;
+                sum += d * d;
+            }
+        sum = Team::sum(sum, scratch);
+        if (tid == 0 && p.mean) p.mean[t] = mean;
+    }
     const float rstd = 1.f / sqrtf(sum / (float)D + p.eps);
     if (tid == 0 && p.rstd) p.rstd[t] = rstd;
 #pragma unroll
@@ -109,10 +128,15 @@ __global__ void __launch_bounds__(RowTeam<NT>::THREADS) rmsnorm_kernel(NormArgs 
         const int c = (v * NT + tid) * 8, valid = D - c;
         const Raw8<float> w = raw_weight(p.W, p.w_f32, x, c, valid);
         if (p.H) store8(static_cast<T *>(p.H) + t * p.ldh + c, valid, h[v]);
+        Raw8<float> b = {};
+        if constexpr (CENTER) {
+            if (p.B) b = raw_weight(p.B, p.w_f32, x, c, valid);
+        }
         float y[8], amax = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            y[i] = h[v][i] * rstd * w.v[i];
+            y[i] = CENTER ? (h[v][i] - mean) * rstd * w.v[i] + b.v[i] : h[v][i] * rstd * w.v[i];
+            // (columns past the end, which would be b - mean rstd w, are zeros already: w and b are)
             if constexpr (QUANT) amax = fmaxf(amax, finite_abs(y[i]));
         }
         if constexpr (QUANT) {
@@ -125,10 +149,10 @@ __global__ void __launch_bounds__(RowTeam<NT>::THREADS) rmsnorm_kernel(NormArgs 
     }
 }
 
-// A workgroup per row, any number of columns: one pass for the sum of
-// squares, another that reads the row again.
-template <typename T, bool QUANT>
-__global__ void __launch_bounds__(kThreads) rmsnorm_loop_kernel(NormArgs p) {
+// A workgroup per row, any number of columns: a pass for the sum of squares
+// (CENTER: one for the mean before it), another that reads the row again.
+template <typename T, bool QUANT, bool CENTER>
+__global__ void __launch_bounds__(kThreads) norm_loop_kernel(NormArgs p) {
     __shared__ float scratch[kThreads / 64];
     const int tid = threadIdx.x, D = p.D;
     for (int64_t t = blockIdx.x; t < p.T; t += gridDim.x) {
@@ -143,12 +167,26 @@ __global__ void __launch_bounds__(kThreads) rmsnorm_loop_kernel(NormArgs p) {
                 for (int i = 0; i < 8; ++i) h[i] += q[i];
             }
         };
-        float sum = 0.f;
+        float sum = 0.f, mean = 0.f;
+        if constexpr (CENTER) {
+            for (int c = tid * 8; c < D; c += kStep) {
+                float h[8];
+                load_h(c, h);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum += h[i];
+            }
+            mean = group_sum(sum, scratch) / (float)D;
+            if (tid == 0 && p.mean) p.mean[t] = mean;
+            sum = 0.f;
+        }
         for (int c = tid * 8; c < D; c += kStep) {
             float h[8];
             load_h(c, h);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum += h[i] * h[i];
+            for (int i = 0; i < 8; ++i) {
+                const float d = CENTER ? (c + i < D ? h[i] - mean : 0.f) : h[i];
+                sum += d * d;
+            }
         }
         sum = group_sum(sum, scratch);
         const float rstd = 1.f / sqrtf(sum / (float)D + p.eps);
@@ -156,12 +194,15 @@ __global__ void __launch_bounds__(kThreads) rmsnorm_loop_kernel(NormArgs p) {
         // (whole trips: the lanes that share a block's scale stay together)
         for (int c0 = 0; c0 < D; c0 += kStep) {
             const int c = c0 + tid * 8, valid = D - c;
-            float h[8], w[8], y[8];
+            float h[8], w[8], b[8] = {}, y[8];
             load_h(c, h);
             load_weight(p.W, p.w_f32, x, c, valid, w);
+            if constexpr (CENTER) {
+                if (p.B) load_weight(p.B, p.w_f32, x, c, valid, b);
+            }
             if (p.H) store8(static_cast<T *>(p.H) + t * p.ldh + c, valid, h);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = h[i] * rstd * w[i];
+            for (int i = 0; i < 8; ++i) y[i] = CENTER ? (h[i] - mean) * rstd * w[i] + b[i] : h[i] * rstd * w[i];
             if constexpr (QUANT) {
                 float amax = 0.f;
 #pragma unroll
@@ -177,19 +218,20 @@ __global__ void __launch_bounds__(kThreads) rmsnorm_loop_kernel(NormArgs p) {
 }
 
 // The gradient in one pass: team by team, rows t, t + teams, ...; a thread keeps
-// the sums over its rows of its columns' part of DW, and the workgroup leaves
-// one row of partial sums.  The next row is on its way while one is computed.
+// the sums over its rows of its columns' part of DW (CENTER: and of DB), and the
+// workgroup leaves one row of partial sums (CENTER: of 2D, DW's first).  The next row is on its way while one is computed.
 // 8191 x 2048 bf16, bound by memory: 28.6 us, 4.7 TB/s; DX and DW by kernels of
 // their own, which read the rows twice, took 151 us.
-template <typename T, int NT, int NV>
-__global__ void __launch_bounds__(RowTeam<NT>::THREADS) rmsnorm_backward_kernel(NormBackwardArgs p) {
+template <typename T, bool CENTER, int NT, int NV>
+__global__ void __launch_bounds__(RowTeam<NT>::THREADS) norm_backward_kernel(NormBackwardArgs p) {
     typedef RowTeam<NT> Team;
     __shared__ float scratch[NT / 64];
     __shared__ float sums[NT == 64 ? 3 * 64 * NV * 8 : 1];   // of the workgroup's other teams
+    constexpr int NB = CENTER ? NV : 1;
     const int tid = threadIdx.x % NT, team = threadIdx.x / NT, D = p.D;
     const int64_t step = (int64_t)gridDim.x * Team::ROWS;
     Raw8<T> rx[NV], ry[NV], rr[NV];
-    float w[NV][8], dw[NV][8], rstd_next = 0.f;
+    float w[NV][8], dw[NV][8], db[NB][8], rstd_next = 0.f, mean_next = 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         const int c = (v * NT + tid) * 8;
@@ -198,6 +240,7 @@ __global__ void __launch_bounds__(RowTeam<NT>::THREADS) rmsnorm_backward_kernel(
         for (int i = 0; i < 8; ++i) {
             w[v][i] = q.v[i];
             dw[v][i] = 0.f;
+            if constexpr (CENTER) db[v][i] = 0.f;
         }
     }
     auto fetch = [&](int64_t t) {
@@ -209,81 +252,103 @@ __global__ void __launch_bounds__(RowTeam<NT>::THREADS) rmsnorm_backward_kernel(
             if (p.DR) rr[v] = raw8(static_cast<const T *>(p.DR) + t * p.lddr + c, valid);
         }
         rstd_next = t < p.T ? p.rstd[t] : 0.f;
+        if constexpr (CENTER) mean_next = t < p.T ? p.mean[t] : 0.f;
     };
     // (every team of a workgroup takes part in every trip: the sums below have barriers)
     int64_t t = (int64_t)blockIdx.x * Team::ROWS + team;
     fetch(t);
     for (int64_t t0 = (int64_t)blockIdx.x * Team::ROWS; t0 < p.T; t0 += step, t += step) {
-        const float rstd = rstd_next;
-        float h[NV][8], g[NV][8], d[NV][8], sum = 0.f;
+        const float rstd = rstd_next, centre = mean_next;
+        float h[NV][8], g[NV][8], d[NV][8], sum = 0.f, sum_g = 0.f;
 #pragma unroll
         for (int v = 0; v < NV; ++v)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                h[v][i] = rx[v].at(i) * rstd;
+                // (of columns past the end y and w are zeros, whatever h)
+                h[v][i] = CENTER ? (rx[v].at(i) - centre) * rstd : rx[v].at(i) * rstd;
                 const float y = ry[v].at(i);
                 dw[v][i] += y * h[v][i];
+                if constexpr (CENTER) db[v][i] += y;
                 g[v][i] = y * w[v][i];
+                if constexpr (CENTER) sum_g += g[v][i];
                 d[v][i] = p.DR ? rr[v].at(i) : 0.f;
                 sum += g[v][i] * h[v][i];
             }
         fetch(t + step);
         const float mean = Team::sum(sum, scratch) / (float)D;
+        float mean_g = 0.f;
+        if constexpr (CENTER) mean_g = Team::sum(sum_g, scratch) / (float)D;
         if (t < p.T) {
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 const int c = (v * NT + tid) * 8;
                 float o[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) o[i] = d[v][i] + rstd * (g[v][i] - h[v][i] * mean);
+                for (int i = 0; i < 8; ++i) o[i] = d[v][i] + rstd * (CENTER ? g[v][i] - mean_g - h[v][i] * mean : g[v][i] - h[v][i] * mean);
                 store8(static_cast<T *>(p.DX) + t * p.lddx + c, D - c, o);
             }
         }
     }
-    if constexpr (NT == 64) {
-        if (team > 0) {
+    // the other teams' sums are added, and the workgroup's row of them written
+    auto leave = [&](auto &sum, float *to) __attribute__((always_inline)) {
+        if constexpr (NT == 64) {
+            if (team > 0) {
 #pragma unroll
-            for (int v = 0; v < NV; ++v)
+                for (int v = 0; v < NV; ++v)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sums[((team - 1) * NV * 8 + v * 8 + i) * 64 + tid] = dw[v][i];
+                    for (int i = 0; i < 8; ++i) sums[((team - 1) * NV * 8 + v * 8 + i) * 64 + tid] = sum[v][i];
+            }
+            __syncthreads();
+            if (team == 0) {
+#pragma unroll
+                for (int v = 0; v < NV; ++v)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+#pragma unroll
+                        for (int q = 0; q < 3; ++q) sum[v][i] += sums[(q * NV * 8 + v * 8 + i) * 64 + tid];
+            }
         }
+        if (NT > 64 || team == 0) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int c = (v * NT + tid) * 8;
+                store8(to + c, D - c, sum[v]);
+            }
+        }
+    };
+    float *to = p.partial + (int64_t)blockIdx.x * D * (CENTER ? 2 : 1);
+    leave(dw, to);
+    if constexpr (CENTER) {
         __syncthreads();
-        if (team > 0) return;
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-#pragma unroll
-                for (int q = 0; q < 3; ++q) dw[v][i] += sums[(q * NV * 8 + v * 8 + i) * 64 + tid];
-    }
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const int c = (v * NT + tid) * 8;
-        store8(p.partial + (int64_t)blockIdx.x * D + c, D - c, dw[v]);
+        leave(db, to + D);
     }
 }
 
 // Rows of more columns than registers hold: DX and DW by kernels of their own, which
 // read X and DY three times in all (4096 x 16384 bf16: 311 us, 1.7 TB/s of what one
 // pass would move; 4096 x 8192 in one pass 64 us, 4.2 TB/s).
-template <typename T>
-__global__ void __launch_bounds__(kThreads) rmsnorm_dx_kernel(NormBackwardArgs p) {
+template <typename T, bool CENTER>
+__global__ void __launch_bounds__(kThreads) norm_dx_kernel(NormBackwardArgs p) {
     __shared__ float scratch[kThreads / 64];
     const int tid = threadIdx.x, D = p.D;
     for (int64_t t = blockIdx.x; t < p.T; t += gridDim.x) {
         const T *x = static_cast<const T *>(p.X) + t * p.ldx;
         const T *dy = static_cast<const T *>(p.DY) + t * p.lddy;
-        const float rstd = p.rstd[t];
-        float sum = 0.f;
+        const float rstd = p.rstd[t], centre = CENTER ? p.mean[t] : 0.f;
+        float sum = 0.f, sum_g = 0.f;
         for (int c = tid * 8; c < D; c += kStep) {
             float h[8], g[8], w[8];
             load8(x + c, D - c, h);
             load8(dy + c, D - c, g);
             load_weight(p.W, p.w_f32, x, c, D - c, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum += (g[i] * w[i]) * (h[i] * rstd);
+            for (int i = 0; i < 8; ++i) {
+                sum += (g[i] * w[i]) * ((CENTER ? h[i] - centre : h[i]) * rstd);
+                if constexpr (CENTER) sum_g += g[i] * w[i];
+            }
         }
         const float mean = group_sum(sum, scratch) / (float)D;
+        const float mean_g = CENTER ? group_sum(sum_g, scratch) / (float)D : 0.f;
         for (int c = tid * 8; c < D; c += kStep) {
             float h[8], g[8], w[8], d[8];
             load8(x + c, D - c, h);
@@ -292,7 +357,8 @@ __global__ void __launch_bounds__(kThreads) rmsnorm_dx_kernel(NormBackwardArgs p
             if (p.DR) load8(static_cast<const T *>(p.DR) + t * p.lddr + c, D - c, d);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float v = rstd * (g[i] * w[i] - h[i] * rstd * mean);
+                const float v = CENTER ? rstd * (g[i] * w[i] - mean_g - (h[i] - centre) * rstd * mean)
+                                       : rstd * (g[i] * w[i] - h[i] * rstd * mean);
                 d[i] = p.DR ? d[i] + v : v;
             }
             store8(static_cast<T *>(p.DX) + t * p.lddx + c, D - c, d);
@@ -300,35 +366,42 @@ __global__ void __launch_bounds__(kThreads) rmsnorm_dx_kernel(NormBackwardArgs p
     }
 }
 
-// Sums of dy * xh over the slab blockIdx.y of rows.
-template <typename T>
-__global__ void __launch_bounds__(kThreads) rmsnorm_dw_kernel(NormBackwardArgs p) {
+// Sums of dy * xh (CENTER: and of dy) over the slab blockIdx.y of rows.
+template <typename T, bool CENTER>
+__global__ void __launch_bounds__(kThreads) norm_dw_kernel(NormBackwardArgs p) {
     const int c = (blockIdx.x * kThreads + threadIdx.x) * 8, valid = p.D - c;
     if (valid <= 0) return;
-    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0}, sum_y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     for (int64_t t = blockIdx.y; t < p.T; t += gridDim.y) {
         float h[8], g[8];
         load8(static_cast<const T *>(p.X) + t * p.ldx + c, valid, h);
         load8(static_cast<const T *>(p.DY) + t * p.lddy + c, valid, g);
-        const float rstd = p.rstd[t];
+        const float rstd = p.rstd[t], centre = CENTER ? p.mean[t] : 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum[i] += g[i] * (h[i] * rstd);
+        for (int i = 0; i < 8; ++i) {
+            sum[i] += g[i] * ((CENTER ? h[i] - centre : h[i]) * rstd);
+            if constexpr (CENTER) sum_y[i] += g[i];
+        }
     }
-    store8(p.partial + (int64_t)blockIdx.y * p.D + c, valid, sum);
+    float *to = p.partial + (int64_t)blockIdx.y * p.D * (CENTER ? 2 : 1) + c;
+    store8(to, valid, sum);
+    if constexpr (CENTER) store8(to + p.D, valid, sum_y);
 }
 
 // Column sums of the slabs: sixteen columns a workgroup, 64 runs of slabs, each
 // in its order, joined by halves (1024 rows of 2048 sums: 5 us, a few trips to
 // memory and as many barriers).
 constexpr int kJoinColumns = 16, kJoinThreads = 1024;
-__global__ void __launch_bounds__(kJoinThreads) rmsnorm_dw_join_kernel(const float *partial, int slabs, int D, float *DW) {
+__global__ void __launch_bounds__(kJoinThreads) norm_dw_join_kernel(const float *partial, int slabs, int D, float *DW, float *DB) {
     __shared__ float s[kJoinThreads];
-    const int c = blockIdx.x * kJoinColumns + threadIdx.x % kJoinColumns, run = threadIdx.x / kJoinColumns;
+    const int run = threadIdx.x / kJoinColumns;
+    // (with DB: 2D sums a slab)
+    const int64_t c = (int64_t)blockIdx.x * kJoinColumns + threadIdx.x % kJoinColumns, columns = DB ? 2 * (int64_t)D : D;
     constexpr int RUNS = kJoinThreads / kJoinColumns;
     float sum = 0.f;
-    if (c < D) {
+    if (c < columns) {
 #pragma unroll 8
-        for (int g = run; g < slabs; g += RUNS) sum += partial[(int64_t)g * D + c];
+        for (int g = run; g < slabs; g += RUNS) sum += partial[g * columns + c];
     }
     s[threadIdx.x] = sum;
 #pragma unroll
@@ -336,7 +409,7 @@ __global__ void __launch_bounds__(kJoinThreads) rmsnorm_dw_join_kernel(const flo
         __syncthreads();
         if (run < half) s[threadIdx.x] += s[threadIdx.x + half * kJoinColumns];
     }
-    if (run == 0 && c < D) DW[c] = s[threadIdx.x];
+    if (run == 0 && c < columns) (c < D ? DW : DB - D)[c] = s[threadIdx.x];
 }
 
 // e4m3 with a scale per 1 x 128 block: sixteen lanes a block.  Bound by memory:
@@ -454,11 +527,14 @@ int norm_backward_slabs(int64_t T, int64_t D) {
     return (int)(groups < most ? groups : most);
 }
 
-xtc_status launch_rmsnorm(const NormArgs &a, xtc_dtype dtype, bool quantize, hipStream_t s) {
+namespace {
+
+template <bool CENTER>
+xtc_status launch_norm(const NormArgs &a, xtc_dtype dtype, bool quantize, hipStream_t s) {
     const bool done = with_team(a.D, [&](auto nt, auto nv) {
         constexpr int NT = nt(), NV = nv();
-        const auto kernel = dtype == XTC_F32 ? (quantize ? rmsnorm_kernel<float, true, NT, NV> : rmsnorm_kernel<float, false, NT, NV>)
-                                             : (quantize ? rmsnorm_kernel<Bf16, true, NT, NV> : rmsnorm_kernel<Bf16, false, NT, NV>);
+        const auto kernel = dtype == XTC_F32 ? (quantize ? norm_kernel<float, true, CENTER, NT, NV> : norm_kernel<float, false, CENTER, NT, NV>)
+                                             : (quantize ? norm_kernel<Bf16, true, CENTER, NT, NV> : norm_kernel<Bf16, false, CENTER, NT, NV>);
         constexpr int ROWS = RowTeam<NT>::ROWS;
         const int64_t groups = (a.T + ROWS - 1) / ROWS;
         // (a launch has fewer than 2^32 threads)
@@ -473,34 +549,53 @@ xtc_status launch_rmsnorm(const NormArgs &a, xtc_dtype dtype, bool quantize, hip
             b.S = static_cast<float *>(on(a.S, t0 * a.lds * 4));
             b.H = on(a.H, t0 * a.ldh * e);
             b.rstd = static_cast<float *>(on(a.rstd, t0 * 4));
+            b.mean = static_cast<float *>(on(a.mean, t0 * 4));
             kernel<<<(unsigned)((b.T + ROWS - 1) / ROWS), RowTeam<NT>::THREADS, 0, s>>>(b);
         }
     });
     if (!done) {
-        const auto kernel = dtype == XTC_F32 ? (quantize ? rmsnorm_loop_kernel<float, true> : rmsnorm_loop_kernel<float, false>)
-                                             : (quantize ? rmsnorm_loop_kernel<Bf16, true> : rmsnorm_loop_kernel<Bf16, false>);
+        const auto kernel = dtype == XTC_F32 ? (quantize ? norm_loop_kernel<float, true, CENTER> : norm_loop_kernel<float, false, CENTER>)
+                                             : (quantize ? norm_loop_kernel<Bf16, true, CENTER> : norm_loop_kernel<Bf16, false, CENTER>);
         kernel<<<grid_of(a.T), kThreads, 0, s>>>(a);
     }
     return hip_status(hipGetLastError());
 }
 
-xtc_status launch_rmsnorm_backward(const NormBackwardArgs &a, xtc_dtype dtype, hipStream_t s) {
+template <bool CENTER>
+xtc_status launch_norm_backward(const NormBackwardArgs &a, xtc_dtype dtype, hipStream_t s) {
     const int slabs = norm_backward_slabs(a.T, a.D);
     if (a.T > 0) {
         const bool done = with_backward_team(a.D, [&](auto nt, auto nv) {
             constexpr int NT = nt(), NV = nv();
-            const auto kernel = dtype == XTC_F32 ? rmsnorm_backward_kernel<float, NT, NV> : rmsnorm_backward_kernel<Bf16, NT, NV>;
+            const auto kernel = dtype == XTC_F32 ? norm_backward_kernel<float, CENTER, NT, NV> : norm_backward_kernel<Bf16, CENTER, NT, NV>;
             kernel<<<(unsigned)slabs, RowTeam<NT>::THREADS, 0, s>>>(a);
         });
         if (!done) {
-            const auto dx = dtype == XTC_F32 ? rmsnorm_dx_kernel<float> : rmsnorm_dx_kernel<Bf16>;
-            const auto dw = dtype == XTC_F32 ? rmsnorm_dw_kernel<float> : rmsnorm_dw_kernel<Bf16>;
+            const auto dx = dtype == XTC_F32 ? norm_dx_kernel<float, CENTER> : norm_dx_kernel<Bf16, CENTER>;
+            const auto dw = dtype == XTC_F32 ? norm_dw_kernel<float, CENTER> : norm_dw_kernel<Bf16, CENTER>;
             dx<<<grid_of(a.T), kThreads, 0, s>>>(a);
             dw<<<dim3((unsigned)(((int64_t)a.D + kStep - 1) / kStep), (unsigned)slabs), kThreads, 0, s>>>(a);
         }
     }
-    rmsnorm_dw_join_kernel<<<(unsigned)(((int64_t)a.D + kJoinColumns - 1) / kJoinColumns), kJoinThreads, 0, s>>>(a.partial, slabs, a.D, a.DW);
+    const int64_t columns = CENTER ? 2 * (int64_t)a.D : a.D;
+    norm_dw_join_kernel<<<(unsigned)((columns + kJoinColumns - 1) / kJoinColumns), kJoinThreads, 0, s>>>(
+        a.partial, slabs, a.D, a.DW, CENTER ? a.DB : nullptr);
     return hip_status(hipGetLastError());
+}
+
+}  // namespace
+
+xtc_status launch_rmsnorm(const NormArgs &a, xtc_dtype dtype, bool quantize, hipStream_t s) {
+    return launch_norm<false>(a, dtype, quantize, s);
+}
+xtc_status launch_layernorm(const NormArgs &a, xtc_dtype dtype, bool quantize, hipStream_t s) {
+    return launch_norm<true>(a, dtype, quantize, s);
+}
+xtc_status launch_rmsnorm_backward(const NormBackwardArgs &a, xtc_dtype dtype, hipStream_t s) {
+    return launch_norm_backward<false>(a, dtype, s);
+}
+xtc_status launch_layernorm_backward(const NormBackwardArgs &a, xtc_dtype dtype, hipStream_t s) {
+    return launch_norm_backward<true>(a, dtype, s);
 }
 
 xtc_status launch_quantize(const QuantArgs &a, xtc_dtype dtype, hipStream_t s) {

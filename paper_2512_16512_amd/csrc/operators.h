@@ -33,6 +33,8 @@ struct NormArgs {
     void *H;            // X + R (null: not kept)
     int64_t ldh;
     float *rstd;        // null: not kept
+    const void *B;      // layer norm: added last, of W's type (null: nothing)
+    float *mean;        // layer norm (null: not kept)
 };
 
 struct NormBackwardArgs {
@@ -50,7 +52,9 @@ struct NormBackwardArgs {
     void *DX;
     int64_t lddx;
     float *DW;
-    float *partial;     // norm_backward_slabs(T) x D sums of a slab of rows each
+    float *partial;     // norm_backward_slabs(T) x D (layer norm: 2D) sums of a slab of rows each
+    const float *mean;  // layer norm
+    float *DB;
 };
 
 struct QuantArgs {
@@ -92,6 +96,8 @@ constexpr int64_t kMostGroups = int64_t(1) << 24;
 int norm_backward_slabs(int64_t T, int64_t D);
 xtc_status launch_rmsnorm(const NormArgs &a, xtc_dtype dtype, bool quantize, hipStream_t s);
 xtc_status launch_rmsnorm_backward(const NormBackwardArgs &a, xtc_dtype dtype, hipStream_t s);
+xtc_status launch_layernorm(const NormArgs &a, xtc_dtype dtype, bool quantize, hipStream_t s);
+xtc_status launch_layernorm_backward(const NormBackwardArgs &a, xtc_dtype dtype, hipStream_t s);
 xtc_status launch_quantize(const QuantArgs &a, xtc_dtype dtype, hipStream_t s);
 
 // e4m3 A [T, K], B [N, K]

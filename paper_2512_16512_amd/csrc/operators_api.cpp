@@ -40,7 +40,7 @@ xtc_status xtc_rmsnorm(int64_t T, int64_t D, const void *X, int64_t ldx, const v
     if (!aligned_to(X, e) || !aligned_to(R, e) || !aligned_to(H, e) || !aligned_to(W, size_of(w_dtype)) ||
         !aligned_to(Y, size_of(out_dtype)) || !aligned_to(S, 4) || !aligned_to(rstd, 4))
         return XTC_ERR_MISALIGNED;
-    NormArgs a;
+    NormArgs a = {};
     a.T = T; a.D = (int)D;
     a.X = X; a.ldx = ldx; a.R = R; a.ldr = ldr;
     a.W = W; a.w_f32 = w_dtype == XTC_F32; a.eps = eps;
@@ -71,13 +71,73 @@ xtc_status xtc_rmsnorm_backward(int64_t T, int64_t D, const void *DY, int64_t ld
         !aligned_to(W, size_of(w_dtype)) || !aligned_to(rstd, 4) || !aligned_to(DW, 4) || !aligned_to(workspace, 16))
         return XTC_ERR_MISALIGNED;
     if (workspace_bytes < xtc_rmsnorm_backward_workspace(T, D)) return XTC_ERR_BAD_SHAPE;
-    NormBackwardArgs a;
+    NormBackwardArgs a = {};
     a.T = T; a.D = (int)D;
     a.DY = DY; a.lddy = lddy; a.X = X; a.ldx = ldx;
     a.W = W; a.w_f32 = w_dtype == XTC_F32; a.rstd = rstd;
     a.DR = DR; a.lddr = lddr; a.DX = DX; a.lddx = lddx;
     a.DW = DW; a.partial = static_cast<float *>(workspace);
     return launch_rmsnorm_backward(a, dtype, static_cast<hipStream_t>(stream));
+}
+
+xtc_status xtc_layernorm(int64_t T, int64_t D, const void *X, int64_t ldx, const void *R, int64_t ldr, const void *W,
+                         const void *B, float eps, void *Y, int64_t ldy, float *S, int64_t lds, void *H, int64_t ldh,
+                         float *mean, float *rstd, xtc_dtype dtype, xtc_dtype w_dtype, xtc_dtype out_dtype,
+                         void *stream) {
+    const bool quantize = out_dtype == XTC_FP8;
+    if (!known(dtype) || (w_dtype != dtype && w_dtype != XTC_F32) || (!quantize && out_dtype != dtype))
+        return XTC_ERR_BAD_DTYPE;
+    if (T < 0 || D < 0 || !(eps >= 0.f)) return XTC_ERR_BAD_SHAPE;
+    if (T == 0 || D == 0) return XTC_OK;
+    if (T > kMostExtent || D > kMostExtent || ldx > kMostStride || ldy > kMostStride || (R && ldr > kMostStride) ||
+        (H && ldh > kMostStride) || (quantize && lds > kMostStride))
+        return XTC_ERR_TOO_LARGE;
+    if (ldx < D || ldy < D || (R && ldr < D) || (H && ldh < D) || (quantize && lds < scale_blocks(D)))
+        return XTC_ERR_BAD_LEADING_DIM;
+    if (!X || !W || !Y || (quantize && !S) || (H && !R)) return XTC_ERR_NULL_POINTER;
+    const int64_t e = size_of(dtype), w = size_of(w_dtype);
+    if (!aligned_to(X, e) || !aligned_to(R, e) || !aligned_to(H, e) || !aligned_to(W, w) || !aligned_to(B, w) ||
+        !aligned_to(Y, size_of(out_dtype)) || !aligned_to(S, 4) || !aligned_to(mean, 4) || !aligned_to(rstd, 4))
+        return XTC_ERR_MISALIGNED;
+    NormArgs a = {};
+    a.T = T; a.D = (int)D;
+    a.X = X; a.ldx = ldx; a.R = R; a.ldr = ldr;
+    a.W = W; a.w_f32 = w_dtype == XTC_F32; a.B = B; a.eps = eps;
+    a.Y = Y; a.ldy = ldy; a.S = S; a.lds = lds;
+    a.H = H; a.ldh = ldh; a.mean = mean; a.rstd = rstd;
+    return launch_layernorm(a, dtype, quantize, static_cast<hipStream_t>(stream));
+}
+
+int64_t xtc_layernorm_backward_workspace(int64_t T, int64_t D) {
+    if (T < 0 || D < 0 || T > kMostExtent || D > kMostExtent) return -1;
+    return 8 * norm_backward_slabs(T, D) * D;
+}
+
+xtc_status xtc_layernorm_backward(int64_t T, int64_t D, const void *DY, int64_t lddy, const void *X, int64_t ldx,
+                                  const void *W, const float *mean, const float *rstd, const void *DR, int64_t lddr,
+                                  void *DX, int64_t lddx, float *DW, float *DB, void *workspace,
+                                  int64_t workspace_bytes, xtc_dtype dtype, xtc_dtype w_dtype, void *stream) {
+    if (!known(dtype) || (w_dtype != dtype && w_dtype != XTC_F32)) return XTC_ERR_BAD_DTYPE;
+    if (T < 0 || D < 0) return XTC_ERR_BAD_SHAPE;
+    if (D == 0) return XTC_OK;
+    if (T > kMostExtent || D > kMostExtent || (T > 0 && (lddy > kMostStride || ldx > kMostStride ||
+        lddx > kMostStride || (DR && lddr > kMostStride))))
+        return XTC_ERR_TOO_LARGE;
+    if (T > 0 && (lddy < D || ldx < D || lddx < D || (DR && lddr < D))) return XTC_ERR_BAD_LEADING_DIM;
+    if (!DW || !DB || (T > 0 && (!DY || !X || !W || !mean || !rstd || !DX || !workspace))) return XTC_ERR_NULL_POINTER;
+    const int64_t e = size_of(dtype);
+    if (!aligned_to(DY, e) || !aligned_to(X, e) || !aligned_to(DR, e) || !aligned_to(DX, e) ||
+        !aligned_to(W, size_of(w_dtype)) || !aligned_to(mean, 4) || !aligned_to(rstd, 4) || !aligned_to(DW, 4) ||
+        !aligned_to(DB, 4) || !aligned_to(workspace, 16))
+        return XTC_ERR_MISALIGNED;
+    if (workspace_bytes < xtc_layernorm_backward_workspace(T, D)) return XTC_ERR_BAD_SHAPE;
+    NormBackwardArgs a = {};
+    a.T = T; a.D = (int)D;
+    a.DY = DY; a.lddy = lddy; a.X = X; a.ldx = ldx;
+    a.W = W; a.w_f32 = w_dtype == XTC_F32; a.mean = mean; a.rstd = rstd;
+    a.DR = DR; a.lddr = lddr; a.DX = DX; a.lddx = lddx;
+    a.DW = DW; a.DB = DB; a.partial = static_cast<float *>(workspace);
+    return launch_layernorm_backward(a, dtype, static_cast<hipStream_t>(stream));
 }
 
 xtc_status xtc_quantize_fp8(int64_t M, int64_t K, const void *X, int64_t ldx, int64_t block_rows, void *Q, int64_t ldq,

@@ -15,6 +15,7 @@
 #include <ATen/hip/EmptyTensor.h>
 #include <ATen/ops/empty.h>
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
@@ -307,6 +308,82 @@ PyObject *rmsnorm_backward(PyObject *, PyObject *const *args, Py_ssize_t n) {
     }
 }
 
+// The tensors as a tuple (None for undefined ones).
+template <int N>
+PyObject *tuple_of(at::Tensor (&t)[N]) {
+    PyObject *r = PyTuple_New(N);
+    if (!r) return nullptr;
+    for (int i = 0; i < N; ++i) PyTuple_SET_ITEM(r, i, wrapped(std::move(t[i])));
+    return r;
+}
+
+// layernorm(x, weight, bias or None, residual or None, eps, quantize): (out, scale or None, residual, mean, rstd)
+PyObject *layernorm(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    const at::Tensor *t[4];
+    xtc_dtype dt, dtw;
+    if (n != 6 || modes_active() || !tensors(args, t, 4 | 8) || !PyFloat_CheckExact(args[4]) || !truth(args[5])) Py_RETURN_NONE;
+    const at::Tensor &x = *t[0], &w = *t[1];
+    if (!row_major(x) || !dtype_code(x, &dt)) Py_RETURN_NONE;
+    const int64_t T = x.size(0), D = x.size(1);
+    // (of no columns the library's call writes nothing, but there are a mean and an rstd to fill)
+    if (D == 0 || !dtype_code(w, &dtw) || (dtw != dt && dtw != XTC_F32) || !vector_of(w, w.scalar_type(), D, x) ||
+        (t[2] && !vector_of(*t[2], w.scalar_type(), D, x)) || (t[3] && !matrix(*t[3], x.scalar_type(), T, D, x)))
+        Py_RETURN_NONE;
+    try {
+        const c10::DeviceGuard on(x.device());
+        const bool quantize = args[5] == Py_True;
+        at::Tensor r[5];     // out, scale, residual, mean, rstd
+        r[0] = fresh({T, D}, quantize ? kE4m3 : x.scalar_type(), x);
+        if (quantize) r[1] = fresh({T, blocks_of(D)}, at::kFloat, x);
+        r[2] = t[3] ? fresh({T, D}, x.scalar_type(), x) : x;
+        r[3] = fresh({T}, at::kFloat, x);
+        r[4] = fresh({T}, at::kFloat, x);
+        const float eps = (float)PyFloat_AS_DOUBLE(args[4]);
+        float *ps = quantize ? static_cast<float *>(r[1].data_ptr()) : nullptr;
+        void *ph = t[3] ? r[2].data_ptr() : nullptr;
+        const int64_t ldr = t[3] ? row_stride(*t[3]) : 0;
+        void *stream = stream_of(x);
+        if (unlocked(xtc_layernorm, T, D, x.data_ptr(), row_stride(x), data(t[3]), ldr, w.data_ptr(), data(t[2]), eps,
+                     r[0].data_ptr(), D, ps, blocks_of(D), ph, D, static_cast<float *>(r[3].data_ptr()),
+                     static_cast<float *>(r[4].data_ptr()), dt, dtw, quantize ? XTC_FP8 : dt, stream) != XTC_OK)
+            Py_RETURN_NONE;
+        return tuple_of(r);
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+}
+
+// layernorm_backward(dy, x, weight, mean, rstd, dresidual or None): (dx, dweight, dbias)
+PyObject *layernorm_backward(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    const at::Tensor *t[6];
+    xtc_dtype dt, dtw;
+    if (n != 6 || modes_active() || !tensors(args, t, 32)) Py_RETURN_NONE;
+    const at::Tensor &dy = *t[0], &x = *t[1], &w = *t[2], &mean = *t[3], &rstd = *t[4];
+    if (!row_major(x) || !dtype_code(x, &dt)) Py_RETURN_NONE;
+    const int64_t T = x.size(0), D = x.size(1);
+    if (!matrix(dy, x.scalar_type(), T, D, x) || !dtype_code(w, &dtw) || (dtw != dt && dtw != XTC_F32) ||
+        !vector_of(w, w.scalar_type(), D, x) || !vector_of(mean, at::kFloat, T, x) || !vector_of(rstd, at::kFloat, T, x) ||
+        (t[5] && !matrix(*t[5], x.scalar_type(), T, D, x)))
+        Py_RETURN_NONE;
+    try {
+        const c10::DeviceGuard on(x.device());
+        const int64_t size = xtc_layernorm_backward_workspace(T, D);
+        if (size < 0) Py_RETURN_NONE;
+        at::Tensor r[3] = {fresh({T, D}, x.scalar_type(), x), fresh({D}, at::kFloat, x), fresh({D}, at::kFloat, x)};
+        at::Tensor work = fresh({size}, at::kByte, x);
+        const int64_t lddr = t[5] ? row_stride(*t[5]) : 0;
+        void *stream = stream_of(x);
+        if (unlocked(xtc_layernorm_backward, T, D, dy.data_ptr(), row_stride(dy), x.data_ptr(), row_stride(x),
+                     w.data_ptr(), static_cast<const float *>(mean.data_ptr()), static_cast<const float *>(rstd.data_ptr()),
+                     data(t[5]), lddr, r[0].data_ptr(), at_least_1(D), static_cast<float *>(r[1].data_ptr()),
+                     static_cast<float *>(r[2].data_ptr()), work.data_ptr(), size, dt, dtw, stream) != XTC_OK)
+            Py_RETURN_NONE;
+        return tuple_of(r);
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+}
+
 // quantize_fp8(x, block_rows): (q, scale)
 PyObject *quantize_fp8(PyObject *, PyObject *const *args, Py_ssize_t n) {
     const at::Tensor *x;
@@ -445,6 +522,8 @@ PyMethodDef kMethods[] = {
      "conv2d_nchw(x, w, stride, pad, out, relu): the convolution, or None likewise"},
     {"rmsnorm", fast<rmsnorm>(), METH_FASTCALL, "rmsnorm(x, weight, residual, eps, quantize): its results, or None likewise"},
     {"rmsnorm_backward", fast<rmsnorm_backward>(), METH_FASTCALL, "rmsnorm_backward(dy, x, weight, rstd, dresidual)"},
+    {"layernorm", fast<layernorm>(), METH_FASTCALL, "layernorm(x, weight, bias, residual, eps, quantize)"},
+    {"layernorm_backward", fast<layernorm_backward>(), METH_FASTCALL, "layernorm_backward(dy, x, weight, mean, rstd, dresidual)"},
     {"quantize_fp8", fast<quantize_fp8>(), METH_FASTCALL, "quantize_fp8(x, block_rows)"},
     {"matmul_fp8", fast<matmul_fp8>(), METH_FASTCALL, "matmul_fp8(a, a_scale, b, b_scale, out, relu, dtype)"},
     {"matmul_grouped", fast<matmul_grouped>(), METH_FASTCALL, "matmul_grouped(a, b, ends, transpose_b, out, relu, dtype)"},

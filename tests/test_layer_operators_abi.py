@@ -1,0 +1,73 @@
+"""Refusals of the layer norm, linear, routing and combining operators, on the CPU:
+every invalid call returns its status before the device is touched (the pointers are
+NULL or dummies), and the conveniences over tensors raise."""
+import pytest
+
+import paper_2512_16512_amd as x
+from test_operators_abi import BAD, BIG, E4M3, call, t
+
+torch = pytest.importorskip("torch")
+
+NORM = dict(T=4, D=200, X=BAD, ldx=200, R=BAD, ldr=200, W=BAD, B=BAD, eps=1e-6, Y=BAD, ldy=200, S=BAD, lds=2, H=BAD,
+            ldh=200, mean=BAD, rstd=BAD, dtype=1, w_dtype=1, out_dtype=2)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(dtype=2), 4), (dict(dtype=7), 4), (dict(w_dtype=2), 4), (dict(out_dtype=0), 4), (dict(dtype=0, w_dtype=1), 4),
+    (dict(T=-1), 2), (dict(D=-1), 2), (dict(eps=-1.0), 2), (dict(eps=float("nan")), 2),
+    (dict(ldx=199), 3), (dict(ldr=199), 3), (dict(ldy=199), 3), (dict(ldh=199), 3), (dict(lds=1), 3),
+    (dict(X=0), 1), (dict(W=0), 1), (dict(Y=0), 1), (dict(S=0), 1), (dict(R=0, ldr=0), 1),
+    (dict(X=BAD + 1), 9), (dict(R=BAD + 1), 9), (dict(W=BAD + 1), 9), (dict(B=BAD + 1), 9), (dict(w_dtype=0, B=BAD + 2), 9),
+    (dict(S=BAD + 2), 9), (dict(H=BAD + 1), 9), (dict(rstd=BAD + 2), 9), (dict(mean=BAD + 2), 9),
+    (dict(out_dtype=1, Y=BAD + 1), 9), (dict(T=BIG), 7), (dict(D=BIG, ldx=BIG, ldr=BIG, ldy=BIG, ldh=BIG), 7),
+    (dict(ldx=BIG), 7), (dict(T=0, X=0), 0), (dict(D=0, Y=0), 0),
+])
+def test_layernorm_refuses(change, status):
+    assert call(x.xtc_layernorm, NORM, **change) == status
+
+
+BACK = dict(T=4, D=200, DY=BAD, lddy=200, X=BAD, ldx=200, W=BAD, mean=BAD, rstd=BAD, DR=BAD, lddr=200, DX=BAD, lddx=200,
+            DW=BAD, DB=BAD, workspace=BAD, workspace_bytes=1 << 20, dtype=0, w_dtype=0)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(dtype=2), 4), (dict(w_dtype=1), 4), (dict(T=-1), 2), (dict(D=-1), 2),
+    (dict(workspace_bytes=x.xtc_layernorm_backward_workspace(4, 200) - 1), 2),
+    (dict(lddy=199), 3), (dict(ldx=199), 3), (dict(lddr=199), 3), (dict(lddx=199), 3),
+    (dict(DY=0), 1), (dict(X=0), 1), (dict(W=0), 1), (dict(mean=0), 1), (dict(rstd=0), 1), (dict(DX=0), 1), (dict(DW=0), 1),
+    (dict(DB=0), 1), (dict(workspace=0), 1), (dict(DX=BAD + 2), 9), (dict(mean=BAD + 2), 9), (dict(DB=BAD + 2), 9),
+    (dict(workspace=BAD + 4), 9), (dict(T=BIG), 7), (dict(lddx=BIG), 7), (dict(D=0), 0),
+])
+def test_layernorm_backward_refuses(change, status):
+    assert call(x.xtc_layernorm_backward, BACK, **change) == status
+
+
+def test_layernorm_backward_workspace():
+    assert x.xtc_layernorm_backward_workspace(-1, 4) == -1 and x.xtc_layernorm_backward_workspace(4, BIG) == -1
+    assert x.xtc_layernorm_backward_workspace(0, 100) >= 0
+    assert x.xtc_layernorm_backward_workspace(4, 200) >= 8 * 200
+
+
+# ------------------------------------------------ the conveniences' own checks
+
+
+F32 = torch.float32
+
+
+@pytest.mark.parametrize("fn,args,error,match", [
+    (x.layernorm, (t(4, 8, dtype=torch.float16), t(8)), TypeError, "x must be float32 or bfloat16"),
+    (x.layernorm, (t(4, 8), t(8)), ValueError, "CUDA"),
+    (x.layernorm, (t(8, 4).t(), t(8)), ValueError, "unit stride"),
+    (x.layernorm_backward, (t(4, 8), t(4, 8, dtype=E4M3), t(8), t(4), t(4)), TypeError, "x must be"),
+    (x.layernorm_backward, (t(4, 8), t(4, 8), t(8), t(4), t(4)), ValueError, "CUDA"),
+])
+def test_conveniences_refuse(fn, args, error, match):
+    with pytest.raises(error, match=match):
+        fn(*args)
+
+
+def test_the_native_entries_leave_other_tensors_to_python():
+    a, v = t(4, 8), t(4, dtype=F32)
+    for name, args in (("layernorm", (a, t(8), t(8), None, 1e-6, False)), ("layernorm_backward", (a, a, t(8), v, v, None))):
+        fast = getattr(x._fast, name)
+        assert fast(*args) is None and fast() is None and fast(*([None] * len(args))) is None
