@@ -52,6 +52,16 @@ typedef enum { XTC_F32 = 0, XTC_BF16 = 1, XTC_FP8 = 2 } xtc_dtype;
 
 typedef enum { XTC_OP_MATMUL = 0, XTC_OP_CONV2D = 1 } xtc_op;
 
+/* What a linear layer applies to its sums (xtc_linear). */
+typedef enum {
+    XTC_NO_ACTIVATION = 0,
+    XTC_RELU = 1,                     /* v < 0 ? 0 : v                        */
+    XTC_GELU = 2,                     /* v (1 + erf(v / sqrt 2)) / 2          */
+    XTC_GELU_TANH = 3,                /* v (1 + tanh u) / 2, u = sqrt(2/pi)   */
+                                      /* (v + 0.044715 v^3)                   */
+    XTC_SILU = 4                      /* v / (1 + exp(-v))                    */
+} xtc_activation;
+
 typedef enum {
     XTC_OK = 0,
     XTC_ERR_NULL_POINTER = 1,         /* a tensor or output pointer is NULL   */
@@ -415,6 +425,76 @@ xtc_status xtc_matmul_fp8(int64_t M, int64_t N, int64_t K,
                           const void *A, int64_t lda, const float *SA, int64_t ldsa,
                           const void *B, int64_t ldb, const float *SB, int64_t ldsb,
                           void *C, int64_t ldc, xtc_dtype out_dtype, int32_t relu, void *stream);
+
+/*
+ * xtc_linear -- a linear layer and what follows it:
+ *   z = A * B + bias,  C = act(z) + R,
+ * sums and all of that in fp32, z and C rounded once each.
+ *
+ *  A      bf16 (dtype XTC_BF16, else XTC_ERR_BAD_DTYPE) T x K, row stride lda.
+ *  B      bf16 K x N, row stride ldb, or N x K where transpose_b is nonzero (the
+ *         gradient of A is the product of z's gradient with the same B and the
+ *         other transpose_b).
+ *  bias   device, N values of bias_dtype (XTC_F32 or XTC_BF16), or NULL.
+ *  R      device, T x N of r_dtype (XTC_F32 or XTC_BF16), row stride ldr, or NULL.
+ *  activation  an xtc_activation, else XTC_ERR_BAD_SHAPE.
+ *  C      device, out_dtype (XTC_F32 or XTC_BF16) T x N, row stride ldc.
+ *  Z      device, z in out_dtype for the activation's gradient, row stride ldz, or
+ *         NULL.
+ *  workspace  device, workspace_bytes >= xtc_linear_workspace(T, N, K, transpose_b)
+ *         (0 for many sizes: NULL is fine then), 16-byte aligned, written by the
+ *         call; too small is XTC_ERR_BAD_SHAPE.  Calls that may run at the same
+ *         time need one each.
+ * T or N 0 is a no-op; K 0 gives act(bias) + R.  The order of a sum depends on T, N,
+ * K, transpose_b and on whether the rows are 16-byte aligned.  Errors as for
+ * xtc_rmsnorm.
+ */
+xtc_status xtc_linear(int64_t T, int64_t N, int64_t K, const void *A, int64_t lda,
+                      const void *B, int64_t ldb, int32_t transpose_b,
+                      const void *bias, xtc_dtype bias_dtype,
+                      const void *R, int64_t ldr, xtc_dtype r_dtype, int32_t activation,
+                      void *C, int64_t ldc, void *Z, int64_t ldz,
+                      void *workspace, int64_t workspace_bytes,
+                      xtc_dtype dtype, xtc_dtype out_dtype, void *stream);
+
+/* Bytes of workspace; -1 for extents outside the limits.  Pure host function. */
+int64_t xtc_linear_workspace(int64_t T, int64_t N, int64_t K, int32_t transpose_b);
+
+/*
+ * xtc_linear_wgrad -- the gradient of a linear layer's B: DB = A^T * DY (zeros when
+ * T == 0), K x N of out_dtype (XTC_F32 or XTC_BF16), row stride lddb.  A is T x K, DY
+ * (z's gradient) T x N, both bf16.  Of a B that is N x K it is the same call with A
+ * and DY exchanged.  workspace: xtc_linear_wgrad_workspace(T, N, K) bytes, as above.
+ */
+xtc_status xtc_linear_wgrad(int64_t T, int64_t N, int64_t K, const void *A, int64_t lda,
+                            const void *DY, int64_t lddy, void *DB, int64_t lddb,
+                            void *workspace, int64_t workspace_bytes,
+                            xtc_dtype dtype, xtc_dtype out_dtype, void *stream);
+
+/* Bytes of workspace; -1 for extents outside the limits.  Pure host function. */
+int64_t xtc_linear_wgrad_workspace(int64_t T, int64_t N, int64_t K);
+
+/*
+ * xtc_activation_backward -- the gradients of a linear layer's z and bias:
+ *   DZ = DY * act'(Z), DB_j = sum_t DY_tj act'(Z_tj),
+ * the product in fp32, DZ rounded once to bf16 (what xtc_linear and
+ * xtc_linear_wgrad take) and DB summed, in fp32, before that rounding.
+ *
+ *  DY, Z  device, T x N of dy_dtype and z_dtype (XTC_F32 or XTC_BF16 each), row
+ *         strides lddy and ldz.  With XTC_NO_ACTIVATION Z and what describes it are ignored.
+ *  DZ     device, bf16 T x N, row stride lddz.
+ *  DB     device, N fp32 values (zeros when T == 0), or NULL.
+ *  workspace  xtc_activation_backward_workspace(T, N) bytes, as above; without DB
+ *         none is needed.
+ * Sums are taken in an order that depends on T and N alone.
+ */
+xtc_status xtc_activation_backward(int64_t T, int64_t N, const void *DY, int64_t lddy, xtc_dtype dy_dtype,
+                                   const void *Z, int64_t ldz, xtc_dtype z_dtype, int32_t activation,
+                                   void *DZ, int64_t lddz, float *DB,
+                                   void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace; -1 for extents outside the limits.  Pure host function. */
+int64_t xtc_activation_backward_workspace(int64_t T, int64_t N);
 
 /*
  * xtc_matmul_grouped -- products of the rows of A with the matrix of their

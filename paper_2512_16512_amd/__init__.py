@@ -32,6 +32,11 @@ LIB_PATH = os.path.join(_HERE, "libxtc.so")
 XTC_F32 = 0
 XTC_BF16 = 1
 XTC_FP8 = 2
+XTC_NO_ACTIVATION = 0
+XTC_RELU = 1
+XTC_GELU = 2
+XTC_GELU_TANH = 3
+XTC_SILU = 4
 XTC_OP_MATMUL = 0
 XTC_OP_CONV2D = 1
 
@@ -125,6 +130,19 @@ def _load():
     lib.xtc_quantize_fp8.restype = i32
     lib.xtc_matmul_fp8.argtypes = [i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, i32, i32, vp]
     lib.xtc_matmul_fp8.restype = i32
+    lib.xtc_linear.argtypes = [i64] * 3 + [vp, i64, vp, i64, i32, vp, i32, vp, i64, i32, i32, vp, i64, vp, i64, vp, i64,
+                                           i32, i32, vp]
+    lib.xtc_linear.restype = i32
+    lib.xtc_linear_workspace.argtypes = [i64] * 3 + [i32]
+    lib.xtc_linear_workspace.restype = i64
+    lib.xtc_linear_wgrad.argtypes = [i64] * 3 + [vp, i64, vp, i64, vp, i64, vp, i64, i32, i32, vp]
+    lib.xtc_linear_wgrad.restype = i32
+    lib.xtc_linear_wgrad_workspace.argtypes = [i64] * 3
+    lib.xtc_linear_wgrad_workspace.restype = i64
+    lib.xtc_activation_backward.argtypes = [i64] * 2 + [vp, i64, i32, vp, i64, i32, i32, vp, i64, vp, vp, i64, vp]
+    lib.xtc_activation_backward.restype = i32
+    lib.xtc_activation_backward_workspace.argtypes = [i64] * 2
+    lib.xtc_activation_backward_workspace.restype = i64
     lib.xtc_matmul_grouped.argtypes = [i64] * 4 + [vp, i64, vp, i64, i64, i32, vp, vp, i64, i32, i32, i32, vp]
     lib.xtc_matmul_grouped.restype = i32
     lib.xtc_matmul_grouped_wgrad.argtypes = [i64] * 4 + [vp, i64, vp, i64, vp, vp, i64, i64, i32, i32, vp]
@@ -176,7 +194,8 @@ _fast = _load_binding()
 EXPORTS = ("xtc_matmul", "xtc_conv2d_nchw", "xtc_matmul_relu", "xtc_conv2d_nchw_relu",
            "xtc_rmsnorm", "xtc_rmsnorm_backward", "xtc_rmsnorm_backward_workspace", "xtc_layernorm",
            "xtc_layernorm_backward", "xtc_layernorm_backward_workspace", "xtc_quantize_fp8",
-           "xtc_matmul_fp8", "xtc_matmul_grouped", "xtc_matmul_grouped_wgrad", "xtc_matmul_grouped_fp8",
+           "xtc_matmul_fp8", "xtc_linear", "xtc_linear_workspace", "xtc_linear_wgrad", "xtc_linear_wgrad_workspace",
+           "xtc_activation_backward", "xtc_activation_backward_workspace", "xtc_matmul_grouped", "xtc_matmul_grouped_wgrad", "xtc_matmul_grouped_fp8",
            "xtc_default_schedule", "xtc_sched_occupancy", "xtc_sched_check",
            "xtc_sched_list", "xtc_status_str", "xtc_last_hip_error", "xtc_conv_max_k",
            "xtc_version")
@@ -246,6 +265,35 @@ def xtc_quantize_fp8(M, K, X, ldx, block_rows, Q, ldq, S, lds, dtype, stream=0) 
 
 def xtc_matmul_fp8(M, N, K, A, lda, SA, ldsa, B, ldb, SB, ldsb, C, ldc, out_dtype, relu=0, stream=0) -> int:
     return _lib.xtc_matmul_fp8(M, N, K, A, lda, SA, ldsa, B, ldb, SB, ldsb, C, ldc, out_dtype, relu, stream)
+
+
+def xtc_linear(T, N, K, A, lda, B, ldb, transpose_b, bias, bias_dtype, R, ldr, r_dtype, activation, C, ldc, Z, ldz,
+               workspace, workspace_bytes, dtype, out_dtype, stream=0) -> int:
+    return _lib.xtc_linear(T, N, K, A, lda, B, ldb, transpose_b, bias, bias_dtype, R, ldr, r_dtype, activation, C, ldc,
+                           Z, ldz, workspace, workspace_bytes, dtype, out_dtype, stream)
+
+
+def xtc_linear_workspace(T, N, K, transpose_b) -> int:
+    return _lib.xtc_linear_workspace(T, N, K, transpose_b)
+
+
+def xtc_linear_wgrad(T, N, K, A, lda, DY, lddy, DB, lddb, workspace, workspace_bytes, dtype, out_dtype, stream=0) -> int:
+    return _lib.xtc_linear_wgrad(T, N, K, A, lda, DY, lddy, DB, lddb, workspace, workspace_bytes, dtype, out_dtype,
+                                 stream)
+
+
+def xtc_linear_wgrad_workspace(T, N, K) -> int:
+    return _lib.xtc_linear_wgrad_workspace(T, N, K)
+
+
+def xtc_activation_backward(T, N, DY, lddy, dy_dtype, Z, ldz, z_dtype, activation, DZ, lddz, DB, workspace,
+                            workspace_bytes, stream=0) -> int:
+    return _lib.xtc_activation_backward(T, N, DY, lddy, dy_dtype, Z, ldz, z_dtype, activation, DZ, lddz, DB, workspace,
+                                        workspace_bytes, stream)
+
+
+def xtc_activation_backward_workspace(T, N) -> int:
+    return _lib.xtc_activation_backward_workspace(T, N)
 
 
 def xtc_matmul_grouped(G, T, N, K, A, lda, B, ldb, stride_b, transpose_b, ends, C, ldc, dtype, out_dtype, relu=0,
@@ -651,6 +699,106 @@ def matmul_fp8(a, a_scale, b, b_scale, out=None, relu=False, dtype=None):
                           b_scale.data_ptr(), _ld(b_scale), out.data_ptr(), _ld(out), code, int(relu),
                           _stream(torch, a.device)), "xtc_matmul_fp8")
     return out
+
+
+_ACTIVATIONS = {None: XTC_NO_ACTIVATION, "relu": XTC_RELU, "gelu": XTC_GELU, "gelu_tanh": XTC_GELU_TANH,
+                "silu": XTC_SILU}
+
+
+def _activation(name):
+    if name not in _ACTIVATIONS:
+        raise ValueError("activation must be None, 'relu', 'gelu', 'gelu_tanh' or 'silu', not %r" % (name,))
+    return _ACTIVATIONS[name]
+
+
+def linear(a, b, bias=None, residual=None, activation=None, transpose_b=False, keep=False, out=None, dtype=None):
+    """``out = act(a @ b + bias) + residual``, all of it in one kernel and float32, rounded once.
+
+    ``a`` [T, K] and ``b`` [K, N] ([N, K] with ``transpose_b``) are bfloat16, ``bias`` [N] and ``residual`` [T, N] float32
+    or bfloat16 each.  ``activation``: None, "relu", "gelu" (by the error function), "gelu_tanh" or "silu".  ``out``
+    [T, N] is float32 or bfloat16 (``dtype``, when allocated here; float32 unless given).  With ``keep`` the result is
+    ``(out, z)``, z = a @ b + bias in out's type for ``activation_backward``.  The gradient of ``a`` is the same call
+    on z's gradient with the other ``transpose_b``."""
+    code_act = _activation(activation)
+    if _fast is not None:
+        r = _fast.linear(a, b, bias, residual, code_act, transpose_b, keep, out, dtype)
+        if r is not None:
+            return r
+    import torch
+    bf16, either = (torch.bfloat16,), (torch.float32, torch.bfloat16)
+    _matrix(a, "a", bf16)
+    T, K = a.shape
+    _matrix(b, "b", bf16, None, a.device)
+    N = b.shape[0 if transpose_b else 1]
+    if b.shape[1 if transpose_b else 0] != K:
+        raise ValueError("inner dimensions differ: %d vs %d" % (K, b.shape[1 if transpose_b else 0]))
+    if bias is not None:
+        _vector(bias, "bias", either, N, a.device)
+    if residual is not None:
+        _matrix(residual, "residual", either, (T, N), a.device)
+    out, code = _result(torch, (T, N), out, dtype, a.device)
+    z = torch.empty((T, N), dtype=out.dtype, device=a.device) if keep else None
+    size = xtc_linear_workspace(T, N, K, int(transpose_b))
+    work = torch.empty(max(size, 0), dtype=torch.uint8, device=a.device)
+    with _on(torch, a.device):
+        _check(xtc_linear(T, N, K, a.data_ptr(), _ld(a), b.data_ptr(), _ld(b), int(transpose_b), _ptr(bias),
+                          XTC_F32 if bias is None else _dtype_code(torch, bias), _ptr(residual),
+                          0 if residual is None else _ld(residual),
+                          XTC_F32 if residual is None else _dtype_code(torch, residual), code_act, out.data_ptr(),
+                          _ld(out), _ptr(z), max(N, 1), work.data_ptr(), size, XTC_BF16, code, _stream(torch, a.device)),
+               "xtc_linear")
+    return (out, z) if keep else out
+
+
+def linear_wgrad(a, dy, out=None, dtype=None):
+    """The gradient of ``linear``'s ``b`` [K, N] (float32 or bfloat16: ``dtype``): ``a.T @ dy``, of ``a`` [T, K] and the
+    gradient ``dy`` [T, N] of a @ b, both bfloat16.  Of a ``b`` that is [N, K]: ``linear_wgrad(dy, a)``."""
+    if _fast is not None:
+        r = _fast.linear_wgrad(a, dy, out, dtype)
+        if r is not None:
+            return r
+    import torch
+    bf16 = (torch.bfloat16,)
+    _matrix(a, "a", bf16)
+    T, K = a.shape
+    _matrix(dy, "dy", bf16, None, a.device)
+    N = dy.shape[1]
+    if dy.shape[0] != T:
+        raise ValueError("a and dy have %d and %d rows" % (T, dy.shape[0]))
+    out, code = _result(torch, (K, N), out, dtype, a.device)
+    size = xtc_linear_wgrad_workspace(T, N, K)
+    work = torch.empty(max(size, 0), dtype=torch.uint8, device=a.device)
+    with _on(torch, a.device):
+        _check(xtc_linear_wgrad(T, N, K, a.data_ptr(), _ld(a), dy.data_ptr(), _ld(dy), out.data_ptr(), _ld(out),
+                                work.data_ptr(), size, XTC_BF16, code, _stream(torch, a.device)), "xtc_linear_wgrad")
+    return out
+
+
+def activation_backward(dy, z, activation):
+    """``(dz, dbias)`` of ``linear``: ``dy`` [T, N] is the gradient of its result, ``z`` what it kept (float32 or bfloat16
+    each; z is not read where ``activation`` is None).  ``dz = dy * act'(z)`` is bfloat16, as ``linear`` and
+    ``linear_wgrad`` take it; ``dbias`` [N], its column sums before that rounding, float32."""
+    code_act = _activation(activation)
+    if _fast is not None:
+        r = _fast.activation_backward(dy, z, code_act)
+        if r is not None:
+            return r
+    import torch
+    either = (torch.float32, torch.bfloat16)
+    _matrix(dy, "dy", either)
+    T, N = dy.shape
+    if activation is None:
+        z = dy
+    _matrix(z, "z", either, (T, N), dy.device)
+    dz = torch.empty((T, N), dtype=torch.bfloat16, device=dy.device)
+    dbias = torch.empty(N, dtype=torch.float32, device=dy.device)
+    size = xtc_activation_backward_workspace(T, N)
+    work = torch.empty(max(size, 0), dtype=torch.uint8, device=dy.device)
+    with _on(torch, dy.device):
+        _check(xtc_activation_backward(T, N, dy.data_ptr(), _ld(dy), _dtype_code(torch, dy), z.data_ptr(), _ld(z),
+                                       _dtype_code(torch, z), code_act, dz.data_ptr(), max(N, 1), dbias.data_ptr(),
+                                       work.data_ptr(), size, _stream(torch, dy.device)), "xtc_activation_backward")
+    return dz, dbias
 
 
 def matmul_grouped(a, b, ends, transpose_b=False, out=None, relu=False, dtype=None):

@@ -97,21 +97,21 @@ struct TileOrder {
 
 // The id of this workgroup's tile, or -1 (a launch holds the most tiles there
 // can be).  Workgroups go to the 8 XCDs in turn; each XCD gets an equal run of
-// neighbouring tiles, but of a weights' gradient, whose tiles are not equally
-// long, every eighth, the longest groups' first (16384 rows over 16 uneven groups,
+// neighbouring tiles, but of groups' weights' gradients (IN_ORDER), whose tiles are
+// not equally long, every eighth, the longest groups' first (16384 rows over 16 uneven groups,
 // 1024 x 2048 each, tiles of 128x256: in the groups' order a tenth longer).
-template <Kind KIND>
+template <bool IN_ORDER>
 __device__ __forceinline__ int tile_id(int total) {
     const int b = (int)blockIdx.x, x = b & 7, j = b >> 3, q = total >> 3, rem = total & 7;
-    if (KIND == kWgrad) return b < total ? b : -1;
+    if (IN_ORDER) return b < total ? b : -1;
     return j < q + (x < rem ? 1 : 0) ? x * q + (x < rem ? x : rem) + j : -1;
 }
 
 __device__ __forceinline__ float relu_if(int relu, float v) { return relu && v < 0.f ? 0.f : v; }
 
 // Writes v[0 .. 3], the columns n .. n + 3 of a row of C at `c`, of which `left` exist.
-__device__ __forceinline__ void write4(const GroupedArgs &p, unsigned char *c, int n, int left, float (&v)[4]) {
-    if (p.out_bf16) {
+__device__ __forceinline__ void write4(bool bf16, unsigned char *c, int n, int left, float (&v)[4]) {
+    if (bf16) {
         __bf16 t[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) t[i] = (__bf16)v[i];
@@ -161,6 +161,13 @@ template <Kind KIND>
 int64_t tile_count(const GroupedArgs &a, int bm, int bn) {
     return (KIND == kWgrad ? cdiv(a.K, bm) * a.G : row_tiles(a, bm)) * cdiv(a.N, bn);
 }
+
+template <typename Args, Kind KIND, int BM, int BN>
+struct OrderFor {
+    typedef TileOrder<KIND, BM, BN> type;
+};
+template <typename Args, Kind KIND, int BM, int BN>
+using OrderOf = typename OrderFor<Args, KIND, BM, BN>::type;
 
 // A compiled kernel and what a launch of it takes, in microseconds: with n tiles
 // on 256 CUs of per_cu workgroups each, every round costs `fixed` (the first

@@ -31,10 +31,14 @@ __device__ __forceinline__ int swz_row(int r) {
 
 // Chunk swizzle of rows of CB chunks with one k each: spreads the four rows that
 // a transpose read takes at once, and rows k and k + 8, over the banks (rows of
-// 8 chunks fill half of them, so that odd rows are apart by themselves).
+// 8 chunks fill half of them, so that odd rows are apart by themselves; of 4, where four
+// rows fill them, rows 8 apart remain; of 2 those meet).
 template <int CB>
 __device__ __forceinline__ int swz_k(int k) {
-    return CB == 8 ? (k & 2) | ((k >> 1) & 4) : ((k & 1) * 6) ^ ((k & 2) * 5) ^ (((k >> 3) & 1) * 2);
+    return CB == 2   ? 0
+           : CB == 4 ? (k >> 2) & 2
+           : CB == 8 ? (k & 2) | ((k >> 1) & 4)
+                     : ((k & 1) * 6) ^ ((k & 2) * 5) ^ (((k >> 3) & 1) * 2);
 }
 
 // WIDE: e4m3 operands widened to bf16 (fp32 sums; see mfma_fp8.h).

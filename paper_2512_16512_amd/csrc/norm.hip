@@ -392,7 +392,7 @@ __global__ void __launch_bounds__(kThreads) norm_dw_kernel(NormBackwardArgs p) {
 // in its order, joined by halves (1024 rows of 2048 sums: 5 us, a few trips to
 // memory and as many barriers).
 constexpr int kJoinColumns = 16, kJoinThreads = 1024;
-__global__ void __launch_bounds__(kJoinThreads) norm_dw_join_kernel(const float *partial, int slabs, int D, float *DW, float *DB) {
+__global__ void __launch_bounds__(kJoinThreads) column_sums_kernel(const float *partial, int slabs, int D, float *DW, float *DB) {
     __shared__ float s[kJoinThreads];
     const int run = threadIdx.x / kJoinColumns;
     // (with DB: 2D sums a slab)
@@ -527,6 +527,12 @@ int norm_backward_slabs(int64_t T, int64_t D) {
     return (int)(groups < most ? groups : most);
 }
 
+xtc_status launch_column_sums(const float *partial, int slabs, int D, float *DW, float *DB, hipStream_t s) {
+    const int64_t columns = DB ? 2 * (int64_t)D : D;
+    column_sums_kernel<<<(unsigned)((columns + kJoinColumns - 1) / kJoinColumns), kJoinThreads, 0, s>>>(partial, slabs, D, DW, DB);
+    return hip_status(hipGetLastError());
+}
+
 namespace {
 
 template <bool CENTER>
@@ -577,10 +583,7 @@ xtc_status launch_norm_backward(const NormBackwardArgs &a, xtc_dtype dtype, hipS
             dw<<<dim3((unsigned)(((int64_t)a.D + kStep - 1) / kStep), (unsigned)slabs), kThreads, 0, s>>>(a);
         }
     }
-    const int64_t columns = CENTER ? 2 * (int64_t)a.D : a.D;
-    norm_dw_join_kernel<<<(unsigned)((columns + kJoinColumns - 1) / kJoinColumns), kJoinThreads, 0, s>>>(
-        a.partial, slabs, a.D, a.DW, CENTER ? a.DB : nullptr);
-    return hip_status(hipGetLastError());
+    return launch_column_sums(a.partial, slabs, a.D, a.DW, CENTER ? a.DB : nullptr, s);
 }
 
 }  // namespace

@@ -90,6 +90,37 @@ struct GroupedArgs {
     int relu;
 };
 
+// A linear layer: one product of a family (ends null, G 1), and what follows it.
+struct LinearArgs : GroupedArgs {
+    const void *bias;   // N values (null: none)
+    int bias_f32;       // else bf16; likewise the residual
+    const void *R;      // T x N, added last (null: none)
+    int64_t ldr;
+    int r_f32;
+    void *Z;            // what the activation takes, of C's type (null: not kept)
+    int64_t ldz;
+    int act;            // xtc_activation
+    int splits;         // parts of the reduction, k_each long but the last
+    int k_each;
+    float *part;        // several splits: their sums, splits x rows x N
+};
+
+struct ActivationArgs {
+    int64_t T;
+    int N;
+    const void *DY;
+    int64_t lddy;
+    int dy_f32;         // else bf16; likewise Z
+    const void *Z;
+    int64_t ldz;
+    int z_f32;
+    int act;
+    void *DZ;           // bf16
+    int64_t lddz;
+    float *DB;          // column sums of the unrounded DZ (null: not wanted)
+    float *partial;     // activation_slabs() x N sums of a slab of rows each
+};
+
 // Workgroups of a launch: fewer than 2^32 threads of 256 a workgroup.
 constexpr int64_t kMostGroups = int64_t(1) << 24;
 
@@ -98,6 +129,8 @@ xtc_status launch_rmsnorm(const NormArgs &a, xtc_dtype dtype, bool quantize, hip
 xtc_status launch_rmsnorm_backward(const NormBackwardArgs &a, xtc_dtype dtype, hipStream_t s);
 xtc_status launch_layernorm(const NormArgs &a, xtc_dtype dtype, bool quantize, hipStream_t s);
 xtc_status launch_layernorm_backward(const NormBackwardArgs &a, xtc_dtype dtype, hipStream_t s);
+// DW = column sums of `slabs` rows of D values (with DB: of 2D, the second half its), in a fixed order.
+xtc_status launch_column_sums(const float *partial, int slabs, int D, float *DW, float *DB, hipStream_t s);
 xtc_status launch_quantize(const QuantArgs &a, xtc_dtype dtype, hipStream_t s);
 
 // e4m3 A [T, K], B [N, K]
@@ -106,6 +139,16 @@ xtc_status launch_grouped_fp8(const GroupedArgs &a, hipStream_t s);
 xtc_status launch_grouped_bf16(const GroupedArgs &a, bool b_rows_n, hipStream_t s);
 // bf16 A [T, K] and B [T, N]: C of group g [K, N] = A_g^T B_g
 xtc_status launch_grouped_wgrad(const GroupedArgs &a, hipStream_t s);
+
+// bf16 A [T, K] and B [K, N] (b_rows_n: [N, K]).  Its splits' sums go to a.part, of
+// linear_workspace() bytes at least.
+int64_t linear_workspace(const LinearArgs &a, bool b_rows_n);
+xtc_status launch_linear(const LinearArgs &a, bool b_rows_n, hipStream_t s);
+// C [K, N] = A^T B of bf16 A [T, K], B [T, N]
+int64_t linear_wgrad_workspace(const LinearArgs &a);
+xtc_status launch_linear_wgrad(const LinearArgs &a, hipStream_t s);
+int activation_slabs(int64_t T, int64_t N);
+xtc_status launch_activation_backward(const ActivationArgs &a, hipStream_t s);
 
 // Which of the kernels for aligned rows a product takes (-1: the one for rows at
 // any address), and how many there are.  kind: 0 e4m3, 1 bf16 with B [K, N], 2 with

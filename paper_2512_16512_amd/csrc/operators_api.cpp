@@ -253,6 +253,106 @@ xtc_status xtc_matmul_grouped_wgrad(int64_t G, int64_t T, int64_t N, int64_t K, 
     return launch_grouped_wgrad(a, static_cast<hipStream_t>(stream));
 }
 
+int64_t xtc_linear_workspace(int64_t T, int64_t N, int64_t K, int32_t transpose_b) {
+    if (T < 0 || N < 0 || K < 0 || T > kMostExtent || N > kMostExtent || K > kMostExtent) return -1;
+    if (T == 0 || N == 0) return 0;
+    LinearArgs a = {};
+    a.T = T; a.N = (int)N; a.K = (int)K;
+    return linear_workspace(a, transpose_b != 0);
+}
+
+xtc_status xtc_linear(int64_t T, int64_t N, int64_t K, const void *A, int64_t lda, const void *B, int64_t ldb,
+                      int32_t transpose_b, const void *bias, xtc_dtype bias_dtype, const void *R, int64_t ldr,
+                      xtc_dtype r_dtype, int32_t activation, void *C, int64_t ldc, void *Z, int64_t ldz,
+                      void *workspace, int64_t workspace_bytes, xtc_dtype dtype, xtc_dtype out_dtype, void *stream) {
+    if (dtype != XTC_BF16 || !known(out_dtype) || (bias && !known(bias_dtype)) || (R && !known(r_dtype)))
+        return XTC_ERR_BAD_DTYPE;
+    if (T < 0 || N < 0 || K < 0 || activation < XTC_NO_ACTIVATION || activation > XTC_SILU) return XTC_ERR_BAD_SHAPE;
+    LinearArgs a = {};
+    a.T = T; a.N = (int)N; a.K = (int)K; a.G = 1;
+    a.A = A; a.lda = lda; a.B = B; a.ldb = ldb;
+    a.C = C; a.ldc = ldc;
+    a.out_bf16 = out_dtype == XTC_BF16;
+    a.bias = bias; a.bias_f32 = bias_dtype == XTC_F32;
+    a.R = R; a.ldr = ldr; a.r_f32 = r_dtype == XTC_F32;
+    a.Z = Z; a.ldz = ldz;
+    a.act = activation;
+    a.part = static_cast<float *>(workspace);
+    const xtc_status st = check_product(a, N, K, 1, transpose_b ? K : N, transpose_b ? N : K, N, out_dtype, 2);
+    if (st != XTC_OK) return st;
+    if ((R && ldr > kMostStride) || (Z && ldz > kMostStride)) return XTC_ERR_TOO_LARGE;
+    if ((R && ldr < least(N)) || (Z && ldz < least(N))) return XTC_ERR_BAD_LEADING_DIM;
+    if (!aligned_to(bias, size_of(bias_dtype)) || !aligned_to(R, size_of(r_dtype)) || !aligned_to(Z, size_of(out_dtype)) ||
+        !aligned_to(workspace, 16))
+        return XTC_ERR_MISALIGNED;
+    if (T == 0 || N == 0) return XTC_OK;
+    if (!C || (K > 0 && (!A || !B))) return XTC_ERR_NULL_POINTER;
+    const int64_t need = xtc_linear_workspace(T, N, K, transpose_b);
+    if (workspace_bytes < need) return XTC_ERR_BAD_SHAPE;
+    if (need > 0 && !workspace) return XTC_ERR_NULL_POINTER;
+    return launch_linear(a, transpose_b != 0, static_cast<hipStream_t>(stream));
+}
+
+int64_t xtc_linear_wgrad_workspace(int64_t T, int64_t N, int64_t K) {
+    if (T < 0 || N < 0 || K < 0 || T > kMostExtent || N > kMostExtent || K > kMostExtent) return -1;
+    if (N == 0 || K == 0) return 0;
+    LinearArgs a = {};
+    a.T = T; a.N = (int)N; a.K = (int)K;
+    return linear_wgrad_workspace(a);
+}
+
+xtc_status xtc_linear_wgrad(int64_t T, int64_t N, int64_t K, const void *A, int64_t lda, const void *DY, int64_t lddy,
+                            void *DB, int64_t lddb, void *workspace, int64_t workspace_bytes, xtc_dtype dtype,
+                            xtc_dtype out_dtype, void *stream) {
+    if (dtype != XTC_BF16 || !known(out_dtype)) return XTC_ERR_BAD_DTYPE;
+    if (T < 0 || N < 0 || K < 0) return XTC_ERR_BAD_SHAPE;
+    LinearArgs a = {};
+    a.T = T; a.N = (int)N; a.K = (int)K; a.G = 1;
+    a.A = A; a.lda = lda; a.B = DY; a.ldb = lddy;
+    a.C = DB; a.ldc = lddb;
+    a.out_bf16 = out_dtype == XTC_BF16;
+    a.part = static_cast<float *>(workspace);
+    const xtc_status st = check_product(a, N, K, 1, N, T, N, out_dtype, 2);
+    if (st != XTC_OK) return st;
+    if (!aligned_to(workspace, 16)) return XTC_ERR_MISALIGNED;
+    if (N == 0 || K == 0) return XTC_OK;
+    if (!DB || (T > 0 && (!A || !DY))) return XTC_ERR_NULL_POINTER;
+    const int64_t need = xtc_linear_wgrad_workspace(T, N, K);
+    if (workspace_bytes < need) return XTC_ERR_BAD_SHAPE;
+    if (need > 0 && !workspace) return XTC_ERR_NULL_POINTER;
+    return launch_linear_wgrad(a, static_cast<hipStream_t>(stream));
+}
+
+int64_t xtc_activation_backward_workspace(int64_t T, int64_t N) {
+    if (T < 0 || N < 0 || T > kMostExtent || N > kMostExtent) return -1;
+    return N == 0 ? 0 : 4 * activation_slabs(T, N) * N;
+}
+
+xtc_status xtc_activation_backward(int64_t T, int64_t N, const void *DY, int64_t lddy, xtc_dtype dy_dtype, const void *Z,
+                                   int64_t ldz, xtc_dtype z_dtype, int32_t activation, void *DZ, int64_t lddz, float *DB,
+                                   void *workspace, int64_t workspace_bytes, void *stream) {
+    const bool none = activation == XTC_NO_ACTIVATION;      // Z is not read
+    if (!known(dy_dtype) || (!none && !known(z_dtype))) return XTC_ERR_BAD_DTYPE;
+    if (T < 0 || N < 0 || activation < XTC_NO_ACTIVATION || activation > XTC_SILU) return XTC_ERR_BAD_SHAPE;
+    if (T > kMostExtent || N > kMostExtent || lddy > kMostStride || (!none && ldz > kMostStride) || lddz > kMostStride)
+        return XTC_ERR_TOO_LARGE;
+    if (lddy < least(N) || (!none && ldz < least(N)) || lddz < least(N)) return XTC_ERR_BAD_LEADING_DIM;
+    if (!aligned_to(DY, size_of(dy_dtype)) || (!none && !aligned_to(Z, size_of(z_dtype))) || !aligned_to(DZ, 2) ||
+        !aligned_to(DB, 4) || !aligned_to(workspace, 16))
+        return XTC_ERR_MISALIGNED;
+    if (N == 0 || (T == 0 && !DB)) return XTC_OK;
+    if ((T > 0 && (!DY || !DZ || (!none && !Z))) || (DB && !workspace)) return XTC_ERR_NULL_POINTER;
+    if (DB && workspace_bytes < xtc_activation_backward_workspace(T, N)) return XTC_ERR_BAD_SHAPE;
+    ActivationArgs a = {};
+    a.T = T; a.N = (int)N;
+    a.DY = DY; a.lddy = lddy; a.dy_f32 = dy_dtype == XTC_F32;
+    a.Z = none ? DY : Z; a.ldz = none ? lddy : ldz; a.z_f32 = none ? a.dy_f32 : z_dtype == XTC_F32;
+    a.act = activation;
+    a.DZ = DZ; a.lddz = lddz;
+    a.DB = DB; a.partial = static_cast<float *>(workspace);
+    return launch_activation_backward(a, static_cast<hipStream_t>(stream));
+}
+
 // Not part of the ABI: the kernel of a product of contiguous, 16-byte aligned
 // operands (`grouped`: with ends), as grouped_kernel() numbers them, so that the tests
 // can see that their sizes reach every one.  Pure host function.

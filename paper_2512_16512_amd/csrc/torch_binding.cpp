@@ -432,6 +432,104 @@ PyObject *matmul_fp8(PyObject *, PyObject *const *args, Py_ssize_t n) {
     }
 }
 
+xtc_dtype code_of(const at::Tensor *t) { return !t || t->scalar_type() == at::kFloat ? XTC_F32 : XTC_BF16; }
+bool either(const at::Tensor &t) { return t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16; }
+bool small_int(PyObject *o, long *out) {
+    if (!PyLong_CheckExact(o)) return false;
+    int overflow = 0;
+    *out = PyLong_AsLongAndOverflow(o, &overflow);
+    return overflow == 0 && *out > -(1L << 30) && *out < (1L << 30);
+}
+
+// linear(a, b, bias or None, residual or None, activation's code, transpose_b, keep, out or None, dtype or None): out,
+// or (out, z)
+PyObject *linear(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    const at::Tensor *t[4], *given = nullptr;
+    long act;
+    if (n != 9 || modes_active() || !tensors(args, t, 4 | 8) || !small_int(args[4], &act) || !truth(args[5]) ||
+        !truth(args[6]) || (args[7] != Py_None && !plain(args[7], &given)))
+        Py_RETURN_NONE;
+    const at::Tensor &a = *t[0], &b = *t[1];
+    if (a.dim() != 2 || b.dim() != 2) Py_RETURN_NONE;
+    const bool turned = args[5] == Py_True, keep = args[6] == Py_True;
+    const int64_t T = a.size(0), K = a.size(1), N = b.size(turned ? 0 : 1);
+    if (!matrix(a, at::kBFloat16, T, K, a) || !matrix(b, at::kBFloat16, turned ? N : K, turned ? K : N, a) ||
+        (t[2] && (!either(*t[2]) || !vector_of(*t[2], t[2]->scalar_type(), N, a))) ||
+        (t[3] && (!either(*t[3]) || !matrix(*t[3], t[3]->scalar_type(), T, N, a))))
+        Py_RETURN_NONE;
+    try {
+        const c10::DeviceGuard on(a.device());
+        at::Tensor r[2], work;
+        xtc_dtype code;
+        if (!result(given, args[8], {T, N}, a, &r[0], &code)) Py_RETURN_NONE;
+        if (keep) r[1] = fresh({T, N}, r[0].scalar_type(), a);
+        const int64_t size = xtc_linear_workspace(T, N, K, turned);
+        if (size < 0) Py_RETURN_NONE;
+        if (size > 0) work = fresh({size}, at::kByte, a);
+        void *stream = stream_of(a);
+        if (unlocked(xtc_linear, T, N, K, a.data_ptr(), row_stride(a), b.data_ptr(), row_stride(b), turned, data(t[2]),
+                     code_of(t[2]), data(t[3]), t[3] ? row_stride(*t[3]) : 0, code_of(t[3]), (int32_t)act,
+                     r[0].data_ptr(), row_stride(r[0]), keep ? r[1].data_ptr() : nullptr, at_least_1(N),
+                     size > 0 ? work.data_ptr() : nullptr, size, XTC_BF16, code, stream) != XTC_OK)
+            Py_RETURN_NONE;
+        if (keep) return tuple_of(r);
+        return given ? Py_NewRef(args[7]) : wrapped(std::move(r[0]));
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+}
+
+// linear_wgrad(a, dy, out or None, dtype or None)
+PyObject *linear_wgrad(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    const at::Tensor *t[3];
+    if (n != 4 || modes_active() || !tensors(args, t, 4)) Py_RETURN_NONE;
+    const at::Tensor &a = *t[0], &dy = *t[1];
+    if (a.dim() != 2 || dy.dim() != 2) Py_RETURN_NONE;
+    const int64_t T = a.size(0), K = a.size(1), N = dy.size(1);
+    if (!matrix(a, at::kBFloat16, T, K, a) || !matrix(dy, at::kBFloat16, T, N, a)) Py_RETURN_NONE;
+    try {
+        const c10::DeviceGuard on(a.device());
+        at::Tensor c, work;
+        xtc_dtype code;
+        if (!result(t[2], args[3], {K, N}, a, &c, &code)) Py_RETURN_NONE;
+        const int64_t size = xtc_linear_wgrad_workspace(T, N, K);
+        if (size < 0) Py_RETURN_NONE;
+        if (size > 0) work = fresh({size}, at::kByte, a);
+        void *stream = stream_of(a);
+        if (unlocked(xtc_linear_wgrad, T, N, K, a.data_ptr(), row_stride(a), dy.data_ptr(), row_stride(dy), c.data_ptr(),
+                     row_stride(c), size > 0 ? work.data_ptr() : nullptr, size, XTC_BF16, code, stream) != XTC_OK)
+            Py_RETURN_NONE;
+        return t[2] ? Py_NewRef(args[2]) : wrapped(std::move(c));
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+}
+
+// activation_backward(dy, z, activation's code): (dz, dbias)
+PyObject *activation_backward(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    const at::Tensor *t[2];
+    long act;
+    if (n != 3 || modes_active() || !tensors(args, t) || !small_int(args[2], &act)) Py_RETURN_NONE;
+    const at::Tensor &dy = *t[0], &z = *t[1];
+    if (dy.dim() != 2 || !either(dy) || !either(z)) Py_RETURN_NONE;
+    const int64_t T = dy.size(0), N = dy.size(1);
+    if (!matrix(dy, dy.scalar_type(), T, N, dy) || !matrix(z, z.scalar_type(), T, N, dy)) Py_RETURN_NONE;
+    try {
+        const c10::DeviceGuard on(dy.device());
+        const int64_t size = xtc_activation_backward_workspace(T, N);
+        if (size < 0) Py_RETURN_NONE;
+        at::Tensor dz = fresh({T, N}, at::kBFloat16, dy), db = fresh({N}, at::kFloat, dy), work = fresh({size}, at::kByte, dy);
+        void *stream = stream_of(dy);
+        if (unlocked(xtc_activation_backward, T, N, dy.data_ptr(), row_stride(dy), code_of(&dy), z.data_ptr(),
+                     row_stride(z), code_of(&z), (int32_t)act, dz.data_ptr(), at_least_1(N),
+                     static_cast<float *>(db.data_ptr()), work.data_ptr(), size, stream) != XTC_OK)
+            Py_RETURN_NONE;
+        return pair(std::move(dz), std::move(db));
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+}
+
 // matmul_grouped(a, b, ends, transpose_b, out or None, relu, dtype or None)
 PyObject *matmul_grouped(PyObject *, PyObject *const *args, Py_ssize_t n) {
     const at::Tensor *t[3], *given = nullptr;
@@ -526,6 +624,9 @@ PyMethodDef kMethods[] = {
     {"layernorm_backward", fast<layernorm_backward>(), METH_FASTCALL, "layernorm_backward(dy, x, weight, mean, rstd, dresidual)"},
     {"quantize_fp8", fast<quantize_fp8>(), METH_FASTCALL, "quantize_fp8(x, block_rows)"},
     {"matmul_fp8", fast<matmul_fp8>(), METH_FASTCALL, "matmul_fp8(a, a_scale, b, b_scale, out, relu, dtype)"},
+    {"linear", fast<linear>(), METH_FASTCALL, "linear(a, b, bias, residual, activation, transpose_b, keep, out, dtype)"},
+    {"linear_wgrad", fast<linear_wgrad>(), METH_FASTCALL, "linear_wgrad(a, dy, out, dtype)"},
+    {"activation_backward", fast<activation_backward>(), METH_FASTCALL, "activation_backward(dy, z, activation)"},
     {"matmul_grouped", fast<matmul_grouped>(), METH_FASTCALL, "matmul_grouped(a, b, ends, transpose_b, out, relu, dtype)"},
     {"matmul_grouped_wgrad", fast<matmul_grouped_wgrad>(), METH_FASTCALL, "matmul_grouped_wgrad(a, dy, ends, out, dtype)"},
     {"matmul_grouped_fp8", fast<matmul_grouped_fp8>(), METH_FASTCALL,

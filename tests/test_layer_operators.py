@@ -217,3 +217,192 @@ def test_layernorm_backward_gives_the_same_bits_again():
     for _ in range(3):
         again = x.layernorm_backward(dy, dev(xs), dev(w), n.mean, n.rstd)
         assert all(torch.equal(p, q) for p, q in zip(first, again))
+
+
+# ------------------------------------------------------------ linear layer
+
+ACTS = [None, "relu", "gelu", "gelu_tanh", "silu"]
+C2 = 2 * math.sqrt(2 / math.pi)
+
+
+def act_reference(z, act):
+    """The activation and its derivative in 64 bits, and how far the kernel's fp32 values of both may be off for an exact z.
+
+    2^(x log2 e): the product and the constant round (2u |x|), the instruction by 2u; 1 / (1 + e) is a reciprocal
+    (2u) of a rounded sum; six roundings make gelu_tanh's argument.  erff is within 16 steps."""
+    if act is None:
+        return z, torch.ones_like(z), torch.zeros_like(z), torch.zeros_like(z)
+    if act == "relu":
+        return z.clamp_min(0), (z > 0).double(), torch.zeros_like(z), torch.zeros_like(z)
+    if act == "gelu":
+        cdf, pdf = torch.special.ndtr(z), torch.exp(-0.5 * z * z) / math.sqrt(2 * math.pi)
+        return (z * cdf, cdf + z * pdf, 20 * U * z.abs(),
+                20 * U + z.abs() * pdf * (8 * U + 4 * U * z * z))
+    arg = z if act == "silu" else C2 * z * (1 + 0.044715 * z * z)
+    darg = torch.ones_like(z) if act == "silu" else C2 * (1 + 3 * 0.044715 * z * z)
+    q = torch.sigmoid(arg)
+    e_q = q * ((1 - q) * (8 * U * arg.abs() + 4 * U) + 4 * U) + 2.0 ** -126
+    return (z * q, q + z * q * (1 - q) * darg, z.abs() * e_q + 2 * U * (z * q).abs(),
+            e_q * (1 + z.abs() * darg) + 10 * U * (q + z.abs() * q * darg))
+
+
+def linear_reference(a, b, bias, r, act, splits=16):
+    """z and the layer's result in 64 bits, and how far the kernel's unrounded ones may be off."""
+    a, b = a.double(), b.double()
+    K = a.shape[1]
+    z = a @ b
+    e_z = 2 * U * (K + 8 + splits) * (a.abs() @ b.abs())
+    if bias is not None:
+        z = z + bias.double()
+        e_z = e_z + 2 * U * (z.abs() + bias.double().abs())
+    y, _, e_act, _ = act_reference(z, act)
+    e_y = 1.13 * e_z + e_act + U * y.abs()               # no activation is steeper than 1.13
+    if r is not None:
+        y = y + r.double()
+        e_y = e_y + U * (y.abs() + r.double().abs())
+    return z, y, e_z, e_y
+
+
+def linear_case(T, N, K, seed, scale=1.0):
+    a = as_type(normal(seed, T, K), "bf16")
+    b = as_type(scale * normal(seed + 1, K, N) / math.sqrt(max(K, 1)), "bf16")
+    return a, b, normal(seed + 2, N), 2 * normal(seed + 3, T, N)
+
+
+LAYERS = [(1, 1, 1), (1, 64, 64), (3, 5, 7), (1, 4096, 512), (7, 130, 129), (16, 256, 512), (17, 129, 1000), (33, 72, 136),
+          (64, 64, 64), (5, 1000, 2047), (100, 300, 640), (65, 512, 2048), (130, 264, 1032), (257, 513, 384), (300, 1024, 256)]
+
+
+@pytest.mark.parametrize("transpose_b", [False, True])
+@pytest.mark.parametrize("T,N,K", LAYERS)
+def test_linear(T, N, K, transpose_b):
+    a, b, bias, r = linear_case(T, N, K, T + N + K)
+    stored = b.t().contiguous() if transpose_b else b
+    for i, act in enumerate(ACTS):
+        out, other = ("f32", "bf16") if i % 2 else ("bf16", "f32")
+        bias_t, r_t = as_type(bias, other), as_type(r, out if i < 3 else other)
+        for odd in (False, True):
+            what = "linear %s" % ((T, N, K, transpose_b, act, out, odd),)
+            say(what)
+            z, y, e_z, e_y = linear_reference(a, b, bias_t, r_t, act)
+            got, kept = x.linear(dev(a, odd), dev(stored, odd), bias=dev(bias_t), residual=dev(r_t, odd), activation=act,
+                                 transpose_b=transpose_b, keep=True, dtype=torch.float32 if out == "f32" else torch.bfloat16)
+            tail = BF16 if out == "bf16" else U
+            assert got.dtype == kept.dtype == (torch.float32 if out == "f32" else torch.bfloat16)
+            within(host(got), y, tail * y.abs() + (1 + tail) * e_y, what)
+            within(host(kept), z, tail * z.abs() + (1 + tail) * e_z, what + " z")
+    z, y, e_z, e_y = linear_reference(a, b, None, None, None)
+    got = x.linear(dev(a), dev(stored), transpose_b=transpose_b)
+    assert got.dtype == torch.float32
+    within(host(got), y, e_y + U * y.abs(), "nothing but the product")
+
+
+@pytest.mark.parametrize("T,N,K", [(0, 5, 8), (4, 0, 8), (3, 5, 0), (0, 0, 0)])
+def test_linear_empty(T, N, K):
+    a, b, bias, r = linear_case(T, N, K, 3)
+    for turned in (False, True):
+        got, z = x.linear(dev(a), dev(b.t().contiguous() if turned else b), dev(bias.float()), dev(r.float()), "silu", turned, True)
+        assert got.shape == z.shape == (T, N)
+        if K == 0 and T and N:
+            want = bias.float().double()
+            within(host(z), want.expand(T, N), U * want.abs(), "bias alone")
+    dw = x.linear_wgrad(dev(a), dev(as_type(r, "bf16")))
+    assert dw.shape == (K, N) and (T or not bool(dw.any()))
+    dz, db = x.activation_backward(dev(r.float()), dev(r.float()), "gelu")
+    assert dz.shape == (T, N) and db.shape == (N,) and (T or not bool(db.any()))
+
+
+def test_linear_writes_its_own_columns_only():
+    for T, N, K in ((37, 150, 200), (3, 30, 2048), (300, 261, 400)):
+        a, b, bias, _ = linear_case(T, N, K, 11)
+        bias = bias.float()
+        for dtype in (torch.float32, torch.bfloat16):
+            wide = torch.full((T, N + 13), 5.0, device="cuda", dtype=dtype)
+            got = x.linear(dev(a), dev(b), dev(bias), activation="relu", out=wide[:, 3:N + 3])
+            _, y, _, e = linear_reference(a, b, bias, None, "relu")
+            tail = BF16 if dtype == torch.bfloat16 else U
+            within(host(got), y, tail * y.abs() + (1 + tail) * e, "out")
+            assert bool((wide[:, :3] == 5).all()) and bool((wide[:, N + 3:] == 5).all())
+
+
+@pytest.mark.parametrize("T", [3, 200])
+def test_linear_nan_stays_in_its_row_and_column(T):
+    """A NaN behind the end of k, or in another row, does not reach a result; relu keeps it."""
+    K, N = 136, 140
+    a, b, bias, _ = linear_case(T, N, K + 16, 5)
+    a[:, K:], b[K:] = float("nan"), float("nan")
+    a[1, 5], b[130, 77] = float("nan"), float("nan")
+    for turned in (False, True):
+        stored = b.t().contiguous() if turned else b
+        stored = dev(stored)[:, :K] if turned else dev(stored)[:K]
+        got = host(x.linear(dev(a)[:, :K], stored, dev(bias.float()), activation="relu", transpose_b=turned))
+        bad = torch.isnan(got)
+        assert bool(bad[1].all()) and bool(bad[:, 77].all()) and int(bad.sum()) == T + N - 1
+
+
+@pytest.mark.parametrize("T,N,K", [(1, 1, 1), (3, 5, 7), (64, 64, 64), (1000, 130, 72), (129, 264, 136), (2048, 64, 128),
+                                   (4099, 40, 264), (2047, 129, 70), (600, 1032, 520)])
+def test_linear_wgrad(T, N, K):
+    a, dy = as_type(normal(K, T, K), "bf16"), as_type(normal(N, T, N), "bf16")
+    ref, mag = a.double().t() @ dy.double(), a.double().abs().t() @ dy.double().abs()
+    for out in (torch.float32, torch.bfloat16):
+        for odd in (False, True):
+            say("linear_wgrad", T, N, K, out, odd)
+            got = x.linear_wgrad(dev(a, odd), dev(dy, odd), dtype=out)
+            tail = BF16 if out == torch.bfloat16 else U
+            within(host(got), ref, 2 * U * (T + 24) * mag + tail * ref.abs(), "linear_wgrad")
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("T,N", [(1, 1), (3, 7), (5, 512), (600, 130), (33, 1021), (2049, 520), (9000, 40)])
+def test_activation_backward(T, N, act):
+    for dy_t, z_t in (("bf16", "bf16"), ("f32", "f32"), ("f32", "bf16")):
+        dy, z = as_type(normal(T, T, N), dy_t), as_type(3 * normal(N, T, N), z_t)
+        _, slope, _, e = act_reference(z.double(), act)
+        ref, off = dy.double() * slope, dy.double().abs() * e + U * (dy.double() * slope).abs()
+        for odd in (False, True):
+            say("activation_backward", T, N, act, dy_t, z_t, odd)
+            dz, db = x.activation_backward(dev(dy, odd), dev(z, odd), act)
+            assert dz.dtype == torch.bfloat16 and db.dtype == torch.float32
+            within(host(dz), ref, BF16 * ref.abs() + (1 + BF16) * off + 2.0 ** -133, "dz")
+            within(host(db), ref.sum(0), (T + 8) * U * ref.abs().sum(0) + off.sum(0), "dbias")
+
+
+@pytest.mark.parametrize("act", ACTS[1:])
+def test_activations_far_from_zero(act):
+    """Large, infinite and NaN arguments: the limits, and no NaN where there is a limit."""
+    v = torch.tensor([[-3e38, -1e4, -90.0, -20.0, -0.0, 0.0, 20.0, 90.0, 1e4, 3e37, float("inf"), float("nan")]])
+    one = torch.ones(1, 1).bfloat16()
+    got = host(x.linear(dev(one), dev(torch.zeros(1, 12).bfloat16()), dev(v[0]), activation=act))[0]
+    _, slopes = None, host(x.activation_backward(dev(torch.ones(1, 12)), dev(v), act)[0])[0]
+    assert bool((got[:3].abs() < 1e-30).all()) and bool((slopes[:3].abs() < 1e-30).all())
+    assert torch.equal(got[7:11], v[0, 7:11].double()) and bool((slopes[7:10] == 1).all())
+    assert bool(torch.isnan(got[11])) and bool(torch.isnan(slopes[11]))
+    assert abs(got[4].item()) == abs(got[5].item()) == 0
+
+
+@pytest.mark.parametrize("act", ACTS)
+def test_linear_gradients_against_differences(act):
+    """Central differences of the 64-bit layer: the operands of the products are bf16, so is dz."""
+    T, N, K, step = 19, 40, 72, 1e-5
+    a, b, bias, r = linear_case(T, N, K, 8)
+    bias, dout = bias.float(), as_type(normal(9, T, N), "bf16")
+    _, z = x.linear(dev(a), dev(b), dev(bias), dev(r.float()), act, keep=True)
+    dz, db = x.activation_backward(dev(dout), z, act)
+    da, dw, dwt = (host(g) for g in (x.linear(dz, dev(b), transpose_b=True), x.linear_wgrad(dev(a), dz),
+                                     x.linear_wgrad(dz, dev(a))))
+    d, p, q = host(dz).abs(), a.double().abs(), b.double().abs()
+    within(dwt.t(), dw, 4 * U * (T + 24) * (p.t() @ d), "the weights' gradient of the other layout")
+
+    def loss(*leaf):
+        return (act_reference(leaf[0] @ leaf[1] + leaf[2], act)[0] * dout.double()).sum().item()
+
+    # dz is rounded once (2^-8 of each value); the differences' own error is far below that
+    leaf = [a.double(), b.double(), bias.double()]
+    for i, (g, mag) in enumerate(((da, d @ q.t()), (dw, p.t() @ d), (host(db), d.sum(0)))):
+        for seed in range(3):
+            v = normal(40 + 10 * i + seed, *leaf[i].shape)
+            up, down = list(leaf), list(leaf)
+            up[i], down[i] = leaf[i] + step * v, leaf[i] - step * v
+            num = (loss(*up) - loss(*down)) / (2 * step)
+            assert abs(num - (g * v).sum().item()) <= 1.5 * BF16 * (mag * v.abs()).sum().item()

@@ -48,6 +48,68 @@ def test_layernorm_backward_workspace():
     assert x.xtc_layernorm_backward_workspace(4, 200) >= 8 * 200
 
 
+LINEAR = dict(T=4, N=130, K=200, A=BAD, lda=200, B=BAD, ldb=130, transpose_b=0, bias=BAD, bias_dtype=0, R=BAD, ldr=130,
+              r_dtype=1, activation=2, C=BAD, ldc=130, Z=BAD, ldz=130, workspace=BAD, workspace_bytes=1 << 30, dtype=1,
+              out_dtype=1)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(dtype=0), 4), (dict(dtype=2), 4), (dict(out_dtype=2), 4), (dict(bias_dtype=2), 4), (dict(r_dtype=2), 4),
+    (dict(T=-1), 2), (dict(N=-1), 2), (dict(K=-1), 2), (dict(activation=-1), 2), (dict(activation=5), 2),
+    (dict(lda=199), 3), (dict(ldb=129), 3), (dict(ldb=199, transpose_b=1), 3), (dict(ldc=129), 3), (dict(ldr=129), 3),
+    (dict(ldz=129), 3), (dict(A=0), 1), (dict(B=0), 1), (dict(C=0), 1),
+    (dict(A=BAD + 1), 9), (dict(B=BAD + 1), 9), (dict(bias=BAD + 2), 9), (dict(R=BAD + 1), 9), (dict(C=BAD + 1), 9),
+    (dict(Z=BAD + 1), 9), (dict(out_dtype=0, C=BAD + 2), 9), (dict(workspace=BAD + 8), 9),
+    (dict(T=BIG), 7), (dict(N=BIG), 7), (dict(K=BIG), 7), (dict(lda=BIG), 7), (dict(ldr=BIG), 7), (dict(ldz=BIG), 7),
+    (dict(T=1 << 30, N=1 << 30, ldb=1 << 30, ldc=1 << 30, ldr=1 << 30, ldz=1 << 30, workspace_bytes=1 << 62), 7),
+    (dict(T=0, A=0), 0), (dict(N=0, B=0, C=0), 0), (dict(N=0, ldb=1, ldc=1, ldr=1, ldz=1), 0),
+])
+def test_linear_refuses(change, status):
+    assert call(x.xtc_linear, LINEAR, **change) == status
+
+
+def test_linear_workspaces():
+    assert x.xtc_linear_workspace(-1, 4, 4, 0) == -1 and x.xtc_linear_workspace(4, 4, BIG, 0) == -1
+    assert x.xtc_linear_wgrad_workspace(4, -1, 4) == -1 and x.xtc_activation_backward_workspace(BIG, 4) == -1
+    assert x.xtc_linear_workspace(0, 4, 4, 0) == 0 and x.xtc_linear_wgrad_workspace(4, 0, 4) == 0
+    # a reduction long enough that its parts go to several workgroups, each part's sums a whole result
+    need = x.xtc_linear_wgrad_workspace(16384, 256, 256)
+    assert need > 0 and need % (4 * 256 * 256) == 0
+    assert call(x.xtc_linear_wgrad, WGRAD, T=16384, N=256, K=256, lda=256, lddy=256, lddb=256, workspace_bytes=need - 1) == 2
+    assert call(x.xtc_linear_wgrad, WGRAD, T=16384, N=256, K=256, lda=256, lddy=256, lddb=256, workspace_bytes=need,
+                workspace=0) == 1
+    assert x.xtc_activation_backward_workspace(4, 200) >= 4 * 200 and x.xtc_activation_backward_workspace(0, 200) >= 4 * 200
+
+
+WGRAD = dict(T=4, N=130, K=200, A=BAD, lda=200, DY=BAD, lddy=130, DB=BAD, lddb=130, workspace=BAD,
+             workspace_bytes=1 << 30, dtype=1, out_dtype=0)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(dtype=0), 4), (dict(out_dtype=2), 4), (dict(T=-1), 2), (dict(N=-1), 2), (dict(K=-1), 2), (dict(lda=199), 3),
+    (dict(lddy=129), 3), (dict(lddb=129), 3), (dict(A=0), 1), (dict(DY=0), 1), (dict(DB=0), 1), (dict(DY=BAD + 1), 9),
+    (dict(DB=BAD + 2), 9), (dict(workspace=BAD + 4), 9), (dict(T=BIG), 7), (dict(lddb=BIG), 7),
+    (dict(N=0, lddy=1, lddb=1), 0), (dict(K=0, lda=1, DB=0), 0),
+])
+def test_linear_wgrad_refuses(change, status):
+    assert call(x.xtc_linear_wgrad, WGRAD, **change) == status
+
+
+SLOPE = dict(T=4, N=130, DY=BAD, lddy=130, dy_dtype=1, Z=BAD, ldz=130, z_dtype=0, activation=3, DZ=BAD, lddz=130, DB=BAD,
+             workspace=BAD, workspace_bytes=1 << 30)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(dy_dtype=2), 4), (dict(z_dtype=2), 4), (dict(T=-1), 2), (dict(N=-1), 2), (dict(activation=5), 2),
+    (dict(activation=-1), 2), (dict(workspace_bytes=x.xtc_activation_backward_workspace(4, 130) - 1), 2),
+    (dict(lddy=129), 3), (dict(ldz=129), 3), (dict(lddz=129), 3), (dict(DY=0), 1), (dict(Z=0), 1), (dict(DZ=0), 1),
+    (dict(workspace=0), 1), (dict(DY=BAD + 1), 9), (dict(Z=BAD + 2), 9), (dict(DZ=BAD + 1), 9), (dict(DB=BAD + 2), 9),
+    (dict(workspace=BAD + 8), 9), (dict(T=BIG), 7), (dict(lddz=BIG), 7), (dict(N=0), 0), (dict(T=0, DB=0), 0),
+])
+def test_activation_backward_refuses(change, status):
+    assert call(x.xtc_activation_backward, SLOPE, **change) == status
+
+
 # ------------------------------------------------ the conveniences' own checks
 
 
@@ -60,6 +122,12 @@ F32 = torch.float32
     (x.layernorm, (t(8, 4).t(), t(8)), ValueError, "unit stride"),
     (x.layernorm_backward, (t(4, 8), t(4, 8, dtype=E4M3), t(8), t(4), t(4)), TypeError, "x must be"),
     (x.layernorm_backward, (t(4, 8), t(4, 8), t(8), t(4), t(4)), ValueError, "CUDA"),
+    (x.linear, (t(4, 8, dtype=F32), t(8, 4)), TypeError, "a must be bfloat16"),
+    (x.linear, (t(4, 8), t(8, 4)), ValueError, "CUDA"),
+    (x.linear, (t(4, 8), t(8, 4), None, None, "tanh"), ValueError, "activation must be"),
+    (x.linear_wgrad, (t(4, 8), t(4, 4)), ValueError, "CUDA"),
+    (x.activation_backward, (t(4, 8), t(4, 8), "swish"), ValueError, "activation must be"),
+    (x.activation_backward, (t(4, 8, dtype=E4M3), t(4, 8), "relu"), TypeError, "dy must be"),
 ])
 def test_conveniences_refuse(fn, args, error, match):
     with pytest.raises(error, match=match):
@@ -68,6 +136,8 @@ def test_conveniences_refuse(fn, args, error, match):
 
 def test_the_native_entries_leave_other_tensors_to_python():
     a, v = t(4, 8), t(4, dtype=F32)
-    for name, args in (("layernorm", (a, t(8), t(8), None, 1e-6, False)), ("layernorm_backward", (a, a, t(8), v, v, None))):
+    for name, args in (("layernorm", (a, t(8), t(8), None, 1e-6, False)), ("layernorm_backward", (a, a, t(8), v, v, None)),
+                       ("linear", (a, t(8, 4), None, None, 0, False, False, None, None)),
+                       ("linear_wgrad", (a, a, None, None)), ("activation_backward", (a, a, 1))):
         fast = getattr(x._fast, name)
         assert fast(*args) is None and fast() is None and fast(*([None] * len(args))) is None
