@@ -544,6 +544,90 @@ xtc_status xtc_matmul_grouped_fp8(int64_t G, int64_t T, int64_t N, int64_t K,
                                   xtc_dtype out_dtype, int32_t relu, void *stream);
 
 /*
+ * xtc_route_experts -- the router of a mixture of experts: which experts T tokens
+ * go to, with which weights, and where their rows lie when sorted by expert, as
+ * the grouped products take them.
+ *
+ *  E, top     experts (1 to 1024) and how many a token chooses (1 to 16, at most E);
+ *             T * top at most 0x7FFFFF00.
+ *  scores     device, dtype (XTC_F32 or XTC_BF16) T x E, row stride lds.  -inf
+ *             forbids an expert; a NaN counts as above every number.
+ *  mask       device, T bytes, 0 for a token that goes nowhere (padding), or NULL.
+ *  expert     T x top: the experts of each token, the highest score first, of equal
+ *             scores the lowest index; -1 for a masked token.
+ *  p          T x top fp32: the softmax of the chosen scores; 0 for a masked token
+ *             and for one whose scores are all -inf.
+ *  row        T x top: the place of each choice among the rows sorted by expert, those
+ *             of an expert in the order of their tokens; -1 for a masked token.
+ *  token      T * top: the token of each of these rows; -1 behind the last one.
+ *  counts, ends  E each: the rows of each expert, and where they end.
+ *  loss       one fp32: the balance loss E / (top n^2) sum_e counts_e sum_t q_te, q the
+ *             softmax over all experts (0 for a row of -inf), n the tokens that are not
+ *             masked; 0 without any.  It is 1 where all experts are chosen equally.
+ *  workspace  xtc_route_experts_workspace(T, E) bytes, 16-byte aligned, written by the
+ *             call; too small is XTC_ERR_BAD_SHAPE.
+ * All arrays but scores are contiguous.  Outputs are the same bits in every call.  With
+ * T 0 counts, ends and loss are zeros.  Errors as for xtc_rmsnorm.
+ */
+xtc_status xtc_route_experts(int64_t T, int64_t E, int64_t top, const void *scores, int64_t lds,
+                             const uint8_t *mask, int32_t *expert, float *p, int32_t *row,
+                             int32_t *token, int32_t *counts, int32_t *ends, float *loss,
+                             void *workspace, int64_t workspace_bytes,
+                             xtc_dtype dtype, void *stream);
+
+/* Bytes of workspace; -1 for extents outside the limits.  Pure host function. */
+int64_t xtc_route_experts_workspace(int64_t T, int64_t E);
+
+/*
+ * xtc_route_experts_backward -- the gradient of the scores, from DP (T x top fp32, the
+ * gradient of p; NULL: zeros) and dloss, that of the balance loss:
+ *   DS = dloss E / (top n^2) q_e (counts_e - sum_i counts_i q_i), and at the chosen
+ *        experts p_j (DP_j - sum_i p_i DP_i) added; zeros for a masked token.
+ * scores, expert, p and counts as xtc_route_experts took and gave them (n is the sum of
+ * counts over top).  DS: device, out_dtype (XTC_F32 or XTC_BF16) T x E, row stride
+ * ldds.  Errors as for xtc_rmsnorm.
+ */
+xtc_status xtc_route_experts_backward(int64_t T, int64_t E, int64_t top, const float *DP,
+                                      const void *scores, int64_t lds, const int32_t *expert,
+                                      const float *p, const int32_t *counts, float dloss,
+                                      void *DS, int64_t ldds,
+                                      xtc_dtype dtype, xtc_dtype out_dtype, void *stream);
+
+/*
+ * xtc_combine_experts -- the experts' rows back at their tokens:
+ *   C[t] = RES[t] + sum_j p[t][j] * rows[row[t][j]], in fp32, over j in its order.
+ *
+ *  rows   device, dtype (XTC_F32 or XTC_BF16) R x D, row stride ldrows.
+ *  row    device, T x top, contiguous.  What lies outside 0 .. R - 1 (-1: a masked
+ *         choice) counts as a row of zeros.
+ *  p      device, T x top fp32, contiguous, or NULL: ones (the gradient of rows that
+ *         were copied to their experts).
+ *  RES    device, T x D of r_dtype (XTC_F32 or XTC_BF16), row stride ldr, or NULL.
+ *  C      device, out_dtype (XTC_F32 or XTC_BF16) T x D, row stride ldc.
+ * T or D 0 is a no-op; top 0 gives RES.  T * top at most 0x7FFFFF00.  Errors as for
+ * xtc_rmsnorm.
+ */
+xtc_status xtc_combine_experts(int64_t T, int64_t top, int64_t D, int64_t R,
+                               const void *rows, int64_t ldrows, const int32_t *row, const float *p,
+                               const void *RES, int64_t ldr, xtc_dtype r_dtype,
+                               void *C, int64_t ldc, xtc_dtype dtype, xtc_dtype out_dtype, void *stream);
+
+/*
+ * xtc_combine_experts_backward -- its gradients, for T * top rows each of which is one
+ * choice's at most (as xtc_route_experts gives them):
+ *   DROWS[row[t][j]] = p[t][j] * DOUT[t],  DP[t][j] = sum_d DOUT[t][d] rows[row[t][j]][d].
+ * Rows that belong to no token (token -1) are zeros in DROWS, DP of a masked choice is 0.
+ * DOUT: T x D of dout_dtype, row stride lddo; rows and DROWS of dtype (XTC_F32 or
+ * XTC_BF16 each); DP T x top fp32.  top >= 1, else XTC_ERR_BAD_SHAPE; with D 0 DP is
+ * zeros.  Errors as for xtc_rmsnorm.
+ */
+xtc_status xtc_combine_experts_backward(int64_t T, int64_t top, int64_t D, const void *DOUT, int64_t lddo,
+                                        xtc_dtype dout_dtype, const void *rows, int64_t ldrows,
+                                        const int32_t *row, const int32_t *token, const float *p,
+                                        void *DROWS, int64_t lddr, float *DP,
+                                        xtc_dtype dtype, void *stream);
+
+/*
  * xtc_default_schedule -- the schedule used when sched == NULL, chosen from
  * the problem shape (the paper's default_schedule of an exploration
  * strategy, Sec. 5.2).  For op == XTC_OP_CONV2D pass the implicit-GEMM

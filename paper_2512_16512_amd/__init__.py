@@ -143,6 +143,16 @@ def _load():
     lib.xtc_activation_backward.restype = i32
     lib.xtc_activation_backward_workspace.argtypes = [i64] * 2
     lib.xtc_activation_backward_workspace.restype = i64
+    lib.xtc_route_experts.argtypes = [i64] * 3 + [vp, i64] + [vp] * 9 + [i64, i32, vp]
+    lib.xtc_route_experts.restype = i32
+    lib.xtc_route_experts_workspace.argtypes = [i64] * 2
+    lib.xtc_route_experts_workspace.restype = i64
+    lib.xtc_route_experts_backward.argtypes = [i64] * 3 + [vp, vp, i64, vp, vp, vp, f32, vp, i64, i32, i32, vp]
+    lib.xtc_route_experts_backward.restype = i32
+    lib.xtc_combine_experts.argtypes = [i64] * 4 + [vp, i64, vp, vp, vp, i64, i32, vp, i64, i32, i32, vp]
+    lib.xtc_combine_experts.restype = i32
+    lib.xtc_combine_experts_backward.argtypes = [i64] * 3 + [vp, i64, i32, vp, i64, vp, vp, vp, vp, i64, vp, i32, vp]
+    lib.xtc_combine_experts_backward.restype = i32
     lib.xtc_matmul_grouped.argtypes = [i64] * 4 + [vp, i64, vp, i64, i64, i32, vp, vp, i64, i32, i32, i32, vp]
     lib.xtc_matmul_grouped.restype = i32
     lib.xtc_matmul_grouped_wgrad.argtypes = [i64] * 4 + [vp, i64, vp, i64, vp, vp, i64, i64, i32, i32, vp]
@@ -196,7 +206,8 @@ EXPORTS = ("xtc_matmul", "xtc_conv2d_nchw", "xtc_matmul_relu", "xtc_conv2d_nchw_
            "xtc_layernorm_backward", "xtc_layernorm_backward_workspace", "xtc_quantize_fp8",
            "xtc_matmul_fp8", "xtc_linear", "xtc_linear_workspace", "xtc_linear_wgrad", "xtc_linear_wgrad_workspace",
            "xtc_activation_backward", "xtc_activation_backward_workspace", "xtc_matmul_grouped", "xtc_matmul_grouped_wgrad", "xtc_matmul_grouped_fp8",
-           "xtc_default_schedule", "xtc_sched_occupancy", "xtc_sched_check",
+           "xtc_route_experts", "xtc_route_experts_workspace", "xtc_route_experts_backward", "xtc_combine_experts",
+           "xtc_combine_experts_backward", "xtc_default_schedule", "xtc_sched_occupancy", "xtc_sched_check",
            "xtc_sched_list", "xtc_status_str", "xtc_last_hip_error", "xtc_conv_max_k",
            "xtc_version")
 
@@ -312,6 +323,34 @@ def xtc_matmul_grouped_fp8(G, T, N, K, A, lda, SA, ldsa, B, ldb, stride_b, SB, l
                            out_dtype, relu=0, stream=0) -> int:
     return _lib.xtc_matmul_grouped_fp8(G, T, N, K, A, lda, SA, ldsa, B, ldb, stride_b, SB, ldsb, stride_sb, ends, C,
                                        ldc, out_dtype, relu, stream)
+
+
+def xtc_route_experts(T, E, top, scores, lds, mask, expert, p, row, token, counts, ends, loss, workspace,
+                      workspace_bytes, dtype, stream=0) -> int:
+    return _lib.xtc_route_experts(T, E, top, scores, lds, mask, expert, p, row, token, counts, ends, loss, workspace,
+                                  workspace_bytes, dtype, stream)
+
+
+def xtc_route_experts_workspace(T, E) -> int:
+    return _lib.xtc_route_experts_workspace(T, E)
+
+
+def xtc_route_experts_backward(T, E, top, DP, scores, lds, expert, p, counts, dloss, DS, ldds, dtype, out_dtype,
+                               stream=0) -> int:
+    return _lib.xtc_route_experts_backward(T, E, top, DP, scores, lds, expert, p, counts, dloss, DS, ldds, dtype,
+                                           out_dtype, stream)
+
+
+def xtc_combine_experts(T, top, D, R, rows, ldrows, row, p, RES, ldr, r_dtype, C, ldc, dtype, out_dtype,
+                        stream=0) -> int:
+    return _lib.xtc_combine_experts(T, top, D, R, rows, ldrows, row, p, RES, ldr, r_dtype, C, ldc, dtype, out_dtype,
+                                    stream)
+
+
+def xtc_combine_experts_backward(T, top, D, DOUT, lddo, dout_dtype, rows, ldrows, row, token, p, DROWS, lddr, DP, dtype,
+                                 stream=0) -> int:
+    return _lib.xtc_combine_experts_backward(T, top, D, DOUT, lddo, dout_dtype, rows, ldrows, row, token, p, DROWS,
+                                             lddr, DP, dtype, stream)
 
 
 def xtc_default_schedule(op, dtype, M, N, K) -> Sched:
@@ -877,3 +916,146 @@ def matmul_grouped_fp8(a, a_scale, b, b_scale, ends, out=None, relu=False, dtype
                                   ends.data_ptr(), out.data_ptr(), _ld(out), code, int(relu),
                                   _stream(torch, a.device)), "xtc_matmul_grouped_fp8")
     return out
+
+
+# ----------------------------------------------- the routing of a mixture
+
+
+#: What ``route_experts`` returns.  ``expert``, ``p``, ``row`` [T, top]: each token's experts (the highest score first),
+#: their weights, and the place of each choice among the rows sorted by expert; ``token`` [T * top]: the token of each of
+#: these rows; ``counts``, ``ends`` [E]: the rows of each expert and where they end (``matmul_grouped``'s ``ends``);
+#: ``loss``: the balance loss, a float32 scalar.  Places and counts are int32.
+Routing = namedtuple("Routing", "expert p row token counts ends loss")
+
+
+def _block(t, name, dtype, shape, device):
+    """Checks a contiguous operand."""
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, not %s" % (name, str(dtype).split(".")[1], t.dtype))
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError("%s must be contiguous %s" % (name, list(shape)))
+    if t.device != device:
+        raise ValueError("%s must be on %s" % (name, device))
+
+
+def route_experts(scores, top, mask=None):
+    """The ``top`` experts of each token: ``Routing(expert, p, row, token, counts, ends, loss)``.
+
+    ``scores`` [T, E] are float32 or bfloat16, E at most 1024 and ``top`` at most 16.  ``p`` is the softmax over a token's
+    chosen scores; of equal scores the lowest expert comes first.  Tokens where the boolean ``mask`` [T] is false go to
+    no expert: their ``expert`` and ``row`` are -1, their ``p`` zeros, and ``token`` is -1 for the rows behind ``ends[-1]``.
+    The balance loss is ``E / (top * n**2) * sum_e counts[e] * sum_t softmax(scores[t])[e]`` over the n tokens that are
+    left (1 where every expert has as many).  Nothing waits for the GPU."""
+    if _fast is not None:
+        r = _fast.route_experts(scores, top, mask)
+        if r is not None:
+            return Routing._make(r)
+    import torch
+    _matrix(scores, "scores", (torch.float32, torch.bfloat16))
+    T, E = scores.shape
+    if mask is not None:
+        _block(mask, "mask", torch.bool, (T,), scores.device)
+    if not 1 <= top <= E:
+        raise ValueError("top must be from 1 to the %d experts, not %d" % (E, top))
+    i32, f32 = (dict(dtype=d, device=scores.device) for d in (torch.int32, torch.float32))
+    r = Routing(torch.empty((T, top), **i32), torch.empty((T, top), **f32), torch.empty((T, top), **i32),
+                torch.empty(T * top, **i32), torch.empty(E, **i32), torch.empty(E, **i32), torch.empty((), **f32))
+    size = xtc_route_experts_workspace(T, E)
+    work = torch.empty(max(size, 0), dtype=torch.uint8, device=scores.device)
+    with _on(torch, scores.device):
+        _check(xtc_route_experts(T, E, top, scores.data_ptr(), _ld(scores), _ptr(mask), r.expert.data_ptr(),
+                                 r.p.data_ptr(), r.row.data_ptr(), r.token.data_ptr(), r.counts.data_ptr(),
+                                 r.ends.data_ptr(), r.loss.data_ptr(), work.data_ptr(), size,
+                                 _dtype_code(torch, scores), _stream(torch, scores.device)), "xtc_route_experts")
+    return r
+
+
+def route_experts_backward(dp, scores, expert, p, counts, dloss=0.0, dtype=None):
+    """The gradient of ``route_experts``'s ``scores`` [T, E] (of their type, or ``dtype``) from that of ``p`` (``dp``
+    [T, top] float32, or None) and the balance loss's, the number ``dloss``; ``expert``, ``p`` and ``counts`` are its results."""
+    if _fast is not None:
+        r = _fast.route_experts_backward(dp, scores, expert, p, counts, dloss, dtype)
+        if r is not None:
+            return r
+    import torch
+    _matrix(scores, "scores", (torch.float32, torch.bfloat16))
+    T, E = scores.shape
+    if expert.dim() != 2:
+        raise ValueError("expert must be [T, top]")
+    top = expert.shape[1]
+    _block(expert, "expert", torch.int32, (T, top), scores.device)
+    _block(p, "p", torch.float32, (T, top), scores.device)
+    _block(counts, "counts", torch.int32, (E,), scores.device)
+    if dp is not None:
+        _block(dp, "dp", torch.float32, (T, top), scores.device)
+    code = _out_code(torch, scores.dtype if dtype is None else dtype)
+    ds = torch.empty((T, E), dtype=torch.bfloat16 if code else torch.float32, device=scores.device)
+    with _on(torch, scores.device):
+        _check(xtc_route_experts_backward(T, E, top, _ptr(dp), scores.data_ptr(), _ld(scores), expert.data_ptr(),
+                                          p.data_ptr(), counts.data_ptr(), dloss, ds.data_ptr(), max(E, 1),
+                                          _dtype_code(torch, scores), code, _stream(torch, scores.device)),
+               "xtc_route_experts_backward")
+    return ds
+
+
+def combine_experts(rows, row, p=None, residual=None, dtype=None):
+    """``out[t] = residual[t] + sum_j p[t, j] * rows[row[t, j]]`` [T, D] (float32 or bfloat16: ``dtype``): the experts'
+    rows back at their tokens.  ``rows`` [R, D] and ``residual`` [T, D] are float32 or bfloat16, ``row`` int32 and ``p``
+    float32 [T, top] as ``route_experts`` gives them; -1 in ``row`` counts as a row of zeros, no ``p`` as ones (the
+    gradient of ``x[token]``)."""
+    if _fast is not None:
+        r = _fast.combine_experts(rows, row, p, residual, dtype)
+        if r is not None:
+            return r
+    import torch
+    either = (torch.float32, torch.bfloat16)
+    _matrix(rows, "rows", either)
+    R, D = rows.shape
+    if row.dim() != 2:
+        raise ValueError("row must be [T, top]")
+    T, top = row.shape
+    _block(row, "row", torch.int32, (T, top), rows.device)
+    if p is not None:
+        _block(p, "p", torch.float32, (T, top), rows.device)
+    if residual is not None:
+        _matrix(residual, "residual", either, (T, D), rows.device)
+    code = _out_code(torch, dtype)
+    out = torch.empty((T, D), dtype=torch.bfloat16 if code else torch.float32, device=rows.device)
+    with _on(torch, rows.device):
+        _check(xtc_combine_experts(T, top, D, R, rows.data_ptr(), _ld(rows) if R else max(D, 1), row.data_ptr(), _ptr(p),
+                                   _ptr(residual), 0 if residual is None else _ld(residual),
+                                   XTC_F32 if residual is None else _dtype_code(torch, residual), out.data_ptr(),
+                                   max(D, 1), _dtype_code(torch, rows), code, _stream(torch, rows.device)),
+               "xtc_combine_experts")
+    return out
+
+
+def combine_experts_backward(dout, rows, row, token, p):
+    """``(drows, dp)`` of ``combine_experts`` from its result's gradient ``dout`` [T, D]; ``rows`` [T * top, D], ``row``,
+    ``token`` and ``p`` as ``route_experts`` sorts them.  ``drows`` is of the rows' type, zeros where ``token`` is -1;
+    ``dp`` [T, top] float32."""
+    if _fast is not None:
+        r = _fast.combine_experts_backward(dout, rows, row, token, p)
+        if r is not None:
+            return r
+    import torch
+    either = (torch.float32, torch.bfloat16)
+    _matrix(rows, "rows", either)
+    R, D = rows.shape
+    if row.dim() != 2:
+        raise ValueError("row must be [T, top]")
+    T, top = row.shape
+    if R != T * top:
+        raise ValueError("rows must hold %d rows, not %d" % (T * top, R))
+    _block(row, "row", torch.int32, (T, top), rows.device)
+    _block(token, "token", torch.int32, (R,), rows.device)
+    _block(p, "p", torch.float32, (T, top), rows.device)
+    _matrix(dout, "dout", either, (T, D), rows.device)
+    drows = torch.empty((R, D), dtype=rows.dtype, device=rows.device)
+    dp = torch.empty((T, top), dtype=torch.float32, device=rows.device)
+    with _on(torch, rows.device):
+        _check(xtc_combine_experts_backward(T, top, D, dout.data_ptr(), _ld(dout), _dtype_code(torch, dout),
+                                            rows.data_ptr(), _ld(rows), row.data_ptr(), token.data_ptr(), p.data_ptr(),
+                                            drows.data_ptr(), max(D, 1), dp.data_ptr(), _dtype_code(torch, rows),
+                                            _stream(torch, rows.device)), "xtc_combine_experts_backward")
+    return drows, dp

@@ -23,7 +23,7 @@ OBJDIR = os.path.join(HERE, "_build")
 
 SOURCES = ["gemm_f32.hip", "gemm_bf16.hip", "conv2d_f32.hip", "conv2d_bf16.hip", "norm.hip",
            "grouped.hip", "grouped_tile.hip", "grouped_stream.hip", "linear.hip", "linear_tile.hip",
-           "linear_stream.hip", "xtc_api.cpp", "operators_api.cpp"]
+           "linear_stream.hip", "route.hip", "combine.hip", "xtc_api.cpp", "operators_api.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

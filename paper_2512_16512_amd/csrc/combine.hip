@@ -1,0 +1,121 @@
+// The rows of a mixture's experts back at their tokens:
+//
+//   out_t = residual_t + sum_j p_tj rows[row_tj],
+//
+// and the gradients drows[row_tj] = p_tj dout_t, dp_tj = <dout_t, rows[row_tj]>; sums are fp32, over j in
+// its order.  Rows outside the array (-1: a choice that was masked) count as nothing.
+#include "operators.h"
+#include "values.h"
+
+namespace xtc {
+namespace {
+
+constexpr int kWaves = 4, kColumns = 512;      // columns of a wave, eight a lane
+
+// A wave a token and 512 columns of it: kAtOnce rows are on their way together.
+constexpr int kAtOnce = 8;
+template <typename T, typename R, typename O>
+__global__ void __launch_bounds__(kWaves * 64) combine_kernel(CombineArgs p, int chunks) {
+    const int64_t id = (int64_t)blockIdx.x * kWaves + threadIdx.x / 64, t = id / chunks;
+    if (t >= p.T) return;
+    const int c = (int)(id - t * chunks) * kColumns + (threadIdx.x & 63) * 8, valid = p.D - c;
+    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (p.RES) load8(static_cast<const R *>(p.RES) + t * p.ldr + c, valid, sum);
+    for (int j0 = 0; j0 < p.top; j0 += kAtOnce) {
+        Raw8<T> v[kAtOnce];
+        float w[kAtOnce];
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            int64_t r = -1;
+            w[j] = 1.f;
+            if (j0 + j < p.top) {
+                r = p.row[t * p.top + j0 + j];
+                if (p.P) w[j] = p.P[t * p.top + j0 + j];
+            }
+            const bool in = r >= 0 && r < p.R;
+            w[j] = in ? w[j] : 0.f;
+            v[j] = raw8(static_cast<const T *>(p.rows) + (in ? r : 0) * p.ldrows + c, in ? valid : 0);
+        }
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += w[j] * v[j].at(i);
+    }
+    store8(static_cast<O *>(p.out) + t * p.ldo + c, valid, sum);
+}
+
+// A wave a token: its row of dout stays in registers over the rows of up to kAtOnce choices.
+template <typename T, typename G>
+__global__ void __launch_bounds__(kWaves * 64) combine_backward_kernel(CombineBackwardArgs p) {
+    const int64_t t = (int64_t)blockIdx.x * kWaves + threadIdx.x / 64;
+    const int lane = threadIdx.x & 63;
+    if (t >= p.T) return;
+    for (int j0 = 0; j0 < p.top; j0 += kAtOnce) {
+        float w[kAtOnce], dot[kAtOnce];
+        int64_t r[kAtOnce];
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            r[j] = j0 + j < p.top ? p.row[t * p.top + j0 + j] : -1;
+            if (r[j] >= p.R) r[j] = -1;
+            w[j] = r[j] >= 0 ? p.P[t * p.top + j0 + j] : 0.f;
+            dot[j] = 0.f;
+        }
+        for (int c = lane * 8; c < p.D; c += kColumns) {
+            const int valid = p.D - c;
+            float d[8];
+            load8(static_cast<const G *>(p.DOUT) + t * p.lddo + c, valid, d);
+            Raw8<T> v[kAtOnce];
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j)
+                v[j] = raw8(static_cast<const T *>(p.rows) + (r[j] >= 0 ? r[j] : 0) * p.ldrows + c, r[j] >= 0 ? valid : 0);
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) {
+                if (r[j] < 0) continue;
+                float o[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    dot[j] += d[i] * v[j].at(i);
+                    o[i] = w[j] * d[i];
+                }
+                store8(static_cast<T *>(p.DROWS) + r[j] * p.lddr + c, valid, o);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            const float s = lanes_sum<64>(dot[j]);
+            if (lane == 0 && j0 + j < p.top) p.DP[t * p.top + j0 + j] = s;
+        }
+    }
+    // this token's share of the rows that belong to none: zeros
+    for (int j = 0; j < p.top; ++j) {
+        const int64_t i = t * p.top + j;
+        if (i >= p.R || p.token[i] >= 0) continue;
+        const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        for (int c = lane * 8; c < p.D; c += kColumns) store8(static_cast<T *>(p.DROWS) + i * p.lddr + c, p.D - c, zero);
+    }
+}
+
+template <typename T, typename R>
+auto pick(xtc_dtype out_dtype) { return out_dtype == XTC_F32 ? combine_kernel<T, R, float> : combine_kernel<T, R, Bf16>; }
+
+}  // namespace
+
+xtc_status launch_combine(const CombineArgs &a, xtc_dtype dtype, xtc_dtype r_dtype, xtc_dtype out_dtype, hipStream_t s) {
+    const int64_t chunks = (a.D + kColumns - 1) / kColumns, groups = (a.T * chunks + kWaves - 1) / kWaves;
+    if (groups >= kMostGroups) return XTC_ERR_TOO_LARGE;
+    const auto kernel = dtype == XTC_F32 ? (r_dtype == XTC_F32 ? pick<float, float>(out_dtype) : pick<float, Bf16>(out_dtype))
+                                         : (r_dtype == XTC_F32 ? pick<Bf16, float>(out_dtype) : pick<Bf16, Bf16>(out_dtype));
+    kernel<<<(unsigned)groups, kWaves * 64, 0, s>>>(a, (int)chunks);
+    return hip_status(hipGetLastError());
+}
+
+xtc_status launch_combine_backward(const CombineBackwardArgs &a, xtc_dtype dtype, xtc_dtype g_dtype, hipStream_t s) {
+    const int64_t groups = (a.T + kWaves - 1) / kWaves;
+    if (groups >= kMostGroups) return XTC_ERR_TOO_LARGE;
+    const auto kernel = dtype == XTC_F32 ? (g_dtype == XTC_F32 ? combine_backward_kernel<float, float> : combine_backward_kernel<float, Bf16>)
+                                         : (g_dtype == XTC_F32 ? combine_backward_kernel<Bf16, float> : combine_backward_kernel<Bf16, Bf16>);
+    kernel<<<(unsigned)groups, kWaves * 64, 0, s>>>(a);
+    return hip_status(hipGetLastError());
+}
+
+}  // namespace xtc

@@ -121,6 +121,64 @@ struct ActivationArgs {
     float *partial;     // activation_slabs() x N sums of a slab of rows each
 };
 
+struct RouteArgs {
+    int64_t T;
+    int E, top;
+    const void *scores;
+    int64_t lds;
+    const uint8_t *mask;    // 0: the token has no experts (null: every token has)
+    int32_t *expert;        // T x top, like p and row
+    float *p;
+    int32_t *row;
+    int32_t *token;         // T * top
+    int32_t *counts, *ends; // E
+    float *loss;
+    int each;               // tokens of a workgroup
+    int32_t *counts_of;     // of each workgroup: E counts, E sums
+    float *sums_of;
+};
+
+struct RouteBackwardArgs {
+    int64_t T;
+    int E, top;
+    const float *DP;        // null: zeros
+    const void *scores;
+    int64_t lds;
+    const int32_t *expert;
+    const float *p;
+    const int32_t *counts;
+    float dloss;
+    void *DS;
+    int64_t ldds;
+};
+
+struct CombineArgs {
+    int64_t T, R;           // tokens; rows that there are
+    int top, D;
+    const void *rows;
+    int64_t ldrows;
+    const int32_t *row;     // T x top, like P
+    const float *P;         // null: ones
+    const void *RES;        // null: nothing added
+    int64_t ldr;
+    void *out;
+    int64_t ldo;
+};
+
+struct CombineBackwardArgs {
+    int64_t T, R;
+    int top, D;
+    const void *DOUT;
+    int64_t lddo;
+    const void *rows;
+    int64_t ldrows;
+    const int32_t *row, *token;
+    const float *P;
+    void *DROWS;
+    int64_t lddr;
+    float *DP;
+};
+
 // Workgroups of a launch: fewer than 2^32 threads of 256 a workgroup.
 constexpr int64_t kMostGroups = int64_t(1) << 24;
 
@@ -149,6 +207,12 @@ int64_t linear_wgrad_workspace(const LinearArgs &a);
 xtc_status launch_linear_wgrad(const LinearArgs &a, hipStream_t s);
 int activation_slabs(int64_t T, int64_t N);
 xtc_status launch_activation_backward(const ActivationArgs &a, hipStream_t s);
+
+int64_t route_workspace(int64_t T, int64_t E);
+xtc_status launch_route(const RouteArgs &a, xtc_dtype dtype, void *workspace, hipStream_t s);
+xtc_status launch_route_backward(const RouteBackwardArgs &a, xtc_dtype dtype, xtc_dtype out_dtype, hipStream_t s);
+xtc_status launch_combine(const CombineArgs &a, xtc_dtype dtype, xtc_dtype r_dtype, xtc_dtype out_dtype, hipStream_t s);
+xtc_status launch_combine_backward(const CombineBackwardArgs &a, xtc_dtype dtype, xtc_dtype g_dtype, hipStream_t s);
 
 // Which of the kernels for aligned rows a product takes (-1: the one for rows at
 // any address), and how many there are.  kind: 0 e4m3, 1 bf16 with B [K, N], 2 with

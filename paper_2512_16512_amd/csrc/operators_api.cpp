@@ -15,6 +15,8 @@ int64_t size_of(xtc_dtype t) { return t == XTC_F32 ? 4 : t == XTC_BF16 ? 2 : 1; 
 int64_t least(int64_t extent) { return extent > 1 ? extent : 1; }
 int64_t scale_blocks(int64_t k) { return k / kScaleBlock + (k % kScaleBlock != 0); }
 
+constexpr int64_t kMostExperts = 1024, kMostChosen = 16;   // (a lane a choice, 16 scores a lane)
+
 // Row strides are at most 2^30 elements, matrices of a family 2^50 apart: offsets stay in 64 bits.
 constexpr int64_t kMostStride = int64_t(1) << 30;
 
@@ -351,6 +353,105 @@ xtc_status xtc_activation_backward(int64_t T, int64_t N, const void *DY, int64_t
     a.DZ = DZ; a.lddz = lddz;
     a.DB = DB; a.partial = static_cast<float *>(workspace);
     return launch_activation_backward(a, static_cast<hipStream_t>(stream));
+}
+
+// T tokens that choose `top` of E experts: rows are counted in 32 bits.
+static xtc_status check_routing(int64_t T, int64_t E, int64_t top) {
+    if (T < 0 || E < 1 || top < 1 || top > E) return XTC_ERR_BAD_SHAPE;
+    if (E > kMostExperts || top > kMostChosen || T > kMostExtent / top) return XTC_ERR_TOO_LARGE;
+    return XTC_OK;
+}
+
+int64_t xtc_route_experts_workspace(int64_t T, int64_t E) {
+    if (T < 0 || E < 1 || T > kMostExtent || E > kMostExperts) return -1;
+    return route_workspace(T, E);
+}
+
+xtc_status xtc_route_experts(int64_t T, int64_t E, int64_t top, const void *scores, int64_t lds, const uint8_t *mask,
+                             int32_t *expert, float *p, int32_t *row, int32_t *token, int32_t *counts, int32_t *ends,
+                             float *loss, void *workspace, int64_t workspace_bytes, xtc_dtype dtype, void *stream) {
+    if (!known(dtype)) return XTC_ERR_BAD_DTYPE;
+    const xtc_status st = check_routing(T, E, top);
+    if (st != XTC_OK) return st;
+    if (lds > kMostStride) return XTC_ERR_TOO_LARGE;
+    if (lds < E) return XTC_ERR_BAD_LEADING_DIM;
+    if (!counts || !ends || !loss || !workspace || (T > 0 && (!scores || !expert || !p || !row || !token)))
+        return XTC_ERR_NULL_POINTER;
+    if (!aligned_to(scores, size_of(dtype)) || !aligned_to(expert, 4) || !aligned_to(p, 4) || !aligned_to(row, 4) ||
+        !aligned_to(token, 4) || !aligned_to(counts, 4) || !aligned_to(ends, 4) || !aligned_to(loss, 4) ||
+        !aligned_to(workspace, 16))
+        return XTC_ERR_MISALIGNED;
+    if (workspace_bytes < xtc_route_experts_workspace(T, E)) return XTC_ERR_BAD_SHAPE;
+    RouteArgs a = {};
+    a.T = T; a.E = (int)E; a.top = (int)top;
+    a.scores = scores; a.lds = lds; a.mask = mask;
+    a.expert = expert; a.p = p; a.row = row; a.token = token;
+    a.counts = counts; a.ends = ends; a.loss = loss;
+    return launch_route(a, dtype, workspace, static_cast<hipStream_t>(stream));
+}
+
+xtc_status xtc_route_experts_backward(int64_t T, int64_t E, int64_t top, const float *DP, const void *scores, int64_t lds,
+                                      const int32_t *expert, const float *p, const int32_t *counts, float dloss,
+                                      void *DS, int64_t ldds, xtc_dtype dtype, xtc_dtype out_dtype, void *stream) {
+    if (!known(dtype) || !known(out_dtype)) return XTC_ERR_BAD_DTYPE;
+    const xtc_status st = check_routing(T, E, top);
+    if (st != XTC_OK) return st;
+    if (lds > kMostStride || ldds > kMostStride) return XTC_ERR_TOO_LARGE;
+    if (lds < E || ldds < E) return XTC_ERR_BAD_LEADING_DIM;
+    if (!aligned_to(DP, 4) || !aligned_to(scores, size_of(dtype)) || !aligned_to(expert, 4) || !aligned_to(p, 4) ||
+        !aligned_to(counts, 4) || !aligned_to(DS, size_of(out_dtype)))
+        return XTC_ERR_MISALIGNED;
+    if (T == 0) return XTC_OK;
+    if (!scores || !expert || !p || !counts || !DS) return XTC_ERR_NULL_POINTER;
+    RouteBackwardArgs a = {};
+    a.T = T; a.E = (int)E; a.top = (int)top;
+    a.DP = DP; a.scores = scores; a.lds = lds;
+    a.expert = expert; a.p = p; a.counts = counts; a.dloss = dloss;
+    a.DS = DS; a.ldds = ldds;
+    return launch_route_backward(a, dtype, out_dtype, static_cast<hipStream_t>(stream));
+}
+
+xtc_status xtc_combine_experts(int64_t T, int64_t top, int64_t D, int64_t R, const void *rows, int64_t ldrows,
+                               const int32_t *row, const float *p, const void *RES, int64_t ldr, xtc_dtype r_dtype,
+                               void *C, int64_t ldc, xtc_dtype dtype, xtc_dtype out_dtype, void *stream) {
+    if (!known(dtype) || !known(out_dtype) || (RES && !known(r_dtype))) return XTC_ERR_BAD_DTYPE;
+    if (T < 0 || top < 0 || D < 0 || R < 0) return XTC_ERR_BAD_SHAPE;
+    if (top > kMostExtent || T > kMostExtent / (top > 1 ? top : 1) || D > kMostExtent || R > kMostExtent || ldrows > kMostStride ||
+        (RES && ldr > kMostStride) || ldc > kMostStride)
+        return XTC_ERR_TOO_LARGE;
+    if ((R > 0 && ldrows < least(D)) || (RES && ldr < least(D)) || ldc < least(D)) return XTC_ERR_BAD_LEADING_DIM;
+    if (!aligned_to(rows, size_of(dtype)) || !aligned_to(row, 4) || !aligned_to(p, 4) || !aligned_to(RES, size_of(r_dtype)) ||
+        !aligned_to(C, size_of(out_dtype)))
+        return XTC_ERR_MISALIGNED;
+    if (T == 0 || D == 0) return XTC_OK;
+    if (!C || (top > 0 && (!row || (R > 0 && !rows)))) return XTC_ERR_NULL_POINTER;
+    CombineArgs a = {};
+    a.T = T; a.R = R; a.top = (int)top; a.D = (int)D;
+    a.rows = rows; a.ldrows = ldrows; a.row = row; a.P = p;
+    a.RES = RES; a.ldr = ldr; a.out = C; a.ldo = ldc;
+    return launch_combine(a, dtype, RES ? r_dtype : XTC_F32, out_dtype, static_cast<hipStream_t>(stream));
+}
+
+xtc_status xtc_combine_experts_backward(int64_t T, int64_t top, int64_t D, const void *DOUT, int64_t lddo,
+                                        xtc_dtype dout_dtype, const void *rows, int64_t ldrows, const int32_t *row,
+                                        const int32_t *token, const float *p, void *DROWS, int64_t lddr, float *DP,
+                                        xtc_dtype dtype, void *stream) {
+    if (!known(dtype) || !known(dout_dtype)) return XTC_ERR_BAD_DTYPE;
+    if (T < 0 || top < 1 || D < 0) return XTC_ERR_BAD_SHAPE;
+    if (top > kMostExtent || T > kMostExtent / top || D > kMostExtent || lddo > kMostStride || ldrows > kMostStride || lddr > kMostStride)
+        return XTC_ERR_TOO_LARGE;
+    if (lddo < least(D) || ldrows < least(D) || lddr < least(D)) return XTC_ERR_BAD_LEADING_DIM;
+    if (!aligned_to(DOUT, size_of(dout_dtype)) || !aligned_to(rows, size_of(dtype)) || !aligned_to(row, 4) ||
+        !aligned_to(token, 4) || !aligned_to(p, 4) || !aligned_to(DROWS, size_of(dtype)) || !aligned_to(DP, 4))
+        return XTC_ERR_MISALIGNED;
+    if (T == 0) return XTC_OK;
+    if (!row || !token || !p || !DP || (D > 0 && (!DOUT || !rows || !DROWS))) return XTC_ERR_NULL_POINTER;
+    CombineBackwardArgs a = {};
+    a.T = T; a.R = T * top; a.top = (int)top; a.D = (int)D;
+    a.DOUT = DOUT; a.lddo = lddo; a.rows = rows; a.ldrows = ldrows;
+    a.row = row; a.token = token; a.P = p;
+    a.DROWS = DROWS; a.lddr = lddr; a.DP = DP;
+    return launch_combine_backward(a, dtype, dout_dtype, static_cast<hipStream_t>(stream));
 }
 
 // Not part of the ABI: the kernel of a product of contiguous, 16-byte aligned

@@ -1,0 +1,399 @@
+// A mixture's router: each token's best experts and their weights, the rows of the grouped products
+// sorted by expert, the counts and the balance loss, and the gradient of the scores.
+//
+//   chosen  the `top` largest scores, the highest first, of equal ones the lowest index first (a NaN
+//           is above every number)
+//   p       softmax over the chosen,  q  softmax over all E
+//   loss    E / (top n^2) sum_e c_e S_e,  c_e the rows of expert e, S_e = sum_t q_te, n tokens
+//   ds      at the chosen p_j (dp_j - sum_i p_i dp_i), everywhere dloss E / (top n^2) q_e (c_e - sum_i c_i q_i)
+//
+// LANES lanes share a token, VPT neighbouring scores each, in registers; its maximum, sums and the next
+// best expert pass among them by lane rotations.  Lane j keeps the choice j.
+//
+// The order of the rows (by expert, then by token) has no atomics in it that could change it: of 64
+// tokens each expert has a word of 64 bits, one a token, so that a row's place among them is a count of
+// bits; the workgroups' counts go to memory, and a second kernel adds up those before its own.
+#include <type_traits>
+
+#include "activation.h"
+#include "operators.h"
+#include "values.h"
+
+namespace xtc {
+namespace {
+
+constexpr int kThreads = 256, kPlaceThreads = 1024, kGroup = 64;   // tokens whose bits fill a word
+
+// The value of the lane N places on, around the 16 (N 8, 4, 2, 1) or 64 (N 16, 32) that share a token.
+template <int N>
+__device__ __forceinline__ unsigned rotated(unsigned v) {
+    if constexpr (N < 16) return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x120 + N, 0xF, 0xF, false);
+    else return (unsigned)__shfl_xor((int)v, N, 64);
+}
+// f over the lanes, in all of them alike: each step joins halves that hold the same values.
+template <int LANES, typename V, typename F>
+__device__ __forceinline__ V over_lanes(V v, F &&f) {
+    static_assert(sizeof(V) == 4, "a register");
+    auto step = [&](unsigned u) { return f(v, __builtin_bit_cast(V, u)); };
+    v = step(rotated<8>(__builtin_bit_cast(unsigned, v)));
+    v = step(rotated<4>(__builtin_bit_cast(unsigned, v)));
+    v = step(rotated<2>(__builtin_bit_cast(unsigned, v)));
+    v = step(rotated<1>(__builtin_bit_cast(unsigned, v)));
+    if constexpr (LANES == 64) {
+        v = step(rotated<16>(__builtin_bit_cast(unsigned, v)));
+        v = step(rotated<32>(__builtin_bit_cast(unsigned, v)));
+    }
+    return v;
+}
+template <int LANES>
+__device__ __forceinline__ float team_sum(float v) {
+    return over_lanes<LANES>(v, [](float a, float b) { return a + b; });
+}
+
+// Scores as whole numbers in their order: NaN highest, -0 and 0 the same; 0 stands below all.
+__device__ __forceinline__ unsigned key_of(float v) {
+    const unsigned u = __float_as_uint(v + 0.f);
+    return v != v ? ~0u : u >> 31 ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float score_of(unsigned key) {
+    return __uint_as_float(key >> 31 ? key & 0x7FFFFFFFu : ~key);
+}
+
+// VPT scores of a row from e on; -inf past the end.
+template <int VPT, typename T>
+__device__ __forceinline__ void load_scores(const T *row, int e, int E, float (&v)[VPT]) {
+    if (e + VPT <= E) {
+        T t[VPT];
+        __builtin_memcpy(t, row + e, sizeof(t));
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) v[i] = widen(t[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) v[i] = e + i < E ? widen(row[e + i]) : -__builtin_inff();
+    }
+}
+
+// Softmax of a team's scores whose largest is `most`; zeros where that is -inf.
+template <int LANES, int VPT>
+__device__ __forceinline__ void softmax(const float (&v)[VPT], float most, float (&q)[VPT]) {
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+        q[i] = exp_of(v[i] - most);
+        sum += q[i];
+    }
+    const float inv = 1.f / team_sum<LANES>(sum);
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) q[i] = most == -__builtin_inff() ? 0.f : q[i] * inv;
+}
+
+// Tokens t0 .. t0 + p.each - 1: their experts and weights, their rows' places among the workgroup's
+// (into p.row), its counts (E, one after the other) and sums of q.
+template <typename T, int LANES, int VPT>
+__device__ __forceinline__ void choose(const RouteArgs &p, int block, unsigned char *smem) {
+    constexpr int TEAMS = kThreads / LANES, EACH = kGroup / TEAMS;
+    const int E = p.E, top = p.top, tid = threadIdx.x, team = tid / LANES, lane = tid % LANES, e0 = lane * VPT;
+    unsigned long long *bits = reinterpret_cast<unsigned long long *>(smem);
+    int *before = reinterpret_cast<int *>(bits + E);
+    float *sums = reinterpret_cast<float *>(before + E);                    // TEAMS x E
+    for (int e = tid; e < E; e += kThreads) before[e] = 0;
+    float total[VPT];
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) total[i] = 0.f;
+    const int64_t first = (int64_t)block * p.each, end = first + p.each < p.T ? first + p.each : p.T;
+    for (int64_t t0 = first; t0 < end; t0 += kGroup) {
+        for (int e = tid; e < E; e += kThreads) bits[e] = 0;
+        __syncthreads();
+        int mine[EACH];              // lane j: the expert of choice j (-1: none)
+#pragma unroll
+        for (int r = 0; r < EACH; ++r) {
+            const int at = r * TEAMS + team;
+            const int64_t t = t0 + at;
+            const bool there = t < end && (!p.mask || p.mask[t]);
+            mine[r] = -1;
+            if (there) {
+                float v[VPT], q[VPT];
+                load_scores<VPT>(static_cast<const T *>(p.scores) + t * p.lds, e0, E, v);
+                unsigned key[VPT], chosen = 0;
+#pragma unroll
+                for (int i = 0; i < VPT; ++i) key[i] = e0 + i < E ? key_of(v[i]) : 0u;
+                float most = 0.f;
+                for (int j = 0; j < top; ++j) {
+                    unsigned best = key[0];
+#pragma unroll
+                    for (int i = 1; i < VPT; ++i) best = key[i] > best ? key[i] : best;
+                    best = over_lanes<LANES>(best, [](unsigned a, unsigned b) { return a > b ? a : b; });
+                    int e = 0x7FFFFFFF;
+#pragma unroll
+                    for (int i = VPT - 1; i >= 0; --i) e = key[i] == best ? e0 + i : e;
+                    e = over_lanes<LANES>(e, [](int a, int b) { return a < b ? a : b; });
+#pragma unroll
+                    for (int i = 0; i < VPT; ++i) key[i] = e0 + i == e ? 0u : key[i];
+                    if (lane == j) {
+                        mine[r] = e;
+                        chosen = best;
+                    }
+                    if (j == 0) most = score_of(best);
+                }
+                const float w = lane < top ? exp_of(score_of(chosen) - most) : 0.f;
+                const float sum = team_sum<LANES>(w);
+                if (lane < top) {
+                    p.expert[t * top + lane] = mine[r];
+                    p.p[t * top + lane] = most == -__builtin_inff() ? 0.f : w / sum;
+                    atomicOr(&bits[mine[r]], 1ull << at);      // (whichever comes first)
+                }
+                softmax<LANES>(v, most, q);
+#pragma unroll
+                for (int i = 0; i < VPT; ++i) total[i] += q[i];
+            } else if (t < end && lane < top) {
+                p.expert[t * top + lane] = -1;
+                p.p[t * top + lane] = 0.f;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < EACH; ++r) {
+            const int at = r * TEAMS + team;
+            const int64_t t = t0 + at;
+            if (t < end && lane < top)
+                p.row[t * top + lane] = mine[r] < 0 ? -1 : before[mine[r]] + __popcll(bits[mine[r]] & ((1ull << at) - 1));
+        }
+        __syncthreads();
+        for (int e = tid; e < E; e += kThreads) before[e] += __popcll(bits[e]);
+    }
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+        if (e0 + i < E) sums[team * E + e0 + i] = total[i];
+    __syncthreads();
+    for (int e = tid; e < E; e += kThreads) {
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < TEAMS; ++i) s += sums[i * E + e];
+        p.counts_of[(int64_t)block * E + e] = before[e];
+        p.sums_of[(int64_t)block * E + e] = s;
+    }
+}
+
+// The places of a workgroup's rows: those of all lower experts, of this expert in the workgroups before,
+// and the place among its own.  Workgroup 0 also writes what there is once.
+template <int THREADS>
+__device__ __forceinline__ void place(const RouteArgs &p, int block, int blocks, unsigned char *smem) {
+    const int E = p.E, top = p.top, tid = threadIdx.x;
+    int *start = reinterpret_cast<int *>(smem);          // of this workgroup's rows of each expert
+    int *all = start + E;                                // rows of each expert, then up to and with it
+    int *part = all + E;                                 // 2 x THREADS
+    float *fpart = reinterpret_cast<float *>(part + 2 * THREADS);     // THREADS
+    // E threads read one workgroup's counts: the threads take the workgroups in turn, THREADS / E at once
+    const int width = E < THREADS ? E : THREADS, turns = THREADS / width;
+    for (int e0 = 0; e0 < E; e0 += width) {
+        const int e = e0 + tid % width, turn = tid / width;
+        int sum = 0, mine = 0;
+        float s = 0.f;
+        if (turn < turns && e < E) {
+#pragma unroll 4
+            for (int b = turn; b < blocks; b += turns) {
+                const int c = p.counts_of[(int64_t)b * E + e];
+                sum += c;
+                mine += b < block ? c : 0;
+                if (block == 0) s += p.sums_of[(int64_t)b * E + e];
+            }
+        }
+        __syncthreads();
+        part[tid] = sum;
+        part[THREADS + tid] = mine;
+        fpart[tid] = s;
+        __syncthreads();
+        if (tid < width && e < E) {
+            for (int i = 1; i < turns; ++i) {
+                sum += part[tid + i * width];
+                mine += part[THREADS + tid + i * width];
+                s += fpart[tid + i * width];
+            }
+            all[e] = sum;
+            start[e] = mine;
+            if (block == 0) {
+                p.counts[e] = sum;
+                p.sums_of[e] = (float)sum * s;           // (this workgroup alone reads it)
+            }
+        }
+    }
+    __syncthreads();
+    // rows up to and with each expert: a wave at a time, 64 experts a step
+    if (tid < 64) {
+        int before = 0;
+        for (int e0 = 0; e0 < E; e0 += 64) {
+            const int e = e0 + tid;
+            int v = e < E ? all[e] : 0;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const int u = __shfl_up(v, d, 64);
+                if (tid >= d) v += u;
+            }
+            v += before;
+            if (e < E) {
+                start[e] += v - all[e];
+                all[e] = v;
+                if (block == 0) p.ends[e] = v;
+            }
+            before = __shfl(v, 63, 64);
+        }
+    }
+    __syncthreads();
+    const int rows = E > 0 ? all[E - 1] : 0;
+    if (block == 0 && tid < 64) {
+        float s = 0.f;
+        for (int e = tid; e < E; e += 64) s += p.sums_of[e];
+        s = lanes_sum<64>(s);
+        const float n = (float)(rows / top > 1 ? rows / top : 1);
+        if (tid == 0) *p.loss = rows > 0 ? (float)E / ((float)top * n) * (s / n) : 0.f;
+    }
+    const int64_t first = (int64_t)block * p.each * top, end = (first + (int64_t)p.each * top < p.T * top ? first + (int64_t)p.each * top : p.T * top);
+    for (int64_t i = first + tid; i < end; i += THREADS) {
+        const int e = p.expert[i];
+        if (e >= 0) {
+            const int at = start[e] + p.row[i];
+            p.row[i] = at;
+            p.token[at] = (int32_t)(i / top);
+        }
+        if (i >= rows) p.token[i] = -1;
+    }
+}
+
+size_t choose_bytes(int E, int lanes) { return (size_t)E * 12 + (size_t)(kThreads / lanes) * E * 4; }
+template <int THREADS>
+size_t place_bytes(int E) { return (size_t)E * 8 + (size_t)THREADS * 12; }
+
+template <typename T, int LANES, int VPT>
+__global__ void __launch_bounds__(kThreads) route_choose_kernel(RouteArgs p) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    choose<T, LANES, VPT>(p, blockIdx.x, smem);
+}
+
+__global__ void __launch_bounds__(kPlaceThreads) route_place_kernel(RouteArgs p, int blocks) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    place<kPlaceThreads>(p, blockIdx.x, blocks, smem);
+}
+
+// The few tokens of one workgroup, in one launch.
+template <typename T, int LANES, int VPT>
+__global__ void __launch_bounds__(kThreads) route_small_kernel(RouteArgs p) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    choose<T, LANES, VPT>(p, 0, smem);
+    __threadfence_block();
+    __syncthreads();
+    place<kThreads>(p, 0, 1, smem);
+}
+
+// ds of the tokens blockIdx.x, + gridDim.x, ... of each team.
+template <typename T, typename O, int LANES, int VPT>
+__global__ void __launch_bounds__(kThreads) route_backward_kernel(RouteBackwardArgs p) {
+    constexpr int TEAMS = kThreads / LANES;
+    const int E = p.E, top = p.top, team = threadIdx.x / LANES, lane = threadIdx.x % LANES, e0 = lane * VPT;
+    float c[VPT], rows = 0.f;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+        c[i] = e0 + i < E ? (float)p.counts[e0 + i] : 0.f;
+        rows += c[i];
+    }
+    float n = team_sum<LANES>(rows) / (float)top;
+    n = n > 1.f ? n : 1.f;
+    const float scale = p.dloss * ((float)E / ((float)top * n)) / n;
+    for (int64_t t = (int64_t)blockIdx.x * TEAMS + team; t < p.T; t += (int64_t)gridDim.x * TEAMS) {
+        const bool has = lane < top;
+        const int e = has ? p.expert[t * top + lane] : -1;
+        const bool there = __shfl(e, 0, LANES) >= 0;
+        float d[VPT];
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) d[i] = 0.f;
+        if (there) {
+            float v[VPT];
+            load_scores<VPT>(static_cast<const T *>(p.scores) + t * p.lds, e0, E, v);
+            const float w = has ? p.p[t * top + lane] : 0.f, dp = has && p.DP ? p.DP[t * top + lane] : 0.f;
+            float most = v[0];
+#pragma unroll
+            for (int i = 1; i < VPT; ++i) most = fmaxf(most, v[i]);
+            most = over_lanes<LANES>(most, [](float a, float b) { return fmaxf(a, b); });
+            softmax<LANES>(v, most, d);
+            float dot = 0.f;
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) dot += c[i] * d[i];
+            dot = team_sum<LANES>(dot);
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) d[i] = scale * d[i] * (c[i] - dot);
+            const float g = w * (dp - team_sum<LANES>(w * dp));
+            for (int j = 0; j < top; ++j) {
+                const int at = __shfl(e, j, LANES) - e0;
+                const float add = __shfl(g, j, LANES);
+#pragma unroll
+                for (int i = 0; i < VPT; ++i) d[i] += at == i ? add : 0.f;
+            }
+        }
+        O *out = static_cast<O *>(p.DS) + t * p.ldds + e0;
+        O o[VPT];
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) narrow(d[i], &o[i]);
+        if (e0 + VPT <= E) {
+            __builtin_memcpy(out, o, sizeof(o));
+        } else {
+#pragma unroll
+            for (int i = 0; i < VPT; ++i)
+                if (e0 + i < E) out[i] = o[i];
+        }
+    }
+}
+
+// f(lanes, scores a lane) for E experts, as constants.
+template <typename F>
+void with_lanes(int E, F &&f) {
+    typedef std::integral_constant<int, 16> Row;
+    if (E <= 16) f(Row(), std::integral_constant<int, 1>());
+    else if (E <= 32) f(Row(), std::integral_constant<int, 2>());
+    else if (E <= 64) f(Row(), std::integral_constant<int, 4>());
+    else if (E <= 128) f(Row(), std::integral_constant<int, 8>());
+    else if (E <= 256) f(Row(), std::integral_constant<int, 16>());
+    else f(std::integral_constant<int, 64>(), std::integral_constant<int, 16>());
+}
+
+constexpr int kMostBlocks = 256;
+// Tokens of a workgroup (whole groups), and the workgroups.
+int64_t each_of(int64_t T) { return ((T + kGroup - 1) / kGroup + kMostBlocks - 1) / kMostBlocks * kGroup; }
+int blocks_of(int64_t T) { return T > 0 ? (int)((T + each_of(T) - 1) / each_of(T)) : 1; }
+
+}  // namespace
+
+int64_t route_workspace(int64_t T, int64_t E) { return (int64_t)blocks_of(T) * E * 8; }
+
+xtc_status launch_route(const RouteArgs &given, xtc_dtype dtype, void *workspace, hipStream_t s) {
+    RouteArgs a = given;
+    const int blocks = blocks_of(a.T);
+    a.each = a.T > 0 ? (int)each_of(a.T) : kGroup;
+    a.counts_of = static_cast<int32_t *>(workspace);
+    a.sums_of = reinterpret_cast<float *>(a.counts_of + (int64_t)blocks * a.E);
+    with_lanes(a.E, [&](auto lanes, auto vpt) {
+        constexpr int LANES = lanes(), VPT = vpt();
+        if (blocks == 1) {
+            const size_t one = choose_bytes(a.E, LANES), two = place_bytes<kThreads>(a.E);
+            const auto kernel = dtype == XTC_F32 ? route_small_kernel<float, LANES, VPT> : route_small_kernel<Bf16, LANES, VPT>;
+            kernel<<<1, kThreads, one > two ? one : two, s>>>(a);
+        } else {
+            const auto kernel = dtype == XTC_F32 ? route_choose_kernel<float, LANES, VPT> : route_choose_kernel<Bf16, LANES, VPT>;
+            kernel<<<(unsigned)blocks, kThreads, choose_bytes(a.E, LANES), s>>>(a);
+            route_place_kernel<<<(unsigned)blocks, kPlaceThreads, place_bytes<kPlaceThreads>(a.E), s>>>(a, blocks);
+        }
+    });
+    return hip_status(hipGetLastError());
+}
+
+xtc_status launch_route_backward(const RouteBackwardArgs &a, xtc_dtype dtype, xtc_dtype out_dtype, hipStream_t s) {
+    with_lanes(a.E, [&](auto lanes, auto vpt) {
+        constexpr int LANES = lanes(), VPT = vpt(), TEAMS = kThreads / LANES;
+        const int64_t groups = (a.T + TEAMS - 1) / TEAMS;
+        const auto kernel =
+            dtype == XTC_F32 ? (out_dtype == XTC_F32 ? route_backward_kernel<float, float, LANES, VPT> : route_backward_kernel<float, Bf16, LANES, VPT>)
+                             : (out_dtype == XTC_F32 ? route_backward_kernel<Bf16, float, LANES, VPT> : route_backward_kernel<Bf16, Bf16, LANES, VPT>);
+        kernel<<<(unsigned)(groups < 2048 ? groups : 2048), kThreads, 0, s>>>(a);
+    });
+    return hip_status(hipGetLastError());
+}
+
+}  // namespace xtc

@@ -608,6 +608,128 @@ PyObject *matmul_grouped_fp8(PyObject *, PyObject *const *args, Py_ssize_t n) {
     }
 }
 
+bool contiguous(const at::Tensor &t, at::ScalarType type, at::IntArrayRef shape, const at::Tensor &like) {
+    return t.scalar_type() == type && t.sizes() == shape && t.is_contiguous() && t.device() == like.device();
+}
+template <typename T>
+T *as(const at::Tensor &t) { return static_cast<T *>(t.data_ptr()); }
+template <typename T>
+T *as(const at::Tensor *t) { return t ? as<T>(*t) : nullptr; }
+
+// route_experts(scores, top, mask or None): (expert, p, row, token, counts, ends, loss)
+PyObject *route_experts(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    const at::Tensor *s, *mask = nullptr;
+    xtc_dtype dt;
+    long top;
+    if (n != 3 || modes_active() || !plain(args[0], &s) || !small_int(args[1], &top) ||
+        (args[2] != Py_None && !plain(args[2], &mask)) || !row_major(*s) || !dtype_code(*s, &dt))
+        Py_RETURN_NONE;
+    const int64_t T = s->size(0), E = s->size(1);
+    if (top < 1 || top > E || (mask && !contiguous(*mask, at::kBool, {T}, *s))) Py_RETURN_NONE;
+    try {
+        const c10::DeviceGuard on(s->device());
+        const int64_t size = xtc_route_experts_workspace(T, E);
+        if (size < 0) Py_RETURN_NONE;
+        at::Tensor r[7] = {fresh({T, top}, at::kInt, *s), fresh({T, top}, at::kFloat, *s), fresh({T, top}, at::kInt, *s),
+                           fresh({T * top}, at::kInt, *s), fresh({E}, at::kInt, *s), fresh({E}, at::kInt, *s),
+                           fresh({}, at::kFloat, *s)};
+        at::Tensor work = fresh({size}, at::kByte, *s);
+        void *stream = stream_of(*s);
+        if (unlocked(xtc_route_experts, T, E, (int64_t)top, static_cast<const void *>(s->data_ptr()), row_stride(*s),
+                     static_cast<const uint8_t *>(data(mask)), as<int32_t>(r[0]), as<float>(r[1]), as<int32_t>(r[2]),
+                     as<int32_t>(r[3]), as<int32_t>(r[4]), as<int32_t>(r[5]), as<float>(r[6]), work.data_ptr(), size, dt,
+                     stream) != XTC_OK)
+            Py_RETURN_NONE;
+        return tuple_of(r);
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+}
+
+// route_experts_backward(dp or None, scores, expert, p, counts, dloss, dtype or None): dscores
+PyObject *route_experts_backward(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    const at::Tensor *t[5];
+    xtc_dtype dt;
+    if (n != 7 || modes_active() || !tensors(args, t, 1) || !PyFloat_CheckExact(args[5])) Py_RETURN_NONE;
+    const at::Tensor &s = *t[1], &e = *t[2], &p = *t[3], &counts = *t[4];
+    if (!row_major(s) || !dtype_code(s, &dt) || e.dim() != 2) Py_RETURN_NONE;
+    const int64_t T = s.size(0), E = s.size(1), top = e.size(1);
+    if (!contiguous(e, at::kInt, {T, top}, s) || !contiguous(p, at::kFloat, {T, top}, s) ||
+        !contiguous(counts, at::kInt, {E}, s) || (t[0] && !contiguous(*t[0], at::kFloat, {T, top}, s)))
+        Py_RETURN_NONE;
+    xtc_dtype code = dt;
+    if (args[6] != Py_None) {
+        if (!THPDtype_Check(args[6])) Py_RETURN_NONE;
+        const at::ScalarType want = reinterpret_cast<THPDtype *>(args[6])->scalar_type;
+        if (want != at::kFloat && want != at::kBFloat16) Py_RETURN_NONE;
+        code = want == at::kFloat ? XTC_F32 : XTC_BF16;
+    }
+    try {
+        const c10::DeviceGuard on(s.device());
+        at::Tensor ds = fresh({T, E}, code == XTC_F32 ? at::kFloat : at::kBFloat16, s);
+        void *stream = stream_of(s);
+        if (unlocked(xtc_route_experts_backward, T, E, top, as<const float>(t[0]), static_cast<const void *>(s.data_ptr()),
+                     row_stride(s), as<const int32_t>(e), as<const float>(p), as<const int32_t>(counts),
+                     (float)PyFloat_AS_DOUBLE(args[5]), ds.data_ptr(), at_least_1(E), dt, code, stream) != XTC_OK)
+            Py_RETURN_NONE;
+        return wrapped(std::move(ds));
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+}
+
+// combine_experts(rows, row, p or None, residual or None, dtype or None)
+PyObject *combine_experts(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    const at::Tensor *t[4];
+    if (n != 5 || modes_active() || !tensors(args, t, 4 | 8)) Py_RETURN_NONE;
+    const at::Tensor &rows = *t[0], &row = *t[1];
+    if (!row_major(rows) || !either(rows) || row.dim() != 2) Py_RETURN_NONE;
+    const int64_t R = rows.size(0), D = rows.size(1), T = row.size(0), top = row.size(1);
+    if (!contiguous(row, at::kInt, {T, top}, rows) || (t[2] && !contiguous(*t[2], at::kFloat, {T, top}, rows)) ||
+        (t[3] && (!either(*t[3]) || !matrix(*t[3], t[3]->scalar_type(), T, D, rows))))
+        Py_RETURN_NONE;
+    try {
+        const c10::DeviceGuard on(rows.device());
+        at::Tensor out;
+        xtc_dtype code;
+        if (!result(nullptr, args[4], {T, D}, rows, &out, &code)) Py_RETURN_NONE;
+        void *stream = stream_of(rows);
+        if (unlocked(xtc_combine_experts, T, top, D, R, static_cast<const void *>(rows.data_ptr()),
+                     R > 0 ? row_stride(rows) : at_least_1(D), as<const int32_t>(row), as<const float>(t[2]), data(t[3]),
+                     t[3] ? row_stride(*t[3]) : 0, code_of(t[3]), out.data_ptr(), at_least_1(D), code_of(&rows), code,
+                     stream) != XTC_OK)
+            Py_RETURN_NONE;
+        return wrapped(std::move(out));
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+}
+
+// combine_experts_backward(dout, rows, row, token, p): (drows, dp)
+PyObject *combine_experts_backward(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    const at::Tensor *t[5];
+    if (n != 5 || modes_active() || !tensors(args, t)) Py_RETURN_NONE;
+    const at::Tensor &dout = *t[0], &rows = *t[1], &row = *t[2], &token = *t[3], &p = *t[4];
+    if (!row_major(rows) || !either(rows) || !either(dout) || row.dim() != 2) Py_RETURN_NONE;
+    const int64_t R = rows.size(0), D = rows.size(1), T = row.size(0), top = row.size(1);
+    if (R != T * top || !contiguous(row, at::kInt, {T, top}, rows) || !contiguous(token, at::kInt, {R}, rows) ||
+        !contiguous(p, at::kFloat, {T, top}, rows) || !matrix(dout, dout.scalar_type(), T, D, rows))
+        Py_RETURN_NONE;
+    try {
+        const c10::DeviceGuard on(rows.device());
+        at::Tensor drows = fresh({R, D}, rows.scalar_type(), rows), dp = fresh({T, top}, at::kFloat, rows);
+        void *stream = stream_of(rows);
+        if (unlocked(xtc_combine_experts_backward, T, top, D, static_cast<const void *>(dout.data_ptr()), row_stride(dout),
+                     code_of(&dout), static_cast<const void *>(rows.data_ptr()), row_stride(rows), as<const int32_t>(row),
+                     as<const int32_t>(token), as<const float>(p), drows.data_ptr(), at_least_1(D), as<float>(dp),
+                     code_of(&rows), stream) != XTC_OK)
+            Py_RETURN_NONE;
+        return pair(std::move(drows), std::move(dp));
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+}
+
 template <PyObject *(*F)(PyObject *, PyObject *const *, Py_ssize_t)>
 PyCFunction fast() {
     return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(F));
@@ -631,6 +753,12 @@ PyMethodDef kMethods[] = {
     {"matmul_grouped_wgrad", fast<matmul_grouped_wgrad>(), METH_FASTCALL, "matmul_grouped_wgrad(a, dy, ends, out, dtype)"},
     {"matmul_grouped_fp8", fast<matmul_grouped_fp8>(), METH_FASTCALL,
      "matmul_grouped_fp8(a, a_scale, b, b_scale, ends, out, relu, dtype)"},
+    {"route_experts", fast<route_experts>(), METH_FASTCALL, "route_experts(scores, top, mask)"},
+    {"route_experts_backward", fast<route_experts_backward>(), METH_FASTCALL,
+     "route_experts_backward(dp, scores, expert, p, counts, dloss, dtype)"},
+    {"combine_experts", fast<combine_experts>(), METH_FASTCALL, "combine_experts(rows, row, p, residual, dtype)"},
+    {"combine_experts_backward", fast<combine_experts_backward>(), METH_FASTCALL,
+     "combine_experts_backward(dout, rows, row, token, p)"},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};

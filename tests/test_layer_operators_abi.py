@@ -110,6 +110,74 @@ def test_activation_backward_refuses(change, status):
     assert call(x.xtc_activation_backward, SLOPE, **change) == status
 
 
+ROUTE = dict(T=4, E=20, top=3, scores=BAD, lds=20, mask=0, expert=BAD, p=BAD, row=BAD, token=BAD, counts=BAD, ends=BAD,
+             loss=BAD, workspace=BAD, workspace_bytes=1 << 20, dtype=0)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(dtype=2), 4), (dict(T=-1), 2), (dict(E=0), 2), (dict(top=0), 2), (dict(top=21), 2), (dict(top=-1), 2),
+    (dict(workspace_bytes=x.xtc_route_experts_workspace(4, 20) - 1), 2), (dict(lds=19), 3),
+    (dict(E=1025, lds=1025), 7), (dict(E=64, lds=64, top=17), 7), (dict(T=1 << 30), 7), (dict(T=BIG), 7), (dict(lds=BIG), 7),
+    (dict(scores=0), 1), (dict(expert=0), 1), (dict(p=0), 1), (dict(row=0), 1), (dict(token=0), 1), (dict(counts=0), 1),
+    (dict(ends=0), 1), (dict(loss=0), 1), (dict(workspace=0), 1), (dict(scores=BAD + 2), 9), (dict(expert=BAD + 2), 9),
+    (dict(p=BAD + 1), 9), (dict(row=BAD + 2), 9), (dict(token=BAD + 2), 9), (dict(counts=BAD + 2), 9), (dict(ends=BAD + 2), 9),
+    (dict(loss=BAD + 2), 9), (dict(workspace=BAD + 4), 9),
+])
+def test_route_experts_refuses(change, status):
+    assert call(x.xtc_route_experts, ROUTE, **change) == status
+
+
+def test_route_experts_workspace():
+    assert x.xtc_route_experts_workspace(-1, 4) == -1 and x.xtc_route_experts_workspace(4, 0) == -1
+    assert x.xtc_route_experts_workspace(4, 1025) == -1 and x.xtc_route_experts_workspace(BIG, 4) == -1
+    assert x.xtc_route_experts_workspace(0, 20) >= 8 * 20
+
+
+ROUTE_BACK = dict(T=4, E=20, top=3, DP=BAD, scores=BAD, lds=20, expert=BAD, p=BAD, counts=BAD, dloss=0.1, DS=BAD, ldds=20,
+                  dtype=0, out_dtype=1)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(dtype=2), 4), (dict(out_dtype=2), 4), (dict(T=-1), 2), (dict(E=0), 2), (dict(top=0), 2), (dict(top=21), 2),
+    (dict(lds=19), 3), (dict(ldds=19), 3), (dict(E=1025, lds=1025, ldds=1025), 7), (dict(E=64, lds=64, ldds=64, top=17), 7),
+    (dict(T=BIG), 7), (dict(ldds=BIG), 7), (dict(scores=0), 1), (dict(expert=0), 1), (dict(p=0), 1), (dict(counts=0), 1),
+    (dict(DS=0), 1), (dict(DP=BAD + 2), 9), (dict(scores=BAD + 2), 9), (dict(expert=BAD + 1), 9), (dict(DS=BAD + 1), 9),
+    (dict(T=0, scores=0, DS=0), 0),
+])
+def test_route_experts_backward_refuses(change, status):
+    assert call(x.xtc_route_experts_backward, ROUTE_BACK, **change) == status
+
+
+COMBINE = dict(T=4, top=3, D=40, R=12, rows=BAD, ldrows=40, row=BAD, p=BAD, RES=BAD, ldr=40, r_dtype=0, C=BAD, ldc=40,
+               dtype=1, out_dtype=1)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(dtype=2), 4), (dict(out_dtype=2), 4), (dict(r_dtype=2), 4), (dict(T=-1), 2), (dict(top=-1), 2), (dict(D=-1), 2),
+    (dict(R=-1), 2), (dict(ldrows=39), 3), (dict(ldr=39), 3), (dict(ldc=39), 3), (dict(rows=0), 1), (dict(row=0), 1),
+    (dict(C=0), 1), (dict(rows=BAD + 1), 9), (dict(row=BAD + 2), 9), (dict(p=BAD + 2), 9), (dict(RES=BAD + 2), 9),
+    (dict(C=BAD + 1), 9), (dict(T=BIG), 7), (dict(T=1 << 30), 7), (dict(D=BIG, ldrows=BIG), 7), (dict(R=BIG), 7),
+    (dict(ldc=BIG), 7), (dict(T=0, C=0), 0), (dict(D=0, C=0), 0),
+])
+def test_combine_experts_refuses(change, status):
+    assert call(x.xtc_combine_experts, COMBINE, **change) == status
+
+
+COMBINE_BACK = dict(T=4, top=3, D=40, DOUT=BAD, lddo=40, dout_dtype=0, rows=BAD, ldrows=40, row=BAD, token=BAD, p=BAD,
+                    DROWS=BAD, lddr=40, DP=BAD, dtype=1)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(dtype=2), 4), (dict(dout_dtype=2), 4), (dict(T=-1), 2), (dict(top=0), 2), (dict(D=-1), 2), (dict(lddo=39), 3),
+    (dict(ldrows=39), 3), (dict(lddr=39), 3), (dict(DOUT=0), 1), (dict(rows=0), 1), (dict(row=0), 1), (dict(token=0), 1),
+    (dict(p=0), 1), (dict(DROWS=0), 1), (dict(DP=0), 1), (dict(DOUT=BAD + 2), 9), (dict(rows=BAD + 1), 9),
+    (dict(row=BAD + 2), 9), (dict(token=BAD + 2), 9), (dict(p=BAD + 2), 9), (dict(DROWS=BAD + 1), 9), (dict(DP=BAD + 2), 9),
+    (dict(T=BIG), 7), (dict(T=1 << 30), 7), (dict(lddr=BIG), 7), (dict(T=0, DOUT=0), 0),
+])
+def test_combine_experts_backward_refuses(change, status):
+    assert call(x.xtc_combine_experts_backward, COMBINE_BACK, **change) == status
+
+
 # ------------------------------------------------ the conveniences' own checks
 
 
@@ -128,6 +196,12 @@ F32 = torch.float32
     (x.linear_wgrad, (t(4, 8), t(4, 4)), ValueError, "CUDA"),
     (x.activation_backward, (t(4, 8), t(4, 8), "swish"), ValueError, "activation must be"),
     (x.activation_backward, (t(4, 8, dtype=E4M3), t(4, 8), "relu"), TypeError, "dy must be"),
+    (x.route_experts, (t(4, 8, dtype=torch.float16), 2), TypeError, "scores must be"),
+    (x.route_experts, (t(4, 8), 2), ValueError, "CUDA"),
+    (x.route_experts_backward, (None, t(4, 8), t(4, 2), t(4, 2), t(8)), ValueError, "CUDA"),
+    (x.combine_experts, (t(4, 8, dtype=E4M3), t(4, 2)), TypeError, "rows must be"),
+    (x.combine_experts, (t(8, 8), t(4, 2)), ValueError, "CUDA"),
+    (x.combine_experts_backward, (t(4, 8), t(8, 8), t(4, 2), t(8), t(4, 2)), ValueError, "CUDA"),
 ])
 def test_conveniences_refuse(fn, args, error, match):
     with pytest.raises(error, match=match):
@@ -135,9 +209,11 @@ def test_conveniences_refuse(fn, args, error, match):
 
 
 def test_the_native_entries_leave_other_tensors_to_python():
-    a, v = t(4, 8), t(4, dtype=F32)
+    a, v, i = t(4, 8), t(4, dtype=F32), torch.zeros(4, 2, dtype=torch.int32)
     for name, args in (("layernorm", (a, t(8), t(8), None, 1e-6, False)), ("layernorm_backward", (a, a, t(8), v, v, None)),
                        ("linear", (a, t(8, 4), None, None, 0, False, False, None, None)),
-                       ("linear_wgrad", (a, a, None, None)), ("activation_backward", (a, a, 1))):
+                       ("linear_wgrad", (a, a, None, None)), ("activation_backward", (a, a, 1)),
+                       ("route_experts", (a, 2, None)), ("route_experts_backward", (None, a, i, v, i, 0.0, None)),
+                       ("combine_experts", (a, i, None, None, None)), ("combine_experts_backward", (a, a, i, i, v))):
         fast = getattr(x._fast, name)
         assert fast(*args) is None and fast() is None and fast(*([None] * len(args))) is None
