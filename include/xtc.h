@@ -441,13 +441,12 @@ xtc_status xtc_matmul_fp8(int64_t M, int64_t N, int64_t K,
  *  C      device, out_dtype (XTC_F32 or XTC_BF16) T x N, row stride ldc.
  *  Z      device, z in out_dtype for the activation's gradient, row stride ldz, or
  *         NULL.
- *  workspace  device, workspace_bytes >= xtc_linear_workspace(T, N, K, transpose_b)
+ *  workspace  device, workspace_bytes >= xtc_linear_workspace() of the same operands
  *         (0 for many sizes: NULL is fine then), 16-byte aligned, written by the
  *         call; too small is XTC_ERR_BAD_SHAPE.  Calls that may run at the same
  *         time need one each.
  * T or N 0 is a no-op; K 0 gives act(bias) + R.  The order of a sum depends on T, N,
- * K, transpose_b and on whether the rows are 16-byte aligned.  Errors as for
- * xtc_rmsnorm.
+ * K, transpose_b and on which rows are 16-byte aligned.  Errors as for xtc_rmsnorm.
  */
 xtc_status xtc_linear(int64_t T, int64_t N, int64_t K, const void *A, int64_t lda,
                       const void *B, int64_t ldb, int32_t transpose_b,
@@ -457,22 +456,25 @@ xtc_status xtc_linear(int64_t T, int64_t N, int64_t K, const void *A, int64_t ld
                       void *workspace, int64_t workspace_bytes,
                       xtc_dtype dtype, xtc_dtype out_dtype, void *stream);
 
-/* Bytes of workspace; -1 for extents outside the limits.  Pure host function. */
-int64_t xtc_linear_workspace(int64_t T, int64_t N, int64_t K, int32_t transpose_b);
+/* Bytes of workspace; -1 for extents outside the limits.  Pure host function: of the
+ * pointers and strides it takes the alignment (rows off 16 bytes may be copied first). */
+int64_t xtc_linear_workspace(int64_t T, int64_t N, int64_t K, const void *A, int64_t lda,
+                             const void *B, int64_t ldb, int32_t transpose_b);
 
 /*
  * xtc_linear_wgrad -- the gradient of a linear layer's B: DB = A^T * DY (zeros when
  * T == 0), K x N of out_dtype (XTC_F32 or XTC_BF16), row stride lddb.  A is T x K, DY
  * (z's gradient) T x N, both bf16.  Of a B that is N x K it is the same call with A
- * and DY exchanged.  workspace: xtc_linear_wgrad_workspace(T, N, K) bytes, as above.
+ * and DY exchanged.  workspace: xtc_linear_wgrad_workspace() bytes, as above.
  */
 xtc_status xtc_linear_wgrad(int64_t T, int64_t N, int64_t K, const void *A, int64_t lda,
                             const void *DY, int64_t lddy, void *DB, int64_t lddb,
                             void *workspace, int64_t workspace_bytes,
                             xtc_dtype dtype, xtc_dtype out_dtype, void *stream);
 
-/* Bytes of workspace; -1 for extents outside the limits.  Pure host function. */
-int64_t xtc_linear_wgrad_workspace(int64_t T, int64_t N, int64_t K);
+/* Bytes of workspace, as above. */
+int64_t xtc_linear_wgrad_workspace(int64_t T, int64_t N, int64_t K, const void *A, int64_t lda,
+                                   const void *DY, int64_t lddy);
 
 /*
  * xtc_activation_backward -- the gradients of a linear layer's z and bias:

@@ -133,11 +133,11 @@ def _load():
     lib.xtc_linear.argtypes = [i64] * 3 + [vp, i64, vp, i64, i32, vp, i32, vp, i64, i32, i32, vp, i64, vp, i64, vp, i64,
                                            i32, i32, vp]
     lib.xtc_linear.restype = i32
-    lib.xtc_linear_workspace.argtypes = [i64] * 3 + [i32]
+    lib.xtc_linear_workspace.argtypes = [i64] * 3 + [vp, i64, vp, i64, i32]
     lib.xtc_linear_workspace.restype = i64
     lib.xtc_linear_wgrad.argtypes = [i64] * 3 + [vp, i64, vp, i64, vp, i64, vp, i64, i32, i32, vp]
     lib.xtc_linear_wgrad.restype = i32
-    lib.xtc_linear_wgrad_workspace.argtypes = [i64] * 3
+    lib.xtc_linear_wgrad_workspace.argtypes = [i64] * 3 + [vp, i64, vp, i64]
     lib.xtc_linear_wgrad_workspace.restype = i64
     lib.xtc_activation_backward.argtypes = [i64] * 2 + [vp, i64, i32, vp, i64, i32, i32, vp, i64, vp, vp, i64, vp]
     lib.xtc_activation_backward.restype = i32
@@ -284,8 +284,8 @@ def xtc_linear(T, N, K, A, lda, B, ldb, transpose_b, bias, bias_dtype, R, ldr, r
                            Z, ldz, workspace, workspace_bytes, dtype, out_dtype, stream)
 
 
-def xtc_linear_workspace(T, N, K, transpose_b) -> int:
-    return _lib.xtc_linear_workspace(T, N, K, transpose_b)
+def xtc_linear_workspace(T, N, K, A, lda, B, ldb, transpose_b) -> int:
+    return _lib.xtc_linear_workspace(T, N, K, A, lda, B, ldb, transpose_b)
 
 
 def xtc_linear_wgrad(T, N, K, A, lda, DY, lddy, DB, lddb, workspace, workspace_bytes, dtype, out_dtype, stream=0) -> int:
@@ -293,8 +293,8 @@ def xtc_linear_wgrad(T, N, K, A, lda, DY, lddy, DB, lddb, workspace, workspace_b
                                  stream)
 
 
-def xtc_linear_wgrad_workspace(T, N, K) -> int:
-    return _lib.xtc_linear_wgrad_workspace(T, N, K)
+def xtc_linear_wgrad_workspace(T, N, K, A, lda, DY, lddy) -> int:
+    return _lib.xtc_linear_wgrad_workspace(T, N, K, A, lda, DY, lddy)
 
 
 def xtc_activation_backward(T, N, DY, lddy, dy_dtype, Z, ldz, z_dtype, activation, DZ, lddz, DB, workspace,
@@ -777,7 +777,7 @@ def linear(a, b, bias=None, residual=None, activation=None, transpose_b=False, k
         _matrix(residual, "residual", either, (T, N), a.device)
     out, code = _result(torch, (T, N), out, dtype, a.device)
     z = torch.empty((T, N), dtype=out.dtype, device=a.device) if keep else None
-    size = xtc_linear_workspace(T, N, K, int(transpose_b))
+    size = xtc_linear_workspace(T, N, K, a.data_ptr(), _ld(a), b.data_ptr(), _ld(b), int(transpose_b))
     work = torch.empty(max(size, 0), dtype=torch.uint8, device=a.device)
     with _on(torch, a.device):
         _check(xtc_linear(T, N, K, a.data_ptr(), _ld(a), b.data_ptr(), _ld(b), int(transpose_b), _ptr(bias),
@@ -805,7 +805,7 @@ def linear_wgrad(a, dy, out=None, dtype=None):
     if dy.shape[0] != T:
         raise ValueError("a and dy have %d and %d rows" % (T, dy.shape[0]))
     out, code = _result(torch, (K, N), out, dtype, a.device)
-    size = xtc_linear_wgrad_workspace(T, N, K)
+    size = xtc_linear_wgrad_workspace(T, N, K, a.data_ptr(), _ld(a), dy.data_ptr(), _ld(dy))
     work = torch.empty(max(size, 0), dtype=torch.uint8, device=a.device)
     with _on(torch, a.device):
         _check(xtc_linear_wgrad(T, N, K, a.data_ptr(), _ld(a), dy.data_ptr(), _ld(dy), out.data_ptr(), _ld(out),

@@ -115,7 +115,7 @@ struct Source {
         const int bk = KB / elt, ks = left < bk ? left : bk;
         int bytes = 0;
         // (whole chunks: one that holds any value of a row is mapped)
-        if (left > 0) bytes = K_ROWS ? (ks - 1) * (int)ld + ((rows * 2 + 15) & ~15) : (rows - 1) * (int)ld + ks * elt;
+        if (left > 0) bytes = K_ROWS ? (ks - 1) * (int)ld + ((rows * 2 + 15) & ~15) : (rows - 1) * (int)ld + ((ks * elt + 15) & ~15);
         const i32x4 r = make_rsrc(base, bytes);
         base += stages * (K_ROWS ? bk * ld : KB);
         return r;

@@ -163,14 +163,24 @@ __device__ __forceinline__ void finish_at(const LinearArgs &p, int row, int n, f
     e.write(0, v, e.residual(0, true));
 }
 
-// The kernels of one file each for bf16 layers; launch_linear_any takes every call, the
-// others those with aligned rows.
+// A compiled kernel and what a launch of it takes, in microseconds: with n tiles on 256 CUs
+// of per_cu workgroups each, every round costs `fixed` (the launch, the first data's way and the
+// results') and for each stage of k (128 bytes) `one` where each CU holds one workgroup, `full`
+// where it holds per_cu; a round that leaves CUs empty has fill * one for a stage at the least.
+struct LinearChoice {
+    int bm, bn, per_cu;
+    float one, full, fixed, fill;
+    xtc_status (*launch)(const GroupedArgs &, hipStream_t);
+};
+
+// The kernels of one file each for bf16 layers; those of linear_any_choices take every call, the
+// others such with aligned rows.
 template <Kind KIND>
-xtc_status launch_linear_any(const LinearArgs &a, hipStream_t s);
+const LinearChoice *linear_any_choices(int *count);
 template <Kind KIND>
-const Choice *linear_tile_choices(int *count);
+const LinearChoice *linear_tile_choices(int *count);
 template <Kind KIND>
-const Choice *linear_stream_choices(int *count);
+const LinearChoice *linear_stream_choices(int *count);
 
 inline int64_t linear_tiles(const LinearArgs &a, Kind kind, int bm, int bn) {
     return cdiv(kind == kWgrad ? a.K : a.T, bm) * cdiv(a.N, bn) * a.splits;

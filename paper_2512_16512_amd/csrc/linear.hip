@@ -7,72 +7,118 @@ namespace {
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-// As for the grouped products: 16-byte aligned rows, whole 16-byte chunks of k where they
-// run along it, strides that keep the offsets within a tile in 31 bits.
-template <Kind KIND>
-bool aligned_rows(const LinearArgs &a) {
-    const int64_t most = (int64_t(1) << 31) / 257;
-    if (!aligned16(a.A) || !aligned16(a.B) || a.lda * 2 % 16 || a.ldb * 2 % 16) return false;
-    if (KIND != kWgrad && a.K * 2 % 16) return false;
-    return a.lda * 2 < most && a.ldb * 2 < most;
-}
+// 16-byte aligned rows, with a stride that keeps the offsets within a tile in 31 bits.
+bool aligned_rows(const void *p, int64_t ld) { return aligned16(p) && ld % 8 == 0 && ld * 2 < (int64_t(1) << 31) / 257; }
 
-// A kernel and the parts of the reduction it is launched with.
+// A kernel, the parts of the reduction it is launched with, and the operands that are first copied
+// to rows that it can take.
 struct Plan {
-    const Choice *choice;     // null: the kernel for rows at any address
-    int splits, k_each;
-    int place;
+    const LinearChoice *choice;
+    int splits, k_each, place;
+    bool copy_a, copy_b;
+    int64_t ld_a, ld_b;                          // of the copies
+    int64_t part_bytes, a_bytes, b_bytes;        // of the workspace, one after the other
 };
 
 constexpr int kSplitStep = 128;      // parts of the reduction are whole stages of every kernel
+constexpr int kMostSplits = 16;
+constexpr double kJoinUs = 2.4, kJoinPartUs = .15;
 
-// Microseconds of a launch over `splits` parts: rounds of tiles on 256 CUs as for the
-// grouped products, and the way of the parts' sums to memory and back.
-double estimate_us(const Choice &c, int64_t rows, int64_t cols, int64_t reduce, int64_t weights, int splits, int64_t k_each) {
-    const double stages = (double)cdiv(k_each < reduce ? k_each : reduce, 64), slots = 256. * c.per_cu;
-    const int64_t n = cdiv(rows, c.bm) * cdiv(cols, c.bn) * splits, whole = (int64_t)(n / slots);
-    const double rest = n - whole * slots;
-    const int64_t held = cdiv((int64_t)rest, 256);
-    const bool from_memory = weights * 2 > 64e6;
-    const double one = from_memory ? c.cold : c.one, full = c.per_cu > 1 ? c.full : one;
-    double us = whole * (stages * full + c.fixed);
-    if (held > 0) {
-        const double last = stages * (held > 1 ? one + (full - one) * (held - 1) / (c.per_cu - 1) : one) + c.fixed;
-        us += whole > 0 && c.per_cu > 1 ? last / 2 : last;
+int64_t padded(int64_t n) { return cdiv(n, 8) * 8; }
+int64_t room(int64_t bytes) { return cdiv(bytes, 256) * 256; }
+
+// Microseconds of a launch over `splits` parts: rounds of tiles, no less than the operands'
+// way from memory, and the way of the parts' sums to memory and back.
+double estimate_us(const LinearChoice &c, int64_t rows, int64_t cols, int64_t reduce, int64_t operands, int splits, int64_t k_each) {
+    const double stages = (double)cdiv(k_each < reduce ? k_each : reduce, 64);
+    const int64_t slots = 256 * c.per_cu, n = cdiv(rows, c.bm) * cdiv(cols, c.bn) * splits, whole = n / slots, rest = n - whole * slots;
+    double us = whole * (stages * (c.per_cu > 1 ? c.full : c.one) + c.fixed);
+    if (rest > 0) {
+        const int64_t held = cdiv(rest, 256);
+        const double stage = held > 1 ? c.one + (c.full - c.one) * (held - 1) / (c.per_cu - 1) : c.one * (c.fill + (1 - c.fill) * rest / 256);
+        const double last = stages * stage + c.fixed;
+        // (where CUs hold several workgroups, those of a last, partial round begin as others end)
+        us += whole > 0 && c.per_cu > 1 ? .75 * last : last;
     }
-    if (splits > 1) us += 3 + 8. * splits * rows * cols / 4e6;
+    const double memory = 2 + operands * 2 / 5e6;
+    us = us > memory ? us : memory;
+    if (splits > 1) us += kJoinUs + kJoinPartUs * splits + 8. * splits * rows * cols / 12e6;
     return us;
 }
+double copy_us(int64_t bytes) { return 3.5 + bytes / 3.2e6; }
 
 template <Kind KIND>
 Plan plan(const LinearArgs &a) {
     const int64_t rows = KIND == kWgrad ? a.K : a.T, reduce = KIND == kWgrad ? a.T : a.K;
-    const int64_t whole = cdiv(reduce > 1 ? reduce : 1, kSplitStep) * kSplitStep;
-    Plan best = {nullptr, 1, (int)whole, -1};
-    if (!aligned_rows<KIND>(a)) return best;
+    const int64_t some = reduce > 1 ? reduce : 1;
+    // (rows along k are read in whole 16 bytes, what lies behind their end among it)
+    const bool whole_k = KIND == kWgrad || a.K % 8 == 0;
+    const bool a_fits = aligned_rows(a.A, a.lda) && whole_k, b_fits = aligned_rows(a.B, a.ldb) && (KIND == kBf16N || whole_k);
+    Plan best = {};
+    best.splits = 1;
+    best.k_each = (int)(cdiv(some, kSplitStep) * kSplitStep);
     double least = 0;
     int seen = 0;
-    auto look = [&](const Choice *c, int count) {
+    auto look = [&](const LinearChoice *c, int count, bool copies) {
         for (int i = 0; i < count; ++i, ++seen)
-            for (int want = 1; want <= 16; want *= 2) {
-                const int64_t each = cdiv(cdiv(reduce > 1 ? reduce : 1, want), kSplitStep) * kSplitStep;
-                const int splits = (int)cdiv(reduce > 1 ? reduce : 1, each);
-                if (want > 1 && (splits < 2 || each < 512)) break;
-                const double us = estimate_us(c[i], rows, a.N, reduce, (int64_t)a.N * a.K, splits, each);
+            for (int want = 1; want <= kMostSplits; want *= 2) {
+                const int64_t each = cdiv(cdiv(some, want), kSplitStep) * kSplitStep;
+                const int splits = (int)cdiv(some, each);
+                if (want > 1 && (splits < 2 || each < 256)) break;
+                Plan w = {};
+                w.choice = &c[i];
+                w.splits = splits;
+                w.k_each = (int)each;
+                w.place = seen;
+                w.ld_a = padded(a.K);
+                w.ld_b = KIND == kBf16T ? padded(a.K) : padded(a.N);
+                if (copies && !a_fits) w.a_bytes = room(a.T * w.ld_a * 2);
+                if (copies && !b_fits) w.b_bytes = room((KIND == kBf16T ? a.N : KIND == kWgrad ? a.T : a.K) * w.ld_b * 2);
+                w.copy_a = w.a_bytes > 0;
+                w.copy_b = w.b_bytes > 0;
+                if (splits > 1) w.part_bytes = room(4 * (int64_t)splits * rows * a.N);
+                double us = estimate_us(c[i], rows, a.N, reduce, a.T * a.K + (KIND == kWgrad ? a.T : a.K) * (int64_t)a.N, splits, each);
+                if (copies && !(a_fits && b_fits)) us += copy_us(w.a_bytes + w.b_bytes);
                 if (!best.choice || us < least) {
-                    best = Plan{&c[i], splits, (int)each, seen};
+                    best = w;
                     least = us;
                 }
             }
     };
     int count = 0;
-    const Choice *tiles = linear_tile_choices<KIND>(&count);
-    look(tiles, count);
-    if constexpr (KIND != kWgrad) {
-        const Choice *streams = linear_stream_choices<KIND>(&count);
-        look(streams, count);
+    if (!a_fits || !b_fits) {
+        const LinearChoice *any = linear_any_choices<KIND>(&count);
+        look(any, count, false);
+    }
+    const int64_t most = (int64_t(1) << 31) / 257;
+    if ((a_fits || padded(a.K) * 2 < most) && (b_fits || padded(KIND == kBf16T ? a.K : a.N) * 2 < most)) {
+        const LinearChoice *tiles = linear_tile_choices<KIND>(&count);
+        look(tiles, count, true);
+        if constexpr (KIND != kWgrad) {
+            const LinearChoice *streams = linear_stream_choices<KIND>(&count);
+            look(streams, count, true);
+        }
     }
     return best;
+}
+
+// Rows of bf16 at any address to aligned ones, zeros behind their ends: eight values a thread.
+struct Copy {
+    const Bf16 *from;
+    int64_t ld;
+    Bf16 *to;
+    int64_t rows, chunks;   // of eight values a row
+    int cols;
+};
+constexpr int kCopyThreads = 256;
+__global__ void __launch_bounds__(kCopyThreads) linear_copy_kernel(Copy a, Copy b, unsigned groups_a) {
+    const bool first = blockIdx.x < groups_a;
+    const Copy &c = first ? a : b;
+    const int64_t id = (int64_t)(first ? blockIdx.x : blockIdx.x - groups_a) * kCopyThreads + threadIdx.x;
+    const int64_t row = id / c.chunks, at = (id - row * c.chunks) * 8;
+    if (row >= c.rows) return;
+    const Raw8<Bf16> v = raw8(c.from + row * c.ld + at, c.cols - (int)at);
+    __builtin_memcpy(__builtin_assume_aligned(c.to + row * c.chunks * 8 + at, 16), v.v, sizeof(v.v));
 }
 
 // The sums of the parts, in their order, and the epilogue: a row's EACH columns a thread.
@@ -96,16 +142,40 @@ __global__ void __launch_bounds__(kJoinThreads) linear_join_kernel(LinearArgs p,
 template <Kind KIND>
 int64_t workspace(const LinearArgs &a) {
     const Plan w = plan<KIND>(a);
-    return w.splits > 1 ? 4 * (int64_t)w.splits * (KIND == kWgrad ? a.K : a.T) * a.N : 0;
+    return w.part_bytes + w.a_bytes + w.b_bytes;
 }
 
 template <Kind KIND>
-xtc_status launch(const LinearArgs &given, hipStream_t s) {
+xtc_status launch(const LinearArgs &given, void *workspace, hipStream_t s) {
     LinearArgs a = given;
     const Plan w = plan<KIND>(a);
+    unsigned char *ws = static_cast<unsigned char *>(workspace);
     a.splits = w.splits;
     a.k_each = w.k_each;
-    if (!w.choice) return launch_linear_any<KIND>(a, s);
+    a.part = reinterpret_cast<float *>(ws);
+    if (w.copy_a || w.copy_b) {
+        Copy ca = {}, cb = {};
+        int64_t groups_a = 0, groups_b = 0;
+        if (w.copy_a) {
+            ca = Copy{static_cast<const Bf16 *>(a.A), a.lda, reinterpret_cast<Bf16 *>(ws + w.part_bytes), a.T, w.ld_a / 8, a.K};
+            groups_a = cdiv(ca.rows * ca.chunks, kCopyThreads);
+            a.A = ca.to;
+            a.lda = w.ld_a;
+        }
+        if (w.copy_b) {
+            cb = Copy{static_cast<const Bf16 *>(a.B), a.ldb, reinterpret_cast<Bf16 *>(ws + w.part_bytes + w.a_bytes),
+                      KIND == kBf16T ? a.N : KIND == kWgrad ? a.T : a.K, w.ld_b / 8, KIND == kBf16T ? a.K : a.N};
+            groups_b = cdiv(cb.rows * cb.chunks, kCopyThreads);
+            a.B = cb.to;
+            a.ldb = w.ld_b;
+        }
+        if (groups_a + groups_b >= kMostGroups) return XTC_ERR_TOO_LARGE;
+        if (groups_a + groups_b > 0) {
+            linear_copy_kernel<<<(unsigned)(groups_a + groups_b), kCopyThreads, 0, s>>>(ca, cb, (unsigned)groups_a);
+            const xtc_status st = hip_status(hipGetLastError());
+            if (st != XTC_OK) return st;
+        }
+    }
     const xtc_status st = w.choice->launch(a, s);
     if (st != XTC_OK || a.splits == 1) return st;
     const int64_t rows = KIND == kWgrad ? a.K : a.T;
@@ -158,11 +228,11 @@ __global__ void __launch_bounds__(kSlopeWaves * 64) activation_backward_kernel(A
 int64_t linear_workspace(const LinearArgs &a, bool b_rows_n) {
     return b_rows_n ? workspace<kBf16T>(a) : workspace<kBf16N>(a);
 }
-xtc_status launch_linear(const LinearArgs &a, bool b_rows_n, hipStream_t s) {
-    return b_rows_n ? launch<kBf16T>(a, s) : launch<kBf16N>(a, s);
+xtc_status launch_linear(const LinearArgs &a, bool b_rows_n, void *workspace, hipStream_t s) {
+    return b_rows_n ? launch<kBf16T>(a, workspace, s) : launch<kBf16N>(a, workspace, s);
 }
 int64_t linear_wgrad_workspace(const LinearArgs &a) { return workspace<kWgrad>(a); }
-xtc_status launch_linear_wgrad(const LinearArgs &a, hipStream_t s) { return launch<kWgrad>(a, s); }
+xtc_status launch_linear_wgrad(const LinearArgs &a, void *workspace, hipStream_t s) { return launch<kWgrad>(a, workspace, s); }
 
 int activation_slabs(int64_t T, int64_t N) {
     const int64_t across = cdiv(N, kSlopeColumns), rows = cdiv(T, kSlopeWaves), most = across < 2048 ? 2048 / across : 1;

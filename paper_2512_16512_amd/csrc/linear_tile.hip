@@ -2,43 +2,73 @@
 #include "grouped_tile.h"
 
 namespace xtc {
+namespace {
 
+template <Kind KIND, int BM, int BN, int WM, int WN, int STAGES, int KB, bool ANY = false>
+constexpr auto kLaunch = launch_tiles<KIND, false, BM, BN, WM, WN, STAGES, KB, ANY, LinearArgs>;
+
+}  // namespace
+
+// Measured, these and those of linear_stream.hip, on 145 layers of 1 to 16384 rows and widths of 512 to 8192, each
+// kernel with 1 to 16 splits: the kernel chosen by the estimate takes 1.5 % longer than the best of all in the mean,
+// 30 % at most (2 rows, 4608 to 576: 9.0 us for 6.9).  8192 x 4096 to 4096 216 us (tiles of 256x256, 1275 TFLOP/s; those
+// of 128x128 263), 1531 x 4096 to 2000 35 us (128x128 in two splits; 56 with the choices of the grouped products).
 template <Kind KIND>
-const Choice *linear_tile_choices(int *count) {
+const LinearChoice *linear_tile_choices(int *count) {
     if constexpr (KIND == kWgrad) {
-        static const Choice all[] = {
-            {256, 256, 1, 1.5f, 1.5f, 1.5f, 12, false, launch_tiles<KIND, false, 256, 256, 128, 64, 4, 64, false, LinearArgs>},
-            {128, 256, 1, .81f, .81f, .81f, 7.9f, false, launch_tiles<KIND, false, 128, 256, 64, 64, 3, 128, false, LinearArgs>},
-            {128, 128, 2, .7f, .7f, 1.18f, 7.1f, false, launch_tiles<KIND, false, 128, 128, 64, 64, 2, 128, false, LinearArgs>},
+        static const LinearChoice all[] = {
+            {256, 256, 1, 1.39f, 1.39f, 14.8f, .79f, kLaunch<KIND, 256, 256, 128, 64, 4, 64>},
+            {128, 256, 1, .78f, .78f, 10.6f, .75f, kLaunch<KIND, 128, 256, 64, 64, 3, 128>},
+            {128, 128, 2, .7f, .87f, 9.5f, .75f, kLaunch<KIND, 128, 128, 64, 64, 2, 128>},
         };
         *count = 3;
         return all;
     } else {
-        static const Choice all[] = {
-            {256, 256, 1, 1.5f, 1.5f, 1.5f, 8, false, launch_tiles<KIND, false, 256, 256, 128, 64, 2, 128, false, LinearArgs>},
-            {128, 256, 2, 1.25f, 1.25f, 2.2f, 5, false, launch_tiles<KIND, false, 128, 256, 64, 128, 3, 64, false, LinearArgs>},
-            {128, 256, 1, .9f, .9f, .9f, 5, false, launch_tiles<KIND, false, 128, 256, 64, 64, 3, 128, false, LinearArgs>},
-            {128, 128, 2, .7f, 1.05f, 1.7f, 3, false, launch_tiles<KIND, false, 128, 128, 64, 64, 2, 128, false, LinearArgs>},
-            {64, 128, 3, .6f, 1.f, 1.5f, 2, false, launch_tiles<KIND, false, 64, 128, 64, 32, 2, 128, false, LinearArgs>},
+        constexpr bool N = KIND == kBf16N;
+        static const LinearChoice all[] = {
+            {256, 256, 1, N ? 1.44f : 1.34f, N ? 1.44f : 1.34f, 11.8f, N ? .64f : .74f, kLaunch<KIND, 256, 256, 128, 64, 2, 128>},
+            {256, 128, 1, N ? .76f : .74f, N ? .76f : .74f, N ? 8.2f : 8.f, .78f, kLaunch<KIND, 256, 128, 64, 64, 3, 128>},
+            {128, 256, 1, N ? .76f : .73f, N ? .76f : .73f, N ? 8.5f : 8.4f, .78f, kLaunch<KIND, 128, 256, 64, 64, 3, 128>},
+            {128, 128, 2, N ? .7f : .63f, N ? .89f : .85f, 7.3f, .73f, kLaunch<KIND, 128, 128, 64, 64, 2, 128>},
+            {128, 128, 1, N ? .44f : .42f, N ? .44f : .42f, N ? 6.6f : 6.1f, .88f, kLaunch<KIND, 128, 128, 64, 32, 4, 128>},
+            {64, 128, 1, N ? .35f : .29f, N ? .35f : .29f, 5.1f, 1, kLaunch<KIND, 64, 128, 64, 16, 4, 128>},
+            {64, 64, 2, N ? .28f : .25f, N ? .39f : .37f, N ? 4.9f : 4.6f, .75f, kLaunch<KIND, 64, 64, 64, 16, 4, 128>},
         };
-        *count = 5;
+        *count = 7;
         return all;
     }
 }
 
+// Rows at any address go through registers; copied first they run the kernels above where that is faster (a
+// weights' gradient of 12190 rows, 803 x 6111: 208 us with the copies of 184 MB, 372 without; one row, 7833 to 2849: 25 us
+// through registers, 30 copied).
 template <Kind KIND>
-xtc_status launch_linear_any(const LinearArgs &a, hipStream_t s) {
-    if constexpr (KIND != kWgrad) {
-        if (a.T <= 64) return launch_tiles<KIND, false, 64, 128, 64, 32, 2, 128, true, LinearArgs>(a, s);
+const LinearChoice *linear_any_choices(int *count) {
+    if constexpr (KIND == kWgrad) {
+        static const LinearChoice all[] = {
+            {128, 128, 2, 1.3f, 2.f, 14.f, 1, kLaunch<KIND, 128, 128, 64, 64, 2, 128, true>},
+            {64, 128, 2, 1.15f, 1.33f, 8.7f, .5f, kLaunch<KIND, 64, 128, 64, 32, 2, 128, true>},
+            {64, 64, 2, .9f, 1.f, 4.4f, .74f, kLaunch<KIND, 64, 64, 64, 16, 2, 128, true>},
+        };
+        *count = 3;
+        return all;
+    } else {
+        constexpr bool N = KIND == kBf16N;
+        static const LinearChoice all[] = {
+            {128, 128, 2, N ? 1.6f : 1.43f, 1.9f, 10.4f, .5f, kLaunch<KIND, 128, 128, 64, 64, 2, 128, true>},
+            {64, 128, 1, N ? .97f : .82f, N ? .97f : .82f, N ? 4.4f : 5.7f, N ? 1.f : .64f, kLaunch<KIND, 64, 128, 64, 16, 2, 128, true>},
+            {64, 64, 2, N ? 1.03f : .7f, N ? 1.03f : .91f, 6.1f, .45f, kLaunch<KIND, 64, 64, 64, 16, 2, 128, true>},
+        };
+        *count = 3;
+        return all;
     }
-    return launch_tiles<KIND, false, 128, 128, 64, 64, 2, 128, true, LinearArgs>(a, s);
 }
 
-template xtc_status launch_linear_any<kBf16N>(const LinearArgs &, hipStream_t);
-template xtc_status launch_linear_any<kBf16T>(const LinearArgs &, hipStream_t);
-template xtc_status launch_linear_any<kWgrad>(const LinearArgs &, hipStream_t);
-template const Choice *linear_tile_choices<kBf16N>(int *);
-template const Choice *linear_tile_choices<kBf16T>(int *);
-template const Choice *linear_tile_choices<kWgrad>(int *);
+template const LinearChoice *linear_any_choices<kBf16N>(int *);
+template const LinearChoice *linear_any_choices<kBf16T>(int *);
+template const LinearChoice *linear_any_choices<kWgrad>(int *);
+template const LinearChoice *linear_tile_choices<kBf16N>(int *);
+template const LinearChoice *linear_tile_choices<kBf16T>(int *);
+template const LinearChoice *linear_tile_choices<kWgrad>(int *);
 
 }  // namespace xtc

@@ -255,11 +255,13 @@ xtc_status xtc_matmul_grouped_wgrad(int64_t G, int64_t T, int64_t N, int64_t K, 
     return launch_grouped_wgrad(a, static_cast<hipStream_t>(stream));
 }
 
-int64_t xtc_linear_workspace(int64_t T, int64_t N, int64_t K, int32_t transpose_b) {
+int64_t xtc_linear_workspace(int64_t T, int64_t N, int64_t K, const void *A, int64_t lda, const void *B, int64_t ldb,
+                             int32_t transpose_b) {
     if (T < 0 || N < 0 || K < 0 || T > kMostExtent || N > kMostExtent || K > kMostExtent) return -1;
     if (T == 0 || N == 0) return 0;
     LinearArgs a = {};
     a.T = T; a.N = (int)N; a.K = (int)K;
+    a.A = A; a.lda = lda; a.B = B; a.ldb = ldb;
     return linear_workspace(a, transpose_b != 0);
 }
 
@@ -279,7 +281,6 @@ xtc_status xtc_linear(int64_t T, int64_t N, int64_t K, const void *A, int64_t ld
     a.R = R; a.ldr = ldr; a.r_f32 = r_dtype == XTC_F32;
     a.Z = Z; a.ldz = ldz;
     a.act = activation;
-    a.part = static_cast<float *>(workspace);
     const xtc_status st = check_product(a, N, K, 1, transpose_b ? K : N, transpose_b ? N : K, N, out_dtype, 2);
     if (st != XTC_OK) return st;
     if ((R && ldr > kMostStride) || (Z && ldz > kMostStride)) return XTC_ERR_TOO_LARGE;
@@ -289,17 +290,19 @@ xtc_status xtc_linear(int64_t T, int64_t N, int64_t K, const void *A, int64_t ld
         return XTC_ERR_MISALIGNED;
     if (T == 0 || N == 0) return XTC_OK;
     if (!C || (K > 0 && (!A || !B))) return XTC_ERR_NULL_POINTER;
-    const int64_t need = xtc_linear_workspace(T, N, K, transpose_b);
+    const int64_t need = xtc_linear_workspace(T, N, K, A, lda, B, ldb, transpose_b);
     if (workspace_bytes < need) return XTC_ERR_BAD_SHAPE;
     if (need > 0 && !workspace) return XTC_ERR_NULL_POINTER;
-    return launch_linear(a, transpose_b != 0, static_cast<hipStream_t>(stream));
+    return launch_linear(a, transpose_b != 0, workspace, static_cast<hipStream_t>(stream));
 }
 
-int64_t xtc_linear_wgrad_workspace(int64_t T, int64_t N, int64_t K) {
+int64_t xtc_linear_wgrad_workspace(int64_t T, int64_t N, int64_t K, const void *A, int64_t lda, const void *DY,
+                                   int64_t lddy) {
     if (T < 0 || N < 0 || K < 0 || T > kMostExtent || N > kMostExtent || K > kMostExtent) return -1;
     if (N == 0 || K == 0) return 0;
     LinearArgs a = {};
     a.T = T; a.N = (int)N; a.K = (int)K;
+    a.A = A; a.lda = lda; a.B = DY; a.ldb = lddy;
     return linear_wgrad_workspace(a);
 }
 
@@ -313,16 +316,15 @@ xtc_status xtc_linear_wgrad(int64_t T, int64_t N, int64_t K, const void *A, int6
     a.A = A; a.lda = lda; a.B = DY; a.ldb = lddy;
     a.C = DB; a.ldc = lddb;
     a.out_bf16 = out_dtype == XTC_BF16;
-    a.part = static_cast<float *>(workspace);
     const xtc_status st = check_product(a, N, K, 1, N, T, N, out_dtype, 2);
     if (st != XTC_OK) return st;
     if (!aligned_to(workspace, 16)) return XTC_ERR_MISALIGNED;
     if (N == 0 || K == 0) return XTC_OK;
     if (!DB || (T > 0 && (!A || !DY))) return XTC_ERR_NULL_POINTER;
-    const int64_t need = xtc_linear_wgrad_workspace(T, N, K);
+    const int64_t need = xtc_linear_wgrad_workspace(T, N, K, A, lda, DY, lddy);
     if (workspace_bytes < need) return XTC_ERR_BAD_SHAPE;
     if (need > 0 && !workspace) return XTC_ERR_NULL_POINTER;
-    return launch_linear_wgrad(a, static_cast<hipStream_t>(stream));
+    return launch_linear_wgrad(a, workspace, static_cast<hipStream_t>(stream));
 }
 
 int64_t xtc_activation_backward_workspace(int64_t T, int64_t N) {

@@ -463,7 +463,7 @@ PyObject *linear(PyObject *, PyObject *const *args, Py_ssize_t n) {
         xtc_dtype code;
         if (!result(given, args[8], {T, N}, a, &r[0], &code)) Py_RETURN_NONE;
         if (keep) r[1] = fresh({T, N}, r[0].scalar_type(), a);
-        const int64_t size = xtc_linear_workspace(T, N, K, turned);
+        const int64_t size = xtc_linear_workspace(T, N, K, a.data_ptr(), row_stride(a), b.data_ptr(), row_stride(b), turned);
         if (size < 0) Py_RETURN_NONE;
         if (size > 0) work = fresh({size}, at::kByte, a);
         void *stream = stream_of(a);
@@ -492,7 +492,7 @@ PyObject *linear_wgrad(PyObject *, PyObject *const *args, Py_ssize_t n) {
         at::Tensor c, work;
         xtc_dtype code;
         if (!result(t[2], args[3], {K, N}, a, &c, &code)) Py_RETURN_NONE;
-        const int64_t size = xtc_linear_wgrad_workspace(T, N, K);
+        const int64_t size = xtc_linear_wgrad_workspace(T, N, K, a.data_ptr(), row_stride(a), dy.data_ptr(), row_stride(dy));
         if (size < 0) Py_RETURN_NONE;
         if (size > 0) work = fresh({size}, at::kByte, a);
         void *stream = stream_of(a);

@@ -69,11 +69,11 @@ def test_linear_refuses(change, status):
 
 
 def test_linear_workspaces():
-    assert x.xtc_linear_workspace(-1, 4, 4, 0) == -1 and x.xtc_linear_workspace(4, 4, BIG, 0) == -1
-    assert x.xtc_linear_wgrad_workspace(4, -1, 4) == -1 and x.xtc_activation_backward_workspace(BIG, 4) == -1
-    assert x.xtc_linear_workspace(0, 4, 4, 0) == 0 and x.xtc_linear_wgrad_workspace(4, 0, 4) == 0
+    assert x.xtc_linear_workspace(-1, 4, 4, BAD, 8, BAD, 8, 0) == -1 and x.xtc_linear_workspace(4, 4, BIG, BAD, 8, BAD, 8, 0) == -1
+    assert x.xtc_linear_wgrad_workspace(4, -1, 4, BAD, 8, BAD, 8) == -1 and x.xtc_activation_backward_workspace(BIG, 4) == -1
+    assert x.xtc_linear_workspace(0, 4, 4, BAD, 8, BAD, 8, 0) == 0 and x.xtc_linear_wgrad_workspace(4, 0, 4, BAD, 8, BAD, 8) == 0
     # a reduction long enough that its parts go to several workgroups, each part's sums a whole result
-    need = x.xtc_linear_wgrad_workspace(16384, 256, 256)
+    need = x.xtc_linear_wgrad_workspace(16384, 256, 256, BAD, 256, BAD, 256)
     assert need > 0 and need % (4 * 256 * 256) == 0
     assert call(x.xtc_linear_wgrad, WGRAD, T=16384, N=256, K=256, lda=256, lddy=256, lddb=256, workspace_bytes=need - 1) == 2
     assert call(x.xtc_linear_wgrad, WGRAD, T=16384, N=256, K=256, lda=256, lddy=256, lddb=256, workspace_bytes=need,
