@@ -12,11 +12,13 @@ namespace {
 
 constexpr int kWaves = 4, kColumns = 512;      // columns of a wave, eight a lane
 
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
 // A wave a token and 512 columns of it: kAtOnce rows are on their way together.
 constexpr int kAtOnce = 8;
 template <typename T, typename R, typename O>
 __global__ void __launch_bounds__(kWaves * 64) combine_kernel(CombineArgs p, int chunks) {
-    const int64_t id = (int64_t)blockIdx.x * kWaves + threadIdx.x / 64, t = id / chunks;
+    const int64_t id = (int64_t)blockIdx.x * kWaves + wave_id(), t = id / chunks;
     if (t >= p.T) return;
     const int c = (int)(id - t * chunks) * kColumns + (threadIdx.x & 63) * 8, valid = p.D - c;
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
@@ -34,7 +36,7 @@ __global__ void __launch_bounds__(kWaves * 64) combine_kernel(CombineArgs p, int
             }
             const bool in = r >= 0 && r < p.R;
             w[j] = in ? w[j] : 0.f;
-            v[j] = raw8(static_cast<const T *>(p.rows) + (in ? r : 0) * p.ldrows + c, in ? valid : 0);
+            v[j] = raw8_once(static_cast<const T *>(p.rows) + (in ? r : 0) * p.ldrows + c, in ? valid : 0);
         }
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j)
@@ -44,12 +46,14 @@ __global__ void __launch_bounds__(kWaves * 64) combine_kernel(CombineArgs p, int
     store8(static_cast<O *>(p.out) + t * p.ldo + c, valid, sum);
 }
 
-// A wave a token: its row of dout stays in registers over the rows of up to kAtOnce choices.
-template <typename T, typename G>
+// SHARE waves a token, 512 columns each in turn: their part of dout's row stays in registers over the
+// rows of up to kAtOnce choices, and their sums of dp meet in LDS.
+template <typename T, typename G, int SHARE>
 __global__ void __launch_bounds__(kWaves * 64) combine_backward_kernel(CombineBackwardArgs p) {
-    const int64_t t = (int64_t)blockIdx.x * kWaves + threadIdx.x / 64;
-    const int lane = threadIdx.x & 63;
-    if (t >= p.T) return;
+    __shared__ float part[kWaves][kAtOnce];
+    const int wave = wave_id(), lane = threadIdx.x & 63, share = wave % SHARE;
+    const int64_t t = (int64_t)blockIdx.x * (kWaves / SHARE) + wave / SHARE;
+    if (t >= p.T) return;                // (SHARE > 1: the whole workgroup)
     for (int j0 = 0; j0 < p.top; j0 += kAtOnce) {
         float w[kAtOnce], dot[kAtOnce];
         int64_t r[kAtOnce];
@@ -60,14 +64,14 @@ __global__ void __launch_bounds__(kWaves * 64) combine_backward_kernel(CombineBa
             w[j] = r[j] >= 0 ? p.P[t * p.top + j0 + j] : 0.f;
             dot[j] = 0.f;
         }
-        for (int c = lane * 8; c < p.D; c += kColumns) {
+        for (int c = share * kColumns + lane * 8; c < p.D; c += SHARE * kColumns) {
             const int valid = p.D - c;
             float d[8];
-            load8(static_cast<const G *>(p.DOUT) + t * p.lddo + c, valid, d);
             Raw8<T> v[kAtOnce];
 #pragma unroll
             for (int j = 0; j < kAtOnce; ++j)
-                v[j] = raw8(static_cast<const T *>(p.rows) + (r[j] >= 0 ? r[j] : 0) * p.ldrows + c, r[j] >= 0 ? valid : 0);
+                v[j] = raw8_once(static_cast<const T *>(p.rows) + (r[j] >= 0 ? r[j] : 0) * p.ldrows + c, r[j] >= 0 ? valid : 0);
+            load8(static_cast<const G *>(p.DOUT) + t * p.lddo + c, valid, d);
 #pragma unroll
             for (int j = 0; j < kAtOnce; ++j) {
                 if (r[j] < 0) continue;
@@ -77,13 +81,29 @@ __global__ void __launch_bounds__(kWaves * 64) combine_backward_kernel(CombineBa
                     dot[j] += d[i] * v[j].at(i);
                     o[i] = w[j] * d[i];
                 }
-                store8(static_cast<T *>(p.DROWS) + r[j] * p.lddr + c, valid, o);
+                store8_to(static_cast<T *>(p.DROWS) + r[j] * p.lddr + c, valid, o, p.past);
             }
         }
+        if constexpr (SHARE > 1) {
+            if (j0 > 0) __syncthreads();
 #pragma unroll
-        for (int j = 0; j < kAtOnce; ++j) {
-            const float s = lanes_sum<64>(dot[j]);
-            if (lane == 0 && j0 + j < p.top) p.DP[t * p.top + j0 + j] = s;
+            for (int j = 0; j < kAtOnce; ++j) {
+                const float s = lanes_sum<64>(dot[j]);
+                if (lane == j) part[wave][j] = s;
+            }
+            __syncthreads();
+            if (wave == 0 && lane < kAtOnce && j0 + lane < p.top) {
+                float s = 0.f;
+#pragma unroll
+                for (int i = 0; i < SHARE; ++i) s += part[i][lane];
+                p.DP[t * p.top + j0 + lane] = s;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) {
+                const float s = lanes_sum<64>(dot[j]);
+                if (lane == 0 && j0 + j < p.top) p.DP[t * p.top + j0 + j] = s;
+            }
         }
     }
     // this token's share of the rows that belong to none: zeros
@@ -91,7 +111,8 @@ __global__ void __launch_bounds__(kWaves * 64) combine_backward_kernel(CombineBa
         const int64_t i = t * p.top + j;
         if (i >= p.R || p.token[i] >= 0) continue;
         const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        for (int c = lane * 8; c < p.D; c += kColumns) store8(static_cast<T *>(p.DROWS) + i * p.lddr + c, p.D - c, zero);
+        for (int c = share * kColumns + lane * 8; c < p.D; c += SHARE * kColumns)
+            store8_to(static_cast<T *>(p.DROWS) + i * p.lddr + c, p.D - c, zero, p.past);
     }
 }
 
@@ -109,13 +130,24 @@ xtc_status launch_combine(const CombineArgs &a, xtc_dtype dtype, xtc_dtype r_dty
     return hip_status(hipGetLastError());
 }
 
-xtc_status launch_combine_backward(const CombineBackwardArgs &a, xtc_dtype dtype, xtc_dtype g_dtype, hipStream_t s) {
-    const int64_t groups = (a.T + kWaves - 1) / kWaves;
+namespace {
+
+template <int SHARE>
+xtc_status launch_shared(const CombineBackwardArgs &a, xtc_dtype dtype, xtc_dtype g_dtype, hipStream_t s) {
+    const int64_t each = kWaves / SHARE, groups = (a.T + each - 1) / each;
     if (groups >= kMostGroups) return XTC_ERR_TOO_LARGE;
-    const auto kernel = dtype == XTC_F32 ? (g_dtype == XTC_F32 ? combine_backward_kernel<float, float> : combine_backward_kernel<float, Bf16>)
-                                         : (g_dtype == XTC_F32 ? combine_backward_kernel<Bf16, float> : combine_backward_kernel<Bf16, Bf16>);
+    const auto kernel = dtype == XTC_F32 ? (g_dtype == XTC_F32 ? combine_backward_kernel<float, float, SHARE> : combine_backward_kernel<float, Bf16, SHARE>)
+                                         : (g_dtype == XTC_F32 ? combine_backward_kernel<Bf16, float, SHARE> : combine_backward_kernel<Bf16, Bf16, SHARE>);
     kernel<<<(unsigned)groups, kWaves * 64, 0, s>>>(a);
     return hip_status(hipGetLastError());
+}
+
+}  // namespace
+
+xtc_status launch_combine_backward(const CombineBackwardArgs &given, xtc_dtype dtype, xtc_dtype g_dtype, hipStream_t s) {
+    CombineBackwardArgs a = given;
+    a.past = whole_lines(a.DROWS, a.lddr, dtype == XTC_F32 ? 4 : 2);
+    return a.D > kColumns ? launch_shared<kWaves>(a, dtype, g_dtype, s) : launch_shared<1>(a, dtype, g_dtype, s);
 }
 
 }  // namespace xtc

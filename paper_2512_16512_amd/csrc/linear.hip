@@ -188,7 +188,7 @@ xtc_status launch(const LinearArgs &given, void *workspace, hipStream_t s) {
 
 // dz = dy act'(z), and the column sums of a slab of rows: a wave takes 512 columns of a row at
 // a time, eight a lane, the workgroup's four waves rows in turn.
-constexpr int kSlopeColumns = 512, kSlopeWaves = 4;
+constexpr int kSlopeColumns = 512, kSlopeWaves = 4, kSlopeRows = 4;   // (rows on their way at once)
 template <typename TY, typename TZ>
 __global__ void __launch_bounds__(kSlopeWaves * 64) activation_backward_kernel(ActivationArgs p) {
     __shared__ float sums[kSlopeWaves - 1][8][64];
@@ -197,16 +197,27 @@ __global__ void __launch_bounds__(kSlopeWaves * 64) activation_backward_kernel(A
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     with_activation(p.act, [&](auto ACT) __attribute__((always_inline)) {
         const int64_t step = (int64_t)gridDim.y * kSlopeWaves;
-        for (int64_t t = (int64_t)blockIdx.y * kSlopeWaves + wave; t < p.T; t += step) {
-            float d[8], z[8];
-            load8(static_cast<const TY *>(p.DY) + t * p.lddy + c, valid, d);
-            load8(static_cast<const TZ *>(p.Z) + t * p.ldz + c, valid, z);
+        for (int64_t t = (int64_t)blockIdx.y * kSlopeWaves + wave; t < p.T; t += kSlopeRows * step) {
+            Raw8<TY> y[kSlopeRows];
+            Raw8<TZ> z[kSlopeRows];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                d[i] *= slope<ACT()>(z[i]);
-                sum[i] += d[i];
+            for (int r = 0; r < kSlopeRows; ++r) {
+                const int64_t at = t + r * step;
+                const int in = at < p.T ? valid : 0;
+                y[r] = raw8_once(static_cast<const TY *>(p.DY) + at * p.lddy + c, in);
+                z[r] = raw8_once(static_cast<const TZ *>(p.Z) + at * p.ldz + c, in);
             }
-            store8(static_cast<Bf16 *>(p.DZ) + t * p.lddz + c, valid, d);
+#pragma unroll
+            for (int r = 0; r < kSlopeRows; ++r) {
+                const int64_t at = t + r * step;
+                float d[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    d[i] = y[r].at(i) * slope<ACT()>(z[r].at(i));
+                    sum[i] += d[i];
+                }
+                store8_to(static_cast<Bf16 *>(p.DZ) + at * p.lddz + c, at < p.T ? valid : 0, d, p.past);
+            }
         }
     });
     if (!p.DB) return;
@@ -239,7 +250,9 @@ int activation_slabs(int64_t T, int64_t N) {
     return (int)(rows < most ? (rows > 1 ? rows : 1) : most);
 }
 
-xtc_status launch_activation_backward(const ActivationArgs &a, hipStream_t s) {
+xtc_status launch_activation_backward(const ActivationArgs &given, hipStream_t s) {
+    ActivationArgs a = given;
+    a.past = whole_lines(a.DZ, a.lddz, 2);
     const int slabs = activation_slabs(a.T, a.N);
     const auto kernel = a.dy_f32 ? (a.z_f32 ? activation_backward_kernel<float, float> : activation_backward_kernel<float, Bf16>)
                                  : (a.z_f32 ? activation_backward_kernel<Bf16, float> : activation_backward_kernel<Bf16, Bf16>);

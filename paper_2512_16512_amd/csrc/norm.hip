@@ -95,8 +95,8 @@ __global__ void __launch_bounds__(RowTeam<NT>::THREADS) norm_kernel(NormArgs p) 
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         const int c = (v * NT + tid) * 8;
-        rx[v] = raw8(x + c, D - c);
-        if (r) rr[v] = raw8(r + c, D - c);
+        rx[v] = CENTER ? raw8_once(x + c, D - c) : raw8(x + c, D - c);
+        if (r) rr[v] = CENTER ? raw8_once(r + c, D - c) : raw8(r + c, D - c);
     }
     float h[NV][8], sum = 0.f;
 #pragma unroll
@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(RowTeam<NT>::THREADS) norm_kernel(NormArgs p) 
     for (int v = 0; v < NV; ++v) {
         const int c = (v * NT + tid) * 8, valid = D - c;
         const Raw8<float> w = raw_weight(p.W, p.w_f32, x, c, valid);
-        if (p.H) store8(static_cast<T *>(p.H) + t * p.ldh + c, valid, h[v]);
+        if (p.H) (CENTER ? store8_past<T> : store8<T>)(static_cast<T *>(p.H) + t * p.ldh + c, valid, h[v]);
         Raw8<float> b = {};
         if constexpr (CENTER) {
             if (p.B) b = raw_weight(p.B, p.w_f32, x, c, valid);
@@ -144,7 +144,7 @@ __global__ void __launch_bounds__(RowTeam<NT>::THREADS) norm_kernel(NormArgs p) 
             store_fp8(static_cast<uint8_t *>(p.Y) + t * p.ldy + c, valid, to_fp8(y, s));
             if ((tid & 15) == 0 && valid > 0) p.S[t * p.lds + c / kScaleBlock] = s;
         } else {
-            store8(static_cast<T *>(p.Y) + t * p.ldy + c, valid, y);
+            (CENTER ? store8_past<T> : store8<T>)(static_cast<T *>(p.Y) + t * p.ldy + c, valid, y);
         }
     }
 }
@@ -222,14 +222,15 @@ __global__ void __launch_bounds__(kThreads) norm_loop_kernel(NormArgs p) {
 // workgroup leaves one row of partial sums (CENTER: of 2D, DW's first).  The next row is on its way while one is computed.
 // 8191 x 2048 bf16, bound by memory: 28.6 us, 4.7 TB/s; DX and DW by kernels of
 // their own, which read the rows twice, took 151 us.
-template <typename T, bool CENTER, int NT, int NV>
-__global__ void __launch_bounds__(RowTeam<NT>::THREADS) norm_backward_kernel(NormBackwardArgs p) {
+template <typename T, bool CENTER, int NT, int NV, int TEAMS>
+__global__ void __launch_bounds__(NT * TEAMS) norm_backward_kernel(NormBackwardArgs p) {
     typedef RowTeam<NT> Team;
     __shared__ float scratch[NT / 64];
-    __shared__ float sums[NT == 64 ? 3 * 64 * NV * 8 : 1];   // of the workgroup's other teams
+    __shared__ float two[CENTER ? 2 : 1][TEAMS][NT / 64][2];          // the centred sums, of two trips in turn
+    __shared__ float sums[TEAMS > 1 ? (TEAMS - 1) * NT * NV * 8 : 1];   // of the workgroup's other teams
     constexpr int NB = CENTER ? NV : 1;
     const int tid = threadIdx.x % NT, team = threadIdx.x / NT, D = p.D;
-    const int64_t step = (int64_t)gridDim.x * Team::ROWS;
+    const int64_t step = (int64_t)gridDim.x * TEAMS;
     Raw8<T> rx[NV], ry[NV], rr[NV];
     float w[NV][8], dw[NV][8], db[NB][8], rstd_next = 0.f, mean_next = 0.f;
 #pragma unroll
@@ -247,17 +248,19 @@ __global__ void __launch_bounds__(RowTeam<NT>::THREADS) norm_backward_kernel(Nor
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c = (v * NT + tid) * 8, valid = t < p.T ? D - c : 0;
-            rx[v] = raw8(static_cast<const T *>(p.X) + t * p.ldx + c, valid);
-            ry[v] = raw8(static_cast<const T *>(p.DY) + t * p.lddy + c, valid);
-            if (p.DR) rr[v] = raw8(static_cast<const T *>(p.DR) + t * p.lddr + c, valid);
+            const auto read = CENTER ? raw8_once<T> : raw8<T>;
+            rx[v] = read(static_cast<const T *>(p.X) + t * p.ldx + c, valid);
+            ry[v] = read(static_cast<const T *>(p.DY) + t * p.lddy + c, valid);
+            if (p.DR) rr[v] = read(static_cast<const T *>(p.DR) + t * p.lddr + c, valid);
         }
         rstd_next = t < p.T ? p.rstd[t] : 0.f;
         if constexpr (CENTER) mean_next = t < p.T ? p.mean[t] : 0.f;
     };
     // (every team of a workgroup takes part in every trip: the sums below have barriers)
-    int64_t t = (int64_t)blockIdx.x * Team::ROWS + team;
+    int64_t t = (int64_t)blockIdx.x * TEAMS + team;
+    int turn = 0;
     fetch(t);
-    for (int64_t t0 = (int64_t)blockIdx.x * Team::ROWS; t0 < p.T; t0 += step, t += step) {
+    for (int64_t t0 = (int64_t)blockIdx.x * TEAMS; t0 < p.T; t0 += step, t += step) {
         const float rstd = rstd_next, centre = mean_next;
         float h[NV][8], g[NV][8], d[NV][8], sum = 0.f, sum_g = 0.f;
 #pragma unroll
@@ -275,9 +278,31 @@ __global__ void __launch_bounds__(RowTeam<NT>::THREADS) norm_backward_kernel(Nor
                 sum += g[v][i] * h[v][i];
             }
         fetch(t + step);
-        const float mean = Team::sum(sum, scratch) / (float)D;
         float mean_g = 0.f;
-        if constexpr (CENTER) mean_g = Team::sum(sum_g, scratch) / (float)D;
+        if constexpr (CENTER) {
+            // both sums at once; what a wave still reads of one trip the next does not write
+            sum = lanes_sum<64>(sum);
+            sum_g = lanes_sum<64>(sum_g);
+            if constexpr (NT > 64) {
+                float (&at)[NT / 64][2] = two[turn][team];
+                if ((tid & 63) == 0) {
+                    at[tid >> 6][0] = sum;
+                    at[tid >> 6][1] = sum_g;
+                }
+                __syncthreads();
+                sum = sum_g = 0.f;
+#pragma unroll
+                for (int i = 0; i < NT / 64; ++i) {
+                    sum += at[i][0];
+                    sum_g += at[i][1];
+                }
+                turn ^= 1;
+            }
+            mean_g = sum_g / (float)D;
+        } else {
+            sum = Team::sum(sum, scratch);
+        }
+        const float mean = sum / (float)D;
         if (t < p.T) {
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
@@ -285,18 +310,18 @@ __global__ void __launch_bounds__(RowTeam<NT>::THREADS) norm_backward_kernel(Nor
                 float o[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) o[i] = d[v][i] + rstd * (CENTER ? g[v][i] - mean_g - h[v][i] * mean : g[v][i] - h[v][i] * mean);
-                store8(static_cast<T *>(p.DX) + t * p.lddx + c, D - c, o);
+                store8_to(static_cast<T *>(p.DX) + t * p.lddx + c, D - c, o, CENTER && p.past);
             }
         }
     }
     // the other teams' sums are added, and the workgroup's row of them written
     auto leave = [&](auto &sum, float *to) __attribute__((always_inline)) {
-        if constexpr (NT == 64) {
+        if constexpr (TEAMS > 1) {
             if (team > 0) {
 #pragma unroll
                 for (int v = 0; v < NV; ++v)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) sums[((team - 1) * NV * 8 + v * 8 + i) * 64 + tid] = sum[v][i];
+                    for (int i = 0; i < 8; ++i) sums[((team - 1) * NV * 8 + v * 8 + i) * NT + tid] = sum[v][i];
             }
             __syncthreads();
             if (team == 0) {
@@ -305,10 +330,10 @@ __global__ void __launch_bounds__(RowTeam<NT>::THREADS) norm_backward_kernel(Nor
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
 #pragma unroll
-                        for (int q = 0; q < 3; ++q) sum[v][i] += sums[(q * NV * 8 + v * 8 + i) * 64 + tid];
+                        for (int q = 0; q < TEAMS - 1; ++q) sum[v][i] += sums[(q * NV * 8 + v * 8 + i) * NT + tid];
             }
         }
-        if (NT > 64 || team == 0) {
+        if (team == 0) {
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 const int c = (v * NT + tid) * 8;
@@ -503,14 +528,21 @@ bool with_team(int64_t D, F &&f) {
            : D <= 16384 ? with_team_of<1024, 2>(f)
                         : false;
 }
-// The gradient's, which holds three rows, the weight and its gradient's sums.
-template <typename F>
+// The gradient's, which holds three rows, the weight and its gradient's sums: f(threads, groups, teams of a
+// workgroup).
+template <int NT, int NV, int TEAMS, typename F>
+bool with_teams_of(F &&f) {
+    f(std::integral_constant<int, NT>(), std::integral_constant<int, NV>(), std::integral_constant<int, TEAMS>());
+    return true;
+}
+template <bool CENTER, typename F>
 bool with_backward_team(int64_t D, F &&f) {
-    return D <= 512    ? with_team_of<64, 1>(f)
-           : D <= 1024 ? with_team_of<64, 2>(f)
-           : D <= 2048 ? with_team_of<256, 1>(f)
-           : D <= 4096 ? with_team_of<256, 2>(f)
-           : D <= 8192 ? with_team_of<1024, 1>(f)
+    constexpr bool C = CENTER;
+    return D <= 512    ? with_teams_of<64, 1, C ? 16 : 4>(f)
+           : D <= 1024 ? with_teams_of<C ? 128 : 64, C ? 1 : 2, C ? 8 : 4>(f)
+           : D <= 2048 ? with_teams_of<256, 1, C ? 4 : 1>(f)
+           : D <= 4096 ? with_teams_of<C ? 512 : 256, C ? 1 : 2, C ? 2 : 1>(f)
+           : D <= 8192 ? with_teams_of<1024, 1, 1>(f)
                        : false;
 }
 
@@ -518,14 +550,19 @@ bool with_backward_team(int64_t D, F &&f) {
 
 // Workgroups of the gradient's kernel: as many as its registers let the CUs hold,
 // up to four each (8191x2048 with two 44.5 us, the rows in flight too few).
-int norm_backward_slabs(int64_t T, int64_t D) {
+// (CENTER, of two sums a column: teams share a workgroup, whose sums are one row.)
+template <bool CENTER>
+static int backward_slabs(int64_t T, int64_t D) {
     int64_t groups = T, most = 512;
-    with_backward_team(D, [&](auto nt, auto nv) {
-        groups = (T + RowTeam<nt()>::ROWS - 1) / RowTeam<nt()>::ROWS;
+    with_backward_team<CENTER>(D, [&](auto nt, auto nv, auto teams) {
+        groups = (T + teams() - 1) / teams();
         most = nt() == 1024 ? 256 : nv() > 1 ? 768 : 1024;
+        if (CENTER) most = 256;
     });
     return (int)(groups < most ? groups : most);
 }
+int norm_backward_slabs(int64_t T, int64_t D) { return backward_slabs<false>(T, D); }
+int layernorm_backward_slabs(int64_t T, int64_t D) { return backward_slabs<true>(T, D); }
 
 xtc_status launch_column_sums(const float *partial, int slabs, int D, float *DW, float *DB, hipStream_t s) {
     const int64_t columns = DB ? 2 * (int64_t)D : D;
@@ -537,7 +574,7 @@ namespace {
 
 template <bool CENTER>
 xtc_status launch_norm(const NormArgs &a, xtc_dtype dtype, bool quantize, hipStream_t s) {
-    const bool done = with_team(a.D, [&](auto nt, auto nv) {
+    auto run = [&](auto nt, auto nv) {
         constexpr int NT = nt(), NV = nv();
         const auto kernel = dtype == XTC_F32 ? (quantize ? norm_kernel<float, true, CENTER, NT, NV> : norm_kernel<float, false, CENTER, NT, NV>)
                                              : (quantize ? norm_kernel<Bf16, true, CENTER, NT, NV> : norm_kernel<Bf16, false, CENTER, NT, NV>);
@@ -558,7 +595,8 @@ xtc_status launch_norm(const NormArgs &a, xtc_dtype dtype, bool quantize, hipStr
             b.mean = static_cast<float *>(on(a.mean, t0 * 4));
             kernel<<<(unsigned)((b.T + ROWS - 1) / ROWS), RowTeam<NT>::THREADS, 0, s>>>(b);
         }
-    });
+    };
+    const bool done = with_team(a.D, run);
     if (!done) {
         const auto kernel = dtype == XTC_F32 ? (quantize ? norm_loop_kernel<float, true, CENTER> : norm_loop_kernel<float, false, CENTER>)
                                              : (quantize ? norm_loop_kernel<Bf16, true, CENTER> : norm_loop_kernel<Bf16, false, CENTER>);
@@ -569,12 +607,12 @@ xtc_status launch_norm(const NormArgs &a, xtc_dtype dtype, bool quantize, hipStr
 
 template <bool CENTER>
 xtc_status launch_norm_backward(const NormBackwardArgs &a, xtc_dtype dtype, hipStream_t s) {
-    const int slabs = norm_backward_slabs(a.T, a.D);
+    const int slabs = backward_slabs<CENTER>(a.T, a.D);
     if (a.T > 0) {
-        const bool done = with_backward_team(a.D, [&](auto nt, auto nv) {
-            constexpr int NT = nt(), NV = nv();
-            const auto kernel = dtype == XTC_F32 ? norm_backward_kernel<float, CENTER, NT, NV> : norm_backward_kernel<Bf16, CENTER, NT, NV>;
-            kernel<<<(unsigned)slabs, RowTeam<NT>::THREADS, 0, s>>>(a);
+        const bool done = with_backward_team<CENTER>(a.D, [&](auto nt, auto nv, auto teams) {
+            constexpr int NT = nt(), NV = nv(), TEAMS = teams();
+            const auto kernel = dtype == XTC_F32 ? norm_backward_kernel<float, CENTER, NT, NV, TEAMS> : norm_backward_kernel<Bf16, CENTER, NT, NV, TEAMS>;
+            kernel<<<(unsigned)slabs, NT * TEAMS, 0, s>>>(a);
         });
         if (!done) {
             const auto dx = dtype == XTC_F32 ? norm_dx_kernel<float, CENTER> : norm_dx_kernel<Bf16, CENTER>;
@@ -597,7 +635,9 @@ xtc_status launch_layernorm(const NormArgs &a, xtc_dtype dtype, bool quantize, h
 xtc_status launch_rmsnorm_backward(const NormBackwardArgs &a, xtc_dtype dtype, hipStream_t s) {
     return launch_norm_backward<false>(a, dtype, s);
 }
-xtc_status launch_layernorm_backward(const NormBackwardArgs &a, xtc_dtype dtype, hipStream_t s) {
+xtc_status launch_layernorm_backward(const NormBackwardArgs &given, xtc_dtype dtype, hipStream_t s) {
+    NormBackwardArgs a = given;
+    a.past = whole_lines(a.DX, a.lddx, dtype == XTC_F32 ? 4 : 2);
     return launch_norm_backward<true>(a, dtype, s);
 }
 

@@ -52,9 +52,10 @@ struct NormBackwardArgs {
     void *DX;
     int64_t lddx;
     float *DW;
-    float *partial;     // norm_backward_slabs(T) x D (layer norm: 2D) sums of a slab of rows each
+    float *partial;     // norm_backward_slabs() x D (layer norm: layernorm_backward_slabs() x 2D) sums of a slab of rows each
     const float *mean;  // layer norm
     float *DB;
+    int past;           // layer norm: DX's rows begin at 16 bytes
 };
 
 struct QuantArgs {
@@ -117,6 +118,7 @@ struct ActivationArgs {
     int act;
     void *DZ;           // bf16
     int64_t lddz;
+    int past;           // DZ's rows begin at 16 bytes
     float *DB;          // column sums of the unrounded DZ (null: not wanted)
     float *partial;     // activation_slabs() x N sums of a slab of rows each
 };
@@ -176,6 +178,7 @@ struct CombineBackwardArgs {
     const float *P;
     void *DROWS;
     int64_t lddr;
+    int past;               // DROWS' rows begin at 16 bytes
     float *DP;
 };
 
@@ -183,6 +186,7 @@ struct CombineBackwardArgs {
 constexpr int64_t kMostGroups = int64_t(1) << 24;
 
 int norm_backward_slabs(int64_t T, int64_t D);
+int layernorm_backward_slabs(int64_t T, int64_t D);
 xtc_status launch_rmsnorm(const NormArgs &a, xtc_dtype dtype, bool quantize, hipStream_t s);
 xtc_status launch_rmsnorm_backward(const NormBackwardArgs &a, xtc_dtype dtype, hipStream_t s);
 xtc_status launch_layernorm(const NormArgs &a, xtc_dtype dtype, bool quantize, hipStream_t s);

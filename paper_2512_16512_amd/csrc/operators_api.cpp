@@ -112,7 +112,7 @@ xtc_status xtc_layernorm(int64_t T, int64_t D, const void *X, int64_t ldx, const
 
 int64_t xtc_layernorm_backward_workspace(int64_t T, int64_t D) {
     if (T < 0 || D < 0 || T > kMostExtent || D > kMostExtent) return -1;
-    return 8 * norm_backward_slabs(T, D) * D;
+    return 8 * layernorm_backward_slabs(T, D) * D;
 }
 
 xtc_status xtc_layernorm_backward(int64_t T, int64_t D, const void *DY, int64_t lddy, const void *X, int64_t ldx,

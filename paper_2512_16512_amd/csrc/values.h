@@ -73,6 +73,55 @@ __device__ __forceinline__ void store8(T *p, int valid, const float (&v)[8]) {
     }
 }
 
+// store8 and raw8 of values that nothing reads (or read) soon: past the caches.
+template <typename T>
+__device__ __forceinline__ void store8_past(T *p, int valid, const float (&v)[8]) {
+    typedef unsigned u32x4s __attribute__((ext_vector_type(4), aligned(2)));
+    T t[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) narrow(v[i], &t[i]);
+    if (valid >= 8) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(t) / 16; ++i) {
+            u32x4s q;
+            __builtin_memcpy(&q, reinterpret_cast<unsigned char *>(t) + 16 * i, 16);
+            __builtin_nontemporal_store(q, reinterpret_cast<u32x4s *>(p) + i);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < valid) p[i] = t[i];
+    }
+}
+// Whether rows begin at 16 bytes: whole lines leave past the caches, pieces of lines had better meet there.
+inline bool whole_lines(const void *p, int64_t ld, int64_t bytes) {
+    return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * bytes % 16 == 0;
+}
+template <typename T>
+__device__ __forceinline__ void store8_to(T *p, int valid, const float (&v)[8], int past) {
+    if (past) store8_past(p, valid, v);
+    else store8(p, valid, v);
+}
+template <typename T>
+__device__ __forceinline__ Raw8<T> raw8_once(const T *p, int valid) {
+    typedef unsigned u32x4s __attribute__((ext_vector_type(4), aligned(2)));
+    Raw8<T> r;
+    if (valid >= 8) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(r.v) / 16; ++i) {
+            const u32x4s q = __builtin_nontemporal_load(reinterpret_cast<const u32x4s *>(p) + i);
+            __builtin_memcpy(reinterpret_cast<unsigned char *>(r.v) + 16 * i, &q, 16);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            r.v[i] = T{};
+            if (i < valid) r.v[i] = p[i];
+        }
+    }
+    return r;
+}
+
 constexpr float kFp8Most = 448.f;                 // largest e4m3 value
 constexpr float kFp8Tiny = 1.17549435e-38f;       // least scale: 2^-126, whose reciprocal is finite
 
