@@ -566,8 +566,8 @@ xtc_status xtc_matmul_grouped_fp8(int64_t G, int64_t T, int64_t N, int64_t K,
  *  loss       one fp32: the balance loss E / (top n^2) sum_e counts_e sum_t q_te, q the
  *             softmax over all experts (0 for a row of -inf), n the tokens that are not
  *             masked; 0 without any.  It is 1 where all experts are chosen equally.
- *  workspace  xtc_route_experts_workspace(T, E) bytes, 16-byte aligned, written by the
- *             call; too small is XTC_ERR_BAD_SHAPE.
+ *  workspace  xtc_route_experts_workspace(T, E) bytes (0 for few tokens: NULL is fine
+ *             then), 16-byte aligned, written by the call; too small is XTC_ERR_BAD_SHAPE.
  * All arrays but scores are contiguous.  Outputs are the same bits in every call.  With
  * T 0 counts, ends and loss are zeros.  Errors as for xtc_rmsnorm.
  */

@@ -245,6 +245,33 @@ xtc_status launch_linear(const LinearArgs &a, bool b_rows_n, void *workspace, hi
 int64_t linear_wgrad_workspace(const LinearArgs &a) { return workspace<kWgrad>(a); }
 xtc_status launch_linear_wgrad(const LinearArgs &a, void *workspace, hipStream_t s) { return launch<kWgrad>(a, workspace, s); }
 
+namespace {
+
+template <Kind KIND>
+int kernel_place(const LinearArgs &a, int *kernels, int *splits) {
+    const Plan w = plan<KIND>(a);
+    int count = 0;
+    linear_tile_choices<KIND>(kernels);
+    if constexpr (KIND != kWgrad) {
+        linear_stream_choices<KIND>(&count);
+        *kernels += count;
+    }
+    if (!(aligned_rows(a.A, a.lda) && aligned_rows(a.B, a.ldb) && (KIND == kWgrad || a.K % 8 == 0))) {
+        linear_any_choices<KIND>(&count);
+        *kernels += count;
+    }
+    *splits = w.splits;
+    return w.place;
+}
+
+}  // namespace
+
+int linear_kernel(const LinearArgs &a, int kind, int *kernels, int *splits) {
+    return kind == kBf16N   ? kernel_place<kBf16N>(a, kernels, splits)
+           : kind == kBf16T ? kernel_place<kBf16T>(a, kernels, splits)
+                            : kernel_place<kWgrad>(a, kernels, splits);
+}
+
 int activation_slabs(int64_t T, int64_t N) {
     const int64_t across = cdiv(N, kSlopeColumns), rows = cdiv(T, kSlopeWaves), most = across < 2048 ? 2048 / across : 1;
     return (int)(rows < most ? (rows > 1 ? rows : 1) : most);

@@ -28,13 +28,12 @@ const LinearChoice *linear_tile_choices(int *count) {
         static const LinearChoice all[] = {
             {256, 256, 1, N ? 1.44f : 1.34f, N ? 1.44f : 1.34f, 11.8f, N ? .64f : .74f, kLaunch<KIND, 256, 256, 128, 64, 2, 128>},
             {256, 128, 1, N ? .76f : .74f, N ? .76f : .74f, N ? 8.2f : 8.f, .78f, kLaunch<KIND, 256, 128, 64, 64, 3, 128>},
-            {128, 256, 1, N ? .76f : .73f, N ? .76f : .73f, N ? 8.5f : 8.4f, .78f, kLaunch<KIND, 128, 256, 64, 64, 3, 128>},
             {128, 128, 2, N ? .7f : .63f, N ? .89f : .85f, 7.3f, .73f, kLaunch<KIND, 128, 128, 64, 64, 2, 128>},
             {128, 128, 1, N ? .44f : .42f, N ? .44f : .42f, N ? 6.6f : 6.1f, .88f, kLaunch<KIND, 128, 128, 64, 32, 4, 128>},
             {64, 128, 1, N ? .35f : .29f, N ? .35f : .29f, 5.1f, 1, kLaunch<KIND, 64, 128, 64, 16, 4, 128>},
             {64, 64, 2, N ? .28f : .25f, N ? .39f : .37f, N ? 4.9f : 4.6f, .75f, kLaunch<KIND, 64, 64, 64, 16, 4, 128>},
         };
-        *count = 7;
+        *count = 6;
         return all;
     }
 }
@@ -46,20 +45,18 @@ template <Kind KIND>
 const LinearChoice *linear_any_choices(int *count) {
     if constexpr (KIND == kWgrad) {
         static const LinearChoice all[] = {
-            {128, 128, 2, 1.3f, 2.f, 14.f, 1, kLaunch<KIND, 128, 128, 64, 64, 2, 128, true>},
             {64, 128, 2, 1.15f, 1.33f, 8.7f, .5f, kLaunch<KIND, 64, 128, 64, 32, 2, 128, true>},
             {64, 64, 2, .9f, 1.f, 4.4f, .74f, kLaunch<KIND, 64, 64, 64, 16, 2, 128, true>},
         };
-        *count = 3;
+        *count = 2;
         return all;
     } else {
         constexpr bool N = KIND == kBf16N;
         static const LinearChoice all[] = {
-            {128, 128, 2, N ? 1.6f : 1.43f, 1.9f, 10.4f, .5f, kLaunch<KIND, 128, 128, 64, 64, 2, 128, true>},
             {64, 128, 1, N ? .97f : .82f, N ? .97f : .82f, N ? 4.4f : 5.7f, N ? 1.f : .64f, kLaunch<KIND, 64, 128, 64, 16, 2, 128, true>},
             {64, 64, 2, N ? 1.03f : .7f, N ? 1.03f : .91f, 6.1f, .45f, kLaunch<KIND, 64, 64, 64, 16, 2, 128, true>},
         };
-        *count = 3;
+        *count = 2;
         return all;
     }
 }

@@ -136,7 +136,7 @@ struct RouteArgs {
     int32_t *counts, *ends; // E
     float *loss;
     int each;               // tokens of a workgroup
-    int32_t *counts_of;     // of each workgroup: E counts, E sums
+    int32_t *counts_of;     // of each workgroup: E counts and E sums, in whole fours
     float *sums_of;
 };
 
@@ -216,6 +216,10 @@ xtc_status launch_route(const RouteArgs &a, xtc_dtype dtype, void *workspace, hi
 xtc_status launch_route_backward(const RouteBackwardArgs &a, xtc_dtype dtype, xtc_dtype out_dtype, hipStream_t s);
 xtc_status launch_combine(const CombineArgs &a, xtc_dtype dtype, xtc_dtype r_dtype, xtc_dtype out_dtype, hipStream_t s);
 xtc_status launch_combine_backward(const CombineBackwardArgs &a, xtc_dtype dtype, xtc_dtype g_dtype, hipStream_t s);
+
+// The same of a linear layer (1, 2) or its weights' gradient (3): those for rows at any address come first where
+// an operand has such, the others then follow (they run on copies).
+int linear_kernel(const LinearArgs &a, int kind, int *kernels, int *splits);
 
 // Which of the kernels for aligned rows a product takes (-1: the one for rows at
 // any address), and how many there are.  kind: 0 e4m3, 1 bf16 with B [K, N], 2 with

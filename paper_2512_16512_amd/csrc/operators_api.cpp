@@ -377,13 +377,14 @@ xtc_status xtc_route_experts(int64_t T, int64_t E, int64_t top, const void *scor
     if (st != XTC_OK) return st;
     if (lds > kMostStride) return XTC_ERR_TOO_LARGE;
     if (lds < E) return XTC_ERR_BAD_LEADING_DIM;
-    if (!counts || !ends || !loss || !workspace || (T > 0 && (!scores || !expert || !p || !row || !token)))
+    const int64_t need = xtc_route_experts_workspace(T, E);
+    if (!counts || !ends || !loss || (need > 0 && !workspace) || (T > 0 && (!scores || !expert || !p || !row || !token)))
         return XTC_ERR_NULL_POINTER;
     if (!aligned_to(scores, size_of(dtype)) || !aligned_to(expert, 4) || !aligned_to(p, 4) || !aligned_to(row, 4) ||
         !aligned_to(token, 4) || !aligned_to(counts, 4) || !aligned_to(ends, 4) || !aligned_to(loss, 4) ||
         !aligned_to(workspace, 16))
         return XTC_ERR_MISALIGNED;
-    if (workspace_bytes < xtc_route_experts_workspace(T, E)) return XTC_ERR_BAD_SHAPE;
+    if (workspace_bytes < need) return XTC_ERR_BAD_SHAPE;
     RouteArgs a = {};
     a.T = T; a.E = (int)E; a.top = (int)top;
     a.scores = scores; a.lds = lds; a.mask = mask;
@@ -471,6 +472,17 @@ int32_t xtc_test_product_kernel(int32_t kind, int32_t grouped, int64_t G, int64_
     a.ends = grouped ? &ends : nullptr; a.G = (int)G;
     a.out_bf16 = out_bf16;
     return grouped_kernel(a, kind, kernels);
+}
+
+// Not part of the ABI, as above: of a linear layer (kind 1, 2) or its weights' gradient (3) on contiguous
+// operands that begin `off` elements behind 16 bytes.
+int32_t xtc_test_linear_kernel(int32_t kind, int64_t T, int64_t N, int64_t K, int32_t off, int32_t *kernels,
+                               int32_t *splits) {
+    LinearArgs a = {};
+    a.T = T; a.N = (int)N; a.K = (int)K;
+    a.A = a.B = reinterpret_cast<const void *>((uintptr_t)off * 2);
+    a.lda = K; a.ldb = kind == 2 ? K : N;
+    return linear_kernel(a, kind, kernels, splits);
 }
 
 }  // extern "C"

@@ -22,7 +22,7 @@
 namespace xtc {
 namespace {
 
-constexpr int kThreads = 256, kPlaceThreads = 1024, kGroup = 64;   // tokens whose bits fill a word
+constexpr int kThreads = 256, kManyThreads = 1024, kGroup = 64;   // tokens whose bits fill a word
 
 // The value of the lane N places on, around the 16 (N 8, 4, 2, 1) or 64 (N 16, 32) that share a token.
 template <int N>
@@ -87,22 +87,32 @@ __device__ __forceinline__ void softmax(const float (&v)[VPT], float most, float
     for (int i = 0; i < VPT; ++i) q[i] = most == -__builtin_inff() ? 0.f : q[i] * inv;
 }
 
-// Tokens t0 .. t0 + p.each - 1: their experts and weights, their rows' places among the workgroup's
-// (into p.row), its counts (E, one after the other) and sums of q.
-template <typename T, int LANES, int VPT>
-__device__ __forceinline__ void choose(const RouteArgs &p, int block, unsigned char *smem) {
-    constexpr int TEAMS = kThreads / LANES, EACH = kGroup / TEAMS;
+// What the first half of the work leaves for the second: in memory, or in LDS where one workgroup does both.
+struct Halfway {
+    int32_t *counts;     // a row of E in whole fours for each workgroup, likewise the sums of q
+    float *sums;
+    int32_t *expert;     // of each choice of the tokens from `first` on, and its place among the workgroup's
+    int32_t *rank;
+    int64_t first;
+};
+__device__ __forceinline__ int fours(int E) { return (E + 3) & ~3; }
+
+// Tokens t0 .. t0 + p.each - 1: their experts and weights, their rows' places among the workgroup's, its counts
+// and sums of q.
+template <typename T, int LANES, int VPT, int THREADS, bool SMALL>
+__device__ __forceinline__ void choose(const RouteArgs &p, const Halfway &h, int block, unsigned char *smem) {
+    constexpr int TEAMS = THREADS / LANES, EACH = kGroup / TEAMS, WAVES = THREADS / 64;
     const int E = p.E, top = p.top, tid = threadIdx.x, team = tid / LANES, lane = tid % LANES, e0 = lane * VPT;
     unsigned long long *bits = reinterpret_cast<unsigned long long *>(smem);
     int *before = reinterpret_cast<int *>(bits + E);
-    float *sums = reinterpret_cast<float *>(before + E);                    // TEAMS x E
-    for (int e = tid; e < E; e += kThreads) before[e] = 0;
+    float *sums = reinterpret_cast<float *>(before + E);                    // WAVES x E
+    for (int e = tid; e < E; e += THREADS) before[e] = 0;
     float total[VPT];
 #pragma unroll
     for (int i = 0; i < VPT; ++i) total[i] = 0.f;
     const int64_t first = (int64_t)block * p.each, end = first + p.each < p.T ? first + p.each : p.T;
     for (int64_t t0 = first; t0 < end; t0 += kGroup) {
-        for (int e = tid; e < E; e += kThreads) bits[e] = 0;
+        for (int e = tid; e < E; e += THREADS) bits[e] = 0;
         __syncthreads();
         int mine[EACH];              // lane j: the expert of choice j (-1: none)
 #pragma unroll
@@ -139,6 +149,7 @@ __device__ __forceinline__ void choose(const RouteArgs &p, int block, unsigned c
                 const float sum = team_sum<LANES>(w);
                 if (lane < top) {
                     p.expert[t * top + lane] = mine[r];
+                    if constexpr (SMALL) h.expert[(t - h.first) * top + lane] = mine[r];
                     p.p[t * top + lane] = most == -__builtin_inff() ? 0.f : w / sum;
                     atomicOr(&bits[mine[r]], 1ull << at);      // (whichever comes first)
                 }
@@ -147,6 +158,7 @@ __device__ __forceinline__ void choose(const RouteArgs &p, int block, unsigned c
                 for (int i = 0; i < VPT; ++i) total[i] += q[i];
             } else if (t < end && lane < top) {
                 p.expert[t * top + lane] = -1;
+                if constexpr (SMALL) h.expert[(t - h.first) * top + lane] = -1;
                 p.p[t * top + lane] = 0.f;
             }
         }
@@ -156,68 +168,88 @@ __device__ __forceinline__ void choose(const RouteArgs &p, int block, unsigned c
             const int at = r * TEAMS + team;
             const int64_t t = t0 + at;
             if (t < end && lane < top)
-                p.row[t * top + lane] = mine[r] < 0 ? -1 : before[mine[r]] + __popcll(bits[mine[r]] & ((1ull << at) - 1));
+                h.rank[(t - h.first) * top + lane] = mine[r] < 0 ? -1 : before[mine[r]] + __popcll(bits[mine[r]] & ((1ull << at) - 1));
         }
         __syncthreads();
-        for (int e = tid; e < E; e += kThreads) before[e] += __popcll(bits[e]);
+        for (int e = tid; e < E; e += THREADS) before[e] += __popcll(bits[e]);
     }
+    // a wave's teams, then the waves
 #pragma unroll
-    for (int i = 0; i < VPT; ++i)
-        if (e0 + i < E) sums[team * E + e0 + i] = total[i];
+    for (int i = 0; i < VPT; ++i) {
+#pragma unroll
+        for (int d = LANES; d < 64; d *= 2) total[i] += __shfl_xor(total[i], d, 64);
+        if (tid % 64 < LANES && e0 + i < E) sums[tid / 64 * E + e0 + i] = total[i];
+    }
     __syncthreads();
-    for (int e = tid; e < E; e += kThreads) {
+    for (int e = tid; e < E; e += THREADS) {
         float s = 0.f;
 #pragma unroll
-        for (int i = 0; i < TEAMS; ++i) s += sums[i * E + e];
-        p.counts_of[(int64_t)block * E + e] = before[e];
-        p.sums_of[(int64_t)block * E + e] = s;
+        for (int i = 0; i < WAVES; ++i) s += sums[i * E + e];
+        h.counts[block * fours(E) + e] = before[e];
+        h.sums[block * fours(E) + e] = s;
     }
 }
 
-// The places of a workgroup's rows: those of all lower experts, of this expert in the workgroups before,
-// and the place among its own.  Workgroup 0 also writes what there is once.
+// What there is once (block == blocks), or the places of a workgroup's rows: those of all lower experts, of
+// this expert in the workgroups before, and the place among its own.
 template <int THREADS>
-__device__ __forceinline__ void place(const RouteArgs &p, int block, int blocks, unsigned char *smem) {
+__device__ __forceinline__ void place(const RouteArgs &p, const Halfway &h, int block, int blocks, bool once, bool rows_of, unsigned char *smem) {
     const int E = p.E, top = p.top, tid = threadIdx.x;
     int *start = reinterpret_cast<int *>(smem);          // of this workgroup's rows of each expert
     int *all = start + E;                                // rows of each expert, then up to and with it
-    int *part = all + E;                                 // 2 x THREADS
-    float *fpart = reinterpret_cast<float *>(part + 2 * THREADS);     // THREADS
-    // E threads read one workgroup's counts: the threads take the workgroups in turn, THREADS / E at once
-    const int width = E < THREADS ? E : THREADS, turns = THREADS / width;
-    for (int e0 = 0; e0 < E; e0 += width) {
-        const int e = e0 + tid % width, turn = tid / width;
-        int sum = 0, mine = 0;
-        float s = 0.f;
-        if (turn < turns && e < E) {
-#pragma unroll 4
-            for (int b = turn; b < blocks; b += turns) {
-                const int c = p.counts_of[(int64_t)b * E + e];
-                sum += c;
-                mine += b < block ? c : 0;
-                if (block == 0) s += p.sums_of[(int64_t)b * E + e];
+    float *part = reinterpret_cast<float *>(all + E);    // 4 x THREADS, and a value a wave
+    for (int e = tid; e < E; e += THREADS) start[e] = all[e] = 0;
+    __syncthreads();
+    // the workgroups' counts, four experts a load, the threads taking the workgroups in turn; whole numbers,
+    // whose sums do not depend on the order
+    const int width = fours(E) / 4, turns = THREADS / width, g = tid % width, turn = tid / width;
+    if (turn < turns) {
+        int sum[4] = {0, 0, 0, 0}, mine[4] = {0, 0, 0, 0};
+        float q[4] = {0.f, 0.f, 0.f, 0.f};
+        constexpr int AT_ONCE = 8;       // loads on their way together
+        for (int b0 = turn; b0 < blocks; b0 += AT_ONCE * turns) {
+            int c[AT_ONCE][4];
+            float f[AT_ONCE][4];
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) {
+                const int b = b0 + k * turns, at = ((b < blocks ? b : turn) * width + g) * 4;
+                __builtin_memcpy(c[k], __builtin_assume_aligned(h.counts + at, 16), 16);
+                if (once) __builtin_memcpy(f[k], __builtin_assume_aligned(h.sums + at, 16), 16);
+            }
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) {
+                const int b = b0 + k * turns;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    sum[i] += b < blocks ? c[k][i] : 0;
+                    mine[i] += b < block && b < blocks ? c[k][i] : 0;
+                    if (once) q[i] += b < blocks ? f[k][i] : 0.f;
+                }
             }
         }
-        __syncthreads();
-        part[tid] = sum;
-        part[THREADS + tid] = mine;
-        fpart[tid] = s;
-        __syncthreads();
-        if (tid < width && e < E) {
-            for (int i = 1; i < turns; ++i) {
-                sum += part[tid + i * width];
-                mine += part[THREADS + tid + i * width];
-                s += fpart[tid + i * width];
-            }
-            all[e] = sum;
-            start[e] = mine;
-            if (block == 0) {
-                p.counts[e] = sum;
-                p.sums_of[e] = (float)sum * s;           // (this workgroup alone reads it)
-            }
+        if (once) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) part[(turn * width + g) * 4 + i] = q[i];
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (g * 4 + i < E) {
+                atomicAdd(&all[g * 4 + i], sum[i]);
+                if (rows_of) atomicAdd(&start[g * 4 + i], mine[i]);
+            }
     }
     __syncthreads();
+    float weighed = 0.f;         // counts times sums of q, the latter over the turns in their order
+    if (once) {
+        for (int e = tid; e < E; e += THREADS) {
+            float q = 0.f;
+            for (int i = 0; i < turns; ++i) q += part[i * width * 4 + e];
+            weighed += (float)all[e] * q;
+        }
+        weighed = lanes_sum<64>(weighed);
+        if ((tid & 63) == 0) part[4 * THREADS + tid / 64] = weighed;
+        __syncthreads();
+    }
     // rows up to and with each expert: a wave at a time, 64 experts a step
     if (tid < 64) {
         int before = 0;
@@ -232,56 +264,69 @@ __device__ __forceinline__ void place(const RouteArgs &p, int block, int blocks,
             v += before;
             if (e < E) {
                 start[e] += v - all[e];
+                if (once) {
+                    p.counts[e] = all[e];
+                    p.ends[e] = v;
+                }
                 all[e] = v;
-                if (block == 0) p.ends[e] = v;
             }
             before = __shfl(v, 63, 64);
         }
     }
     __syncthreads();
-    const int rows = E > 0 ? all[E - 1] : 0;
-    if (block == 0 && tid < 64) {
+    const int rows = all[E - 1];
+    if (once && tid == 0) {
         float s = 0.f;
-        for (int e = tid; e < E; e += 64) s += p.sums_of[e];
-        s = lanes_sum<64>(s);
+#pragma unroll
+        for (int i = 0; i < THREADS / 64; ++i) s += part[4 * THREADS + i];
         const float n = (float)(rows / top > 1 ? rows / top : 1);
-        if (tid == 0) *p.loss = rows > 0 ? (float)E / ((float)top * n) * (s / n) : 0.f;
+        *p.loss = rows > 0 ? (float)E / ((float)top * n) * (s / n) : 0.f;
     }
+    if (!rows_of) return;
     const int64_t first = (int64_t)block * p.each * top, end = (first + (int64_t)p.each * top < p.T * top ? first + (int64_t)p.each * top : p.T * top);
     for (int64_t i = first + tid; i < end; i += THREADS) {
-        const int e = p.expert[i];
+        const int64_t at_half = i - h.first * top;
+        const int e = h.expert[at_half];
+        int at = -1;
         if (e >= 0) {
-            const int at = start[e] + p.row[i];
-            p.row[i] = at;
-            p.token[at] = (int32_t)(i / top);
+            at = start[e] + h.rank[at_half];
+            p.token[at] = (int32_t)((unsigned)i / (unsigned)top);      // (T top rows fit 31 bits)
         }
+        p.row[i] = at;
         if (i >= rows) p.token[i] = -1;
     }
 }
 
-size_t choose_bytes(int E, int lanes) { return (size_t)E * 12 + (size_t)(kThreads / lanes) * E * 4; }
-template <int THREADS>
-size_t place_bytes(int E) { return (size_t)E * 8 + (size_t)THREADS * 12; }
+size_t choose_bytes(int E, int threads) { return (size_t)E * 12 + (size_t)(threads / 64) * E * 4; }
+size_t place_bytes(int E, int threads) { return (size_t)E * 8 + (size_t)threads * 17; }
+
+__device__ __forceinline__ Halfway in_memory(const RouteArgs &p) { return Halfway{p.counts_of, p.sums_of, p.expert, p.row, 0}; }
 
 template <typename T, int LANES, int VPT>
-__global__ void __launch_bounds__(kThreads) route_choose_kernel(RouteArgs p) {
+__global__ void __launch_bounds__(kManyThreads) route_choose_kernel(RouteArgs p) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    choose<T, LANES, VPT>(p, blockIdx.x, smem);
+    choose<T, LANES, VPT, kManyThreads, false>(p, in_memory(p), blockIdx.x, smem);
 }
 
-__global__ void __launch_bounds__(kPlaceThreads) route_place_kernel(RouteArgs p, int blocks) {
+// (one workgroup more than route_choose_kernel's)
+__global__ void __launch_bounds__(kManyThreads) route_place_kernel(RouteArgs p, int blocks) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    place<kPlaceThreads>(p, blockIdx.x, blocks, smem);
+    const int block = blockIdx.x;
+    place<kManyThreads>(p, in_memory(p), block, blocks, block == blocks, block < blocks, smem);
 }
 
-// The few tokens of one workgroup, in one launch.
+// The few tokens of one workgroup, in one launch; what lies halfway stays in LDS.
+constexpr int kMostChoices = 16;
 template <typename T, int LANES, int VPT>
 __global__ void __launch_bounds__(kThreads) route_small_kernel(RouteArgs p) {
+    __shared__ __attribute__((aligned(16))) int32_t counts[LANES * VPT];
+    __shared__ __attribute__((aligned(16))) float sums[LANES * VPT];
+    __shared__ int32_t expert[kGroup * kMostChoices], rank[kGroup * kMostChoices];
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    choose<T, LANES, VPT>(p, 0, smem);
-    __threadfence_block();
+    const Halfway h = {counts, sums, expert, rank, 0};
+    choose<T, LANES, VPT, kThreads, true>(p, h, 0, smem);
     __syncthreads();
-    place<kThreads>(p, 0, 1, smem);
+    place<kThreads>(p, h, 0, 1, true, true, smem);
 }
 
 // ds of the tokens blockIdx.x, + gridDim.x, ... of each team.
@@ -361,24 +406,24 @@ int blocks_of(int64_t T) { return T > 0 ? (int)((T + each_of(T) - 1) / each_of(T
 
 }  // namespace
 
-int64_t route_workspace(int64_t T, int64_t E) { return (int64_t)blocks_of(T) * E * 8; }
+int64_t route_workspace(int64_t T, int64_t E) { return blocks_of(T) > 1 ? (int64_t)blocks_of(T) * ((E + 3) / 4 * 4) * 8 : 0; }
 
 xtc_status launch_route(const RouteArgs &given, xtc_dtype dtype, void *workspace, hipStream_t s) {
     RouteArgs a = given;
     const int blocks = blocks_of(a.T);
     a.each = a.T > 0 ? (int)each_of(a.T) : kGroup;
     a.counts_of = static_cast<int32_t *>(workspace);
-    a.sums_of = reinterpret_cast<float *>(a.counts_of + (int64_t)blocks * a.E);
+    a.sums_of = workspace ? reinterpret_cast<float *>(a.counts_of + (int64_t)blocks * ((a.E + 3) / 4 * 4)) : nullptr;
     with_lanes(a.E, [&](auto lanes, auto vpt) {
         constexpr int LANES = lanes(), VPT = vpt();
         if (blocks == 1) {
-            const size_t one = choose_bytes(a.E, LANES), two = place_bytes<kThreads>(a.E);
+            const size_t one = choose_bytes(a.E, kThreads), two = place_bytes(a.E, kThreads);
             const auto kernel = dtype == XTC_F32 ? route_small_kernel<float, LANES, VPT> : route_small_kernel<Bf16, LANES, VPT>;
             kernel<<<1, kThreads, one > two ? one : two, s>>>(a);
         } else {
             const auto kernel = dtype == XTC_F32 ? route_choose_kernel<float, LANES, VPT> : route_choose_kernel<Bf16, LANES, VPT>;
-            kernel<<<(unsigned)blocks, kThreads, choose_bytes(a.E, LANES), s>>>(a);
-            route_place_kernel<<<(unsigned)blocks, kPlaceThreads, place_bytes<kPlaceThreads>(a.E), s>>>(a, blocks);
+            kernel<<<(unsigned)blocks, kManyThreads, choose_bytes(a.E, kManyThreads), s>>>(a);
+            route_place_kernel<<<(unsigned)blocks + 1, kManyThreads, place_bytes(a.E, kManyThreads), s>>>(a, blocks);
         }
     });
     return hip_status(hipGetLastError());

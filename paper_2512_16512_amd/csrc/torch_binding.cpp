@@ -630,15 +630,33 @@ PyObject *route_experts(PyObject *, PyObject *const *args, Py_ssize_t n) {
         const c10::DeviceGuard on(s->device());
         const int64_t size = xtc_route_experts_workspace(T, E);
         if (size < 0) Py_RETURN_NONE;
-        at::Tensor r[7] = {fresh({T, top}, at::kInt, *s), fresh({T, top}, at::kFloat, *s), fresh({T, top}, at::kInt, *s),
-                           fresh({T * top}, at::kInt, *s), fresh({E}, at::kInt, *s), fresh({E}, at::kInt, *s),
-                           fresh({}, at::kFloat, *s)};
-        at::Tensor work = fresh({size}, at::kByte, *s);
+        // (one allocation for the results, each at a multiple of 64 bytes of it: eight cost more than the kernel)
+        int64_t at = 0;
+        auto place = [&](int64_t values) {
+            const int64_t here = at;
+            at += (values + 15) / 16 * 16;
+            return here;
+        };
+        const int64_t n_all = T * top, o_e = place(n_all), o_p = place(n_all), o_r = place(n_all), o_t = place(n_all),
+                      o_c = place(E), o_n = place(E), o_l = place(1);
+        const at::Tensor all = fresh({at}, at::kInt, *s);
+        auto part = [&](at::ScalarType type, at::IntArrayRef shape, int64_t offset) {
+            at::Tensor v = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(all.storage()), all.key_set(),
+                                                                    c10::scalarTypeToTypeMeta(type));
+            v.unsafeGetTensorImpl()->set_storage_offset(offset);
+            v.unsafeGetTensorImpl()->set_sizes_contiguous(shape);
+            return v;
+        };
+        at::Tensor r[7] = {part(at::kInt, {T, top}, o_e), part(at::kFloat, {T, top}, o_p), part(at::kInt, {T, top}, o_r),
+                           part(at::kInt, {n_all}, o_t),  part(at::kInt, {E}, o_c),        part(at::kInt, {E}, o_n),
+                           part(at::kFloat, {}, o_l)};
+        at::Tensor work;
+        if (size > 0) work = fresh({size}, at::kByte, *s);
         void *stream = stream_of(*s);
         if (unlocked(xtc_route_experts, T, E, (int64_t)top, static_cast<const void *>(s->data_ptr()), row_stride(*s),
                      static_cast<const uint8_t *>(data(mask)), as<int32_t>(r[0]), as<float>(r[1]), as<int32_t>(r[2]),
-                     as<int32_t>(r[3]), as<int32_t>(r[4]), as<int32_t>(r[5]), as<float>(r[6]), work.data_ptr(), size, dt,
-                     stream) != XTC_OK)
+                     as<int32_t>(r[3]), as<int32_t>(r[4]), as<int32_t>(r[5]), as<float>(r[6]),
+                     size > 0 ? work.data_ptr() : nullptr, size, dt, stream) != XTC_OK)
             Py_RETURN_NONE;
         return tuple_of(r);
     } catch (...) {

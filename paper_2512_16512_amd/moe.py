@@ -1,34 +1,62 @@
-"""A mixture-of-experts block on the norm, 8-bit and grouped operators: one step
-of serving in 8 bits and one of training in bfloat16, as a program would make
-them.
+"""A mixture-of-experts block on the norm, 8-bit, grouped, linear and routing operators: one
+step of serving in 8 bits and one of training in bfloat16, as a program would make them.
 
     h = x + residual,  y = rmsnorm(h),  scores = y @ router.T
     out[t] = sum over t's top experts e of  p[t, e] * relu(y[t] @ w1[e]) @ w2[e]
 
-``python -m paper_2512_16512_amd.moe`` runs both on random weights and prints
-what a step takes.  Routing (top-k, sorting the rows by expert) and the weighted
-sum over a token's experts are torch's.
+With a bias for the norm it is a layer norm.  The training step can train the router too (through the
+weights p and a balance loss) and can have an expert that every token passes, a dense pair of layers with
+biases and an activation:
+
+    out[t] += act(y[t] @ v1 + c1) @ v2 + c2
+
+``python -m paper_2512_16512_amd.moe`` runs these on random weights and prints what a step takes.
+Copying the rows to their experts (an indexing) is torch's.
 """
 from __future__ import annotations
 
 import argparse
 import time
+from collections import namedtuple
 
 import torch
 
-from . import (matmul_fp8, matmul_grouped, matmul_grouped_fp8, matmul_grouped_wgrad, quantize_fp8, rmsnorm,
-               rmsnorm_backward)
+from . import (Routing, activation_backward, combine_experts, combine_experts_backward, layernorm, layernorm_backward,
+               linear, linear_wgrad, matmul_fp8, matmul_grouped, matmul_grouped_fp8, matmul_grouped_wgrad, quantize_fp8,
+               rmsnorm, rmsnorm_backward, route_experts, route_experts_backward)
+
+MOST_EXPERTS, MOST_CHOSEN = 1024, 16      # what route_experts takes
+
+
+def _fits(t):
+    """Whether the operators take a matrix of values as it is."""
+    return t.is_cuda and t.dtype in (torch.float32, torch.bfloat16) and (t.shape[1] <= 1 or t.stride(1) == 1)
+
+
+def routing(scores, top):
+    """``route_experts``, or for more experts or choices than it takes the same from torch (without the loss)."""
+    T, E = scores.shape
+    if E <= MOST_EXPERTS and top <= MOST_CHOSEN and _fits(scores):
+        return route_experts(scores, top)
+    p, chosen = torch.topk(scores.float(), top)
+    p = torch.softmax(p, 1)
+    expert, which = torch.sort(chosen.flatten(), stable=True)
+    # (a count of each expert's rows would be a call that waits for the GPU)
+    ends = torch.searchsorted(expert, torch.arange(E, device=expert.device), right=True, out_int32=True)
+    row = torch.empty(T * top, dtype=torch.int32, device=expert.device)
+    row[which] = torch.arange(T * top, dtype=torch.int32, device=expert.device)
+    return Routing(chosen.int(), p, row.view(T, top), (which // top).int(), torch.diff(ends, prepend=ends.new_zeros(1)),
+                   ends, None)
 
 
 def route(scores, top):
     """The rows of a grouped product for each token's ``top`` experts: ``token`` (the token of each row, rows sorted
     by expert), ``ends`` (int32, for the operators), ``p`` (its weight) and ``which`` (its place in [T, top])."""
-    p, expert = torch.topk(scores.float(), top)
-    p = torch.softmax(p, 1)
-    expert, which = torch.sort(expert.flatten(), stable=True)
-    # (a count of each expert's rows would be a call that waits for the GPU)
-    ends = torch.searchsorted(expert, torch.arange(scores.shape[1], device=expert.device), right=True, out_int32=True)
-    return which // top, ends, p.flatten()[which], which
+    r = routing(scores, top)
+    row = r.row.flatten().long()
+    which = torch.empty_like(row)
+    which[row] = torch.arange(row.shape[0], device=row.device)
+    return r.token.long(), r.ends, r.p.flatten()[which], which
 
 
 def sum_experts(rows, which, T):
@@ -45,45 +73,84 @@ def quantize_family(w):
     return torch.stack([m.view(torch.uint8) for m in q]).view(torch.float8_e4m3fn), torch.stack(s)
 
 
-class Served:
-    """The block's weights in 8 bits: ``norm`` [D], ``router`` [E, D], ``w1`` [E, D, F], ``w2`` [E, F, D]."""
+def _normed(x, norm, bias, residual, quantize=False):
+    if bias is None:
+        return rmsnorm(x, norm, residual, quantize=quantize)
+    return layernorm(x, norm, bias, residual, quantize=quantize)
 
-    def __init__(self, norm, router, w1, w2, top=2):
-        self.norm, self.top = norm, top
+
+class Served:
+    """The block's weights in 8 bits: ``norm`` [D] (with ``bias`` [D] a layer norm's), ``router`` [E, D], ``w1``
+    [E, D, F], ``w2`` [E, F, D]."""
+
+    def __init__(self, norm, router, w1, w2, top=2, bias=None):
+        self.norm, self.bias, self.top = norm, bias, top
         self.router = quantize_fp8(router, block_rows=128)
         self.w1 = quantize_family(w1.transpose(1, 2).contiguous())
         self.w2 = quantize_family(w2.transpose(1, 2).contiguous())
 
     def step(self, x, residual):
         """(out [T, D] float32, the sum that was normed): any number of tokens, one among them."""
-        n = rmsnorm(x, self.norm, residual, quantize=True)
-        token, ends, p, which = route(matmul_fp8(n.out, n.scale, *self.router), self.top)
-        rows = n.out.view(torch.uint8)[token].view(torch.float8_e4m3fn)
-        h = matmul_grouped_fp8(rows, n.scale[token], *self.w1, ends, relu=True, dtype=torch.bfloat16)
-        y = matmul_grouped_fp8(*quantize_fp8(h), *self.w2, ends, dtype=torch.bfloat16)
-        return sum_experts(y.float() * p[:, None], which, x.shape[0]), n.residual
+        n = _normed(x, self.norm, self.bias, residual, quantize=True)
+        r = routing(matmul_fp8(n.out, n.scale, *self.router), self.top)
+        rows = n.out.view(torch.uint8)[r.token].view(torch.float8_e4m3fn)
+        h = matmul_grouped_fp8(rows, n.scale[r.token], *self.w1, r.ends, relu=True, dtype=torch.bfloat16)
+        y = matmul_grouped_fp8(*quantize_fp8(h), *self.w2, r.ends, dtype=torch.bfloat16)
+        return combine_experts(y, r.row, r.p), n.residual
 
 
-def train_step(x, residual, norm, router, w1, w2, dout, top=2):
-    """Forward and backward in bfloat16 for the output's gradient ``dout`` [T, D].  Returns (out, gradients of x (the
-    residual's is the same), norm, w1, w2); the routing is taken as given."""
-    n = rmsnorm(x, norm, residual)
-    T = x.shape[0]
-    token, ends, p, which = route(n.out.float() @ router.float().t(), top)
-    rows = n.out[token]
-    h = matmul_grouped(rows, w1, ends, relu=True, dtype=torch.bfloat16)
-    y = matmul_grouped(h, w2, ends, dtype=torch.bfloat16)
-    out = sum_experts(y.float() * p[:, None], which, T)
+#: What ``train_step`` returns where more than the experts is trained: its result, the gradients (None for what the block
+#: does not have), and the balance loss.  ``dshared`` holds the gradients of (v1, c1, v2, c2).
+TrainStep = namedtuple("TrainStep", "out dx dnorm dw1 dw2 dbias drouter dshared loss")
 
-    dy = (dout.float()[token] * p[:, None]).bfloat16()
-    dw2 = matmul_grouped_wgrad(h, dy, ends)
-    dh = matmul_grouped(dy, w2, ends, transpose_b=True, dtype=torch.bfloat16)
+
+def train_step(x, residual, norm, router, w1, w2, dout, top=2, bias=None, balance=None, shared=None,
+               activation="gelu_tanh"):
+    """Forward and backward in bfloat16 for the output's gradient ``dout`` [T, D].
+
+    Returns (out, gradients of x (the residual's is the same), norm, w1, w2), the routing taken as given.  With
+    ``bias`` [D] the norm is a layer norm; with the number ``balance`` the router is trained too, through the weights
+    of the chosen experts and ``balance`` times the balance loss; ``shared`` = (v1 [D, S], c1 [S], v2 [S, D], c2 [D]) is
+    an expert for every token.  With any of these the result is a ``TrainStep``."""
+    bf16 = torch.bfloat16
+    dout = dout if _fits(dout) else dout.float().contiguous()
+    n = _normed(x, norm, bias, residual)
+    scores = linear(n.out, router, transpose_b=True) if router.dtype == bf16 else n.out.float() @ router.float().t()
+    r = routing(scores, top)
+    rows = n.out[r.token]
+    h = matmul_grouped(rows, w1, r.ends, relu=True, dtype=bf16)
+    y = matmul_grouped(h, w2, r.ends, dtype=bf16)
+    out = combine_experts(y, r.row, r.p)
+    dense = dshared = drouter = None
+    if shared is not None:
+        v1, c1, v2, c2 = shared
+        dense, z = linear(n.out, v1, c1, activation=activation, keep=True, dtype=bf16)
+        out = linear(dense, v2, c2, residual=out)
+
+    dy, dp = combine_experts_backward(dout, y, r.row, r.token, r.p)
+    dw2 = matmul_grouped_wgrad(h, dy, r.ends)
+    dh = matmul_grouped(dy, w2, r.ends, transpose_b=True, dtype=bf16)
     dh = torch.where(h > 0, dh, torch.zeros_like(dh))
-    dw1 = matmul_grouped_wgrad(rows, dh, ends)
-    drows = matmul_grouped(dh, w1, ends, transpose_b=True)
-    dn = sum_experts(drows, which, T).to(x.dtype)
-    dx, dnorm = rmsnorm_backward(dn, n.residual, norm, n.rstd)
-    return out, dx, dnorm, dw1, dw2
+    dw1 = matmul_grouped_wgrad(rows, dh, r.ends)
+    dn = combine_experts(matmul_grouped(dh, w1, r.ends, transpose_b=True), r.row)
+    if balance is not None:
+        ds = route_experts_backward(dp, scores, r.expert, r.p, r.counts, float(balance), dtype=bf16)
+        drouter = linear_wgrad(ds, n.out)
+        dn = linear(ds, router.to(bf16), residual=dn)
+    if shared is not None:
+        d2, dc2 = activation_backward(dout, None, None)
+        d1, dc1 = activation_backward(linear(d2, v2, transpose_b=True, dtype=bf16), z, activation)
+        dshared = (linear_wgrad(n.out, d1), dc1, linear_wgrad(dense, d2), dc2)
+        dn = linear(d1, v1, transpose_b=True, residual=dn)
+    dn = dn.to(x.dtype)
+    if bias is None:
+        dbias = None
+        dx, dnorm = rmsnorm_backward(dn, n.residual, norm, n.rstd)
+    else:
+        dx, dnorm, dbias = layernorm_backward(dn, n.residual, norm, n.mean, n.rstd)
+    if bias is None and balance is None and shared is None:
+        return out, dx, dnorm, dw1, dw2
+    return TrainStep(out, dx, dnorm, dw1, dw2, dbias, drouter, dshared, r.loss)
 
 
 def weights(E, D, F, device="cuda", seed=0):
@@ -121,6 +188,11 @@ def main():
         x, r = (torch.randn(tokens, a.width, device="cuda").bfloat16() for _ in range(2))
         timed("serving %d token(s), 8 bits" % tokens, lambda: served.step(x, r))
     timed("training %d tokens, bfloat16" % a.tokens, lambda: train_step(x, r, norm, router, w1, w2, x))
+    D, S = a.width, a.hidden
+    shared = ((torch.randn(D, S, device="cuda") / D ** 0.5).bfloat16(), torch.zeros(S, device="cuda"),
+              (torch.randn(S, D, device="cuda") / S ** 0.5).bfloat16(), torch.zeros(D, device="cuda"))
+    timed("with its router and a shared expert",
+          lambda: train_step(x, r, norm, router, w1, w2, x, bias=torch.zeros_like(norm), balance=0.01, shared=shared))
 
 
 if __name__ == "__main__":

@@ -406,3 +406,166 @@ def test_linear_gradients_against_differences(act):
             up[i], down[i] = leaf[i] + step * v, leaf[i] - step * v
             num = (loss(*up) - loss(*down)) / (2 * step)
             assert abs(num - (g * v).sum().item()) <= 1.5 * BF16 * (mag * v.abs()).sum().item()
+
+
+# ---------------------------- streams, graphs, far offsets, the two ways of a call
+
+
+def chain(v, w, r):
+    """The operators as a block uses them, from rows ``v`` [T, 256]: everything that they give."""
+    n = x.layernorm(v, w["norm"], w["bias"], v)
+    route = x.route_experts(x.linear(n.out, w["router"], transpose_b=True), 3, r)
+    y, z = x.linear(n.out, w["v1"], w["c1"], activation="gelu", keep=True, dtype=torch.bfloat16)
+    rows = n.out[route.token.clamp_min(0)]
+    out = x.combine_experts(rows, route.row, route.p, residual=x.linear(y, w["v2"], w["c2"], residual=n.residual))
+    drows, dp = x.combine_experts_backward(v, rows, route.row, route.token, route.p)
+    ds = x.route_experts_backward(dp, x.linear(n.out, w["router"], transpose_b=True), route.expert, route.p, route.counts, 0.1)
+    dz, dc = x.activation_backward(x.linear(v, w["v2"], transpose_b=True, dtype=torch.bfloat16), z, "gelu")
+    dn = x.linear(dz, w["v1"], transpose_b=True, residual=x.combine_experts(drows, route.row), dtype=torch.bfloat16)
+    return [*n[:1], *n[2:], *route, y, z, out, drows, dp, ds, dz, dc, x.linear_wgrad(n.out, dz), dn,
+            *x.layernorm_backward(dn, n.residual, w["norm"], n.mean, n.rstd)]
+
+
+def chain_weights(D=256, S=320, E=12):
+    w = {"norm": 1 + 0.1 * normal(1, D), "bias": 0.1 * normal(2, D), "router": normal(3, E, D) / 16, "v1": normal(4, D, S) / 16,
+         "c1": normal(5, S), "v2": normal(6, S, D) / 18, "c2": normal(7, D)}
+    return {k: t.bfloat16().cuda() for k, t in w.items()}
+
+
+@pytest.mark.parametrize("T", [1, 33, 700])
+def test_captured_in_a_graph(T):
+    """Replays give what eager calls give, with new values in the same tensors and eager work between them."""
+    w, v, there = chain_weights(), normal(8, T, 256).bfloat16().cuda(), torch.ones(T, dtype=torch.bool, device="cuda")
+    chain(v, w, there)
+    torch.cuda.synchronize()
+    graph, other = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = chain(v, w, there)
+    u = v.clone()
+    with torch.cuda.graph(other):
+        second = chain(u, w, there)
+    for seed in range(4):
+        v.copy_(normal(10 + seed, T, 256).bfloat16())
+        u.copy_(normal(20 + seed, T, 256).bfloat16())
+        there.copy_(torch.rand(T, generator=torch.Generator().manual_seed(seed)) < (0.8 if seed < 3 else 0))
+        graph.replay()
+        other.replay()
+        want = chain(v, w, there), chain(u, w, there)
+        torch.cuda.synchronize()
+        for a, b in zip(captured + second, want[0] + want[1]):
+            assert torch.equal(torch.nan_to_num(a), torch.nan_to_num(b))
+
+
+def test_operators_run_on_the_current_stream():
+    """Each call is enqueued behind what the current stream holds, and before what follows on it."""
+    w, src = chain_weights(), normal(1, 300, 256).bfloat16().cuda()
+    want = [t.clone() for t in chain(src, w, None)]
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(20_000_000)
+        got = chain(src * 1, w, None)
+        after = [t * 1 for t in got]
+    s.synchronize()
+    for p, q in zip(want, after):
+        assert torch.equal(p, q)
+
+
+def test_native_and_python_paths_agree(monkeypatch):
+    """The plain calls go through the native module; without it the same library is called from Python."""
+    w, v, there = chain_weights(), normal(1, 300, 256).bfloat16().cuda(), (normal(2, 300) < 0.5).cuda()
+    assert x._fast is not None
+    taken = []
+    for name in ("layernorm", "layernorm_backward", "linear", "linear_wgrad", "activation_backward", "route_experts",
+                 "route_experts_backward", "combine_experts", "combine_experts_backward"):
+        def counted(*args, f=getattr(x._fast, name), name=name):
+            r = f(*args)
+            taken.append((name, r is not None))
+            return r
+        monkeypatch.setattr(x._fast, name, counted)
+    q = x.layernorm(v, w["norm"], quantize=True)
+    native = [t.clone() for t in chain(v, w, there)] + [q.out.float(), q.scale]
+    out = torch.empty(300, 320, dtype=torch.bfloat16, device="cuda")
+    assert x.linear(v, w["v1"], out=out) is out and x.linear(v, w["v1"], out=out, keep=True)[0] is out
+    native += [out.clone(), x.linear_wgrad(v, v, dtype=torch.bfloat16), x.activation_backward(v, v, None)[1]]
+    assert len({n for n, _ in taken}) == 9 and all(ok for _, ok in taken)
+    monkeypatch.setattr(x, "_fast", None)
+    q = x.layernorm(v, w["norm"], quantize=True)
+    python = chain(v, w, there) + [q.out.float(), q.scale]
+    assert x.linear(v, w["v1"], out=out) is out
+    python += [out.clone(), x.linear_wgrad(v, v, dtype=torch.bfloat16), x.activation_backward(v, v, None)[1]]
+    for a, b in zip(native, python):
+        assert a.dtype == b.dtype and a.shape == b.shape and torch.equal(a, b)
+
+
+def test_rows_past_32_bit_offsets():
+    """Operands of more than 2^32 bytes: the last rows are the right ones."""
+    T, D = 600_000, 4096
+    a = torch.zeros(T, D, dtype=torch.bfloat16, device="cuda")               # 4.9 GB
+    last = as_type(normal(2, 40, D), "bf16")
+    a[-40:] = last.cuda()
+    w = as_type(1 + 0.1 * normal(3, D), "bf16")
+    n = x.layernorm(a, w.cuda(), None, a)
+    _, mean, rstd, y, e_mean, e_rstd, e_y = norm_reference(last, w, None, last, 1e-5)
+    within(host(n.out[-40:]), y, BF16 * y.abs() + (1 + BF16) * e_y, "layernorm")
+    del n
+    b, bias = as_type(normal(4, D, 64) / 64, "bf16"), as_type(normal(5, 64), "bf16")
+    z, ref, e_z, e = linear_reference(last, b, bias, None, "silu")
+    got = x.linear(a, b.cuda(), bias.cuda(), activation="silu")
+    within(host(got[-40:]), ref, e + U * ref.abs(), "linear")
+    dw = x.linear_wgrad(a, torch.cat([torch.zeros(T - 40, 64, dtype=torch.bfloat16), as_type(normal(6, 40, 64), "bf16")]).cuda())
+    p, q = last.double(), as_type(normal(6, 40, 64), "bf16").double()
+    within(host(dw), p.t() @ q, 2 * U * 64 * (p.abs().t() @ q.abs()) + U * (p.t() @ q).abs(), "linear_wgrad")
+    dz, db = x.activation_backward(a, a, "relu")
+    ref = last.double().clamp_min(0)
+    within(host(dz[-40:]), ref, BF16 * ref, "dz")
+    within(host(db), ref.sum(0), 48 * U * ref.sum(0), "dbias")
+    del dz
+    row = torch.full((3, 2), T - 40, dtype=torch.int32) + torch.arange(6).view(3, 2).int()
+    got = x.combine_experts(a, row.cuda())
+    ref = last.double()[:6].view(3, 2, D).sum(1)
+    within(host(got), ref, 4 * U * last.double()[:6].abs().view(3, 2, D).sum(1), "combine")
+
+
+def test_refusals_on_the_gpu():
+    def c(*shape, dtype=torch.bfloat16):
+        return torch.zeros(*shape).to(dtype).cuda()
+
+    f32, i32 = torch.float32, torch.int32
+    cases = [
+        (lambda: x.layernorm(c(4, 8), c(9)), ValueError, "weight must be a contiguous vector of 8"),
+        (lambda: x.layernorm(c(4, 8), c(8), c(8, dtype=f32)), TypeError, "bias must be bfloat16"),
+        (lambda: x.layernorm(c(4, 8), c(8), None, c(4, 9)), ValueError, "residual must be"),
+        (lambda: x.layernorm(c(4, 8), c(8), eps=-1.0), x.XtcError, "extent|shape"),
+        (lambda: x.layernorm_backward(c(4, 8), c(4, 8), c(8), c(4), c(4, dtype=f32)), TypeError, "mean must be float32"),
+        (lambda: x.linear(c(4, 8), c(9, 4)), ValueError, "inner dimensions differ"),
+        (lambda: x.linear(c(4, 8), c(4, 9), transpose_b=True), ValueError, "inner dimensions differ"),
+        (lambda: x.linear(c(4, 8), c(8, 4), c(5)), ValueError, "bias must be a contiguous vector of 4"),
+        (lambda: x.linear(c(4, 8), c(8, 4), None, c(4, 5)), ValueError, "residual must be"),
+        (lambda: x.linear(c(4, 8), c(8, 4), dtype=torch.float16), TypeError, "dtype must be"),
+        (lambda: x.linear(c(4, 8), c(8, 4), out=c(4, 5)), ValueError, "out must be"),
+        (lambda: x.linear(c(1, 8).expand(4, 8), c(8, 4)), x.XtcError, "leading|stride"),
+        (lambda: x.linear(c(4, 8), c(4, 8).t()), ValueError, "unit stride"),
+        (lambda: x.linear_wgrad(c(4, 8), c(5, 4)), ValueError, "rows"),
+        (lambda: x.activation_backward(c(4, 8), c(4, 9), "silu"), ValueError, "z must be"),
+        (lambda: x.route_experts(c(4, 8), 9), ValueError, "top must be"),
+        (lambda: x.route_experts(c(4, 8), 0), ValueError, "top must be"),
+        (lambda: x.route_experts(c(4, 64), 17), x.XtcError, "too large"),
+        (lambda: x.route_experts(c(4, 2000), 2), x.XtcError, "too large"),
+        (lambda: x.route_experts(c(4, 8), 2, c(4)), TypeError, "mask must be bool"),
+        (lambda: x.route_experts(c(4, 8), 2, c(5).bool()), ValueError, "mask must be"),
+        (lambda: x.route_experts_backward(None, c(4, 8), c(4, 2, dtype=i32), c(4, 2, dtype=f32), c(9, dtype=i32)),
+         ValueError, "counts must be"),
+        (lambda: x.route_experts_backward(c(4, 2), c(4, 8), c(4, 2, dtype=i32), c(4, 2, dtype=f32), c(8, dtype=i32)),
+         TypeError, "dp must be float32"),
+        (lambda: x.combine_experts(c(8, 8), c(4, 2)), TypeError, "row must be int32"),
+        (lambda: x.combine_experts(c(8, 8), c(4, 2, dtype=i32), c(4, 3, dtype=f32)), ValueError, "p must be"),
+        (lambda: x.combine_experts(c(8, 8), c(4, 2, dtype=i32), None, c(4, 9)), ValueError, "residual must be"),
+        (lambda: x.combine_experts_backward(c(4, 8), c(9, 8), c(4, 2, dtype=i32), c(8, dtype=i32), c(4, 2, dtype=f32)),
+         ValueError, "rows must hold 8 rows"),
+        (lambda: x.combine_experts_backward(c(4, 9), c(8, 8), c(4, 2, dtype=i32), c(8, dtype=i32), c(4, 2, dtype=f32)),
+         ValueError, "dout must be"),
+    ]
+    for make, error, match in cases:
+        with pytest.raises(error, match=match):
+            make()

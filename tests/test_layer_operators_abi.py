@@ -116,10 +116,10 @@ ROUTE = dict(T=4, E=20, top=3, scores=BAD, lds=20, mask=0, expert=BAD, p=BAD, ro
 
 @pytest.mark.parametrize("change,status", [
     (dict(dtype=2), 4), (dict(T=-1), 2), (dict(E=0), 2), (dict(top=0), 2), (dict(top=21), 2), (dict(top=-1), 2),
-    (dict(workspace_bytes=x.xtc_route_experts_workspace(4, 20) - 1), 2), (dict(lds=19), 3),
+    (dict(T=4000, workspace_bytes=x.xtc_route_experts_workspace(4000, 20) - 1), 2), (dict(lds=19), 3),
     (dict(E=1025, lds=1025), 7), (dict(E=64, lds=64, top=17), 7), (dict(T=1 << 30), 7), (dict(T=BIG), 7), (dict(lds=BIG), 7),
     (dict(scores=0), 1), (dict(expert=0), 1), (dict(p=0), 1), (dict(row=0), 1), (dict(token=0), 1), (dict(counts=0), 1),
-    (dict(ends=0), 1), (dict(loss=0), 1), (dict(workspace=0), 1), (dict(scores=BAD + 2), 9), (dict(expert=BAD + 2), 9),
+    (dict(ends=0), 1), (dict(loss=0), 1), (dict(T=4000, workspace=0), 1), (dict(scores=BAD + 2), 9), (dict(expert=BAD + 2), 9),
     (dict(p=BAD + 1), 9), (dict(row=BAD + 2), 9), (dict(token=BAD + 2), 9), (dict(counts=BAD + 2), 9), (dict(ends=BAD + 2), 9),
     (dict(loss=BAD + 2), 9), (dict(workspace=BAD + 4), 9),
 ])
@@ -130,7 +130,7 @@ def test_route_experts_refuses(change, status):
 def test_route_experts_workspace():
     assert x.xtc_route_experts_workspace(-1, 4) == -1 and x.xtc_route_experts_workspace(4, 0) == -1
     assert x.xtc_route_experts_workspace(4, 1025) == -1 and x.xtc_route_experts_workspace(BIG, 4) == -1
-    assert x.xtc_route_experts_workspace(0, 20) >= 8 * 20
+    assert x.xtc_route_experts_workspace(0, 20) == 0 and x.xtc_route_experts_workspace(4000, 20) >= 8 * 20
 
 
 ROUTE_BACK = dict(T=4, E=20, top=3, DP=BAD, scores=BAD, lds=20, expert=BAD, p=BAD, counts=BAD, dloss=0.1, DS=BAD, ldds=20,
