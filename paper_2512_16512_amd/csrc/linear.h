@@ -30,6 +30,17 @@ struct LinearOrder {
         const int each = tiles_m * tiles_n, split = id / each;
         int im, in;
         tile_coords(id - split * each, each, tiles_m, tiles_n, kBand, 0, im, in);
+        if constexpr (KIND == kBf16N && BN < 64) {
+            // Few rows: the lines of 128 bytes of B's rows, shared by the strips that read pieces of one, go to the XCDs in turn.
+            // With a run of neighbours each, rows of 8 KB lie in a quarter of an XCD's L2 channels (1 x 4096 to 4096
+            // 11.8 us, so 11.0; 2560 to 2048 6.2 and 5.5).
+            constexpr int G = 64 / BN;
+            const int lines = tiles_n / G;
+            if (tiles_m == 1 && tiles_n % (8 * G) == 0) {
+                const int l = in / G, each = lines / 8;
+                in = (l % each * 8 + l / each) * G + in % G;
+            }
+        }
         const int at = split * p.k_each;
         if constexpr (KIND == kWgrad) {
             const int left = (int)p.T - at;

@@ -27,25 +27,23 @@ constexpr double kJoinUs = 2.4, kJoinPartUs = .15;
 int64_t padded(int64_t n) { return cdiv(n, 8) * 8; }
 int64_t room(int64_t bytes) { return cdiv(bytes, 256) * 256; }
 
-// Microseconds of a launch over `splits` parts: rounds of tiles, no less than the operands'
-// way from memory, and the way of the parts' sums to memory and back.
-double estimate_us(const LinearChoice &c, int64_t rows, int64_t cols, int64_t reduce, int64_t operands, int splits, int64_t k_each) {
-    const double stages = (double)cdiv(k_each < reduce ? k_each : reduce, 64);
-    const int64_t slots = 256 * c.per_cu, n = cdiv(rows, c.bm) * cdiv(cols, c.bn) * splits, whole = n / slots, rest = n - whole * slots;
+// Microseconds of a launch of n tiles with `stages` of k each: rounds of tiles, no less than the operands'
+// way from memory, and the way of the splits' sums to memory and back.  (A call makes up its plan twice; 0.2 us each.)
+double estimate_us(const LinearChoice &c, int64_t n, double stages, double memory, int splits, double sums) {
+    const int64_t slots = 256 * c.per_cu, whole = n < slots ? 0 : n / slots, rest = n - whole * slots;
     double us = whole * (stages * (c.per_cu > 1 ? c.full : c.one) + c.fixed);
     if (rest > 0) {
-        const int64_t held = cdiv(rest, 256);
+        const int64_t held = (rest + 255) >> 8;
         const double stage = held > 1 ? c.one + (c.full - c.one) * (held - 1) / (c.per_cu - 1) : c.one * (c.fill + (1 - c.fill) * rest / 256);
         const double last = stages * stage + c.fixed;
         // (where CUs hold several workgroups, those of a last, partial round begin as others end)
         us += whole > 0 && c.per_cu > 1 ? .75 * last : last;
     }
-    const double memory = 2 + operands * 2 / 5e6;
     us = us > memory ? us : memory;
-    if (splits > 1) us += kJoinUs + kJoinPartUs * splits + 8. * splits * rows * cols / 12e6;
+    if (splits > 1) us += kJoinUs + kJoinPartUs * splits + 8. * splits * sums / 12e6;
     return us;
 }
-double copy_us(int64_t bytes) { return 3.5 + bytes / 3.2e6; }
+double copy_us(double bytes) { return 3.5 + bytes / 3.2e6; }
 
 template <Kind KIND>
 Plan plan(const LinearArgs &a) {
@@ -59,12 +57,22 @@ Plan plan(const LinearArgs &a) {
     best.k_each = (int)(cdiv(some, kSplitStep) * kSplitStep);
     double least = 0;
     int seen = 0;
+    const double size_a = (double)a.T * a.K, size_b = (KIND == kWgrad ? (double)a.T : (double)a.K) * a.N, sums = (double)rows * a.N;
+    const double memory = 2 + (size_a + size_b) * 2 / 5e6;
+    const double copying = a_fits && b_fits ? 0 : copy_us((a_fits ? 0 : 2 * size_a) + (b_fits ? 0 : 2 * size_b));
     auto look = [&](const LinearChoice *c, int count, bool copies) {
-        for (int i = 0; i < count; ++i, ++seen)
-            for (int want = 1; want <= kMostSplits; want *= 2) {
-                const int64_t each = cdiv(cdiv(some, want), kSplitStep) * kSplitStep;
-                const int splits = (int)cdiv(some, each);
-                if (want > 1 && (splits < 2 || each < 256)) break;
+        for (int i = 0; i < count; ++i, ++seen) {
+            const uint32_t bm = (uint32_t)c[i].bm, bn = (uint32_t)c[i].bn;
+            const int64_t tiles = (int64_t)(((uint32_t)rows + bm - 1) / bm) * (((uint32_t)a.N + bn - 1) / bn);
+            for (int want = 1, last = 0; want <= kMostSplits; want *= 2) {
+                const uint32_t each = ((uint32_t)some + want * kSplitStep - 1) / (want * kSplitStep) * kSplitStep;
+                const int splits = (int)(((uint32_t)some + each - 1) / each);
+                // (nothing is gained by splits of tiles that fill the CUs)
+                if (want > 1 && (splits < 2 || each < 256 || tiles * last >= 256 * c[i].per_cu)) break;
+                last = splits;
+                double us = estimate_us(c[i], tiles * splits, (double)(((each < some ? each : (uint32_t)some) + 63) / 64), memory, splits, sums);
+                if (copies) us += copying;
+                if (best.choice && us >= least) continue;
                 Plan w = {};
                 w.choice = &c[i];
                 w.splits = splits;
@@ -77,13 +85,10 @@ Plan plan(const LinearArgs &a) {
                 w.copy_a = w.a_bytes > 0;
                 w.copy_b = w.b_bytes > 0;
                 if (splits > 1) w.part_bytes = room(4 * (int64_t)splits * rows * a.N);
-                double us = estimate_us(c[i], rows, a.N, reduce, a.T * a.K + (KIND == kWgrad ? a.T : a.K) * (int64_t)a.N, splits, each);
-                if (copies && !(a_fits && b_fits)) us += copy_us(w.a_bytes + w.b_bytes);
-                if (!best.choice || us < least) {
-                    best = w;
-                    least = us;
-                }
+                best = w;
+                least = us;
             }
+        }
     };
     int count = 0;
     if (!a_fits || !b_fits) {
@@ -122,7 +127,7 @@ __global__ void __launch_bounds__(kCopyThreads) linear_copy_kernel(Copy a, Copy 
 }
 
 // The sums of the parts, in their order, and the epilogue: a row's EACH columns a thread.
-constexpr int kJoinThreads = 256, kJoinEach = 4;
+constexpr int kJoinThreads = 256, kJoinEach = 4, kJoinAtOnce = 4;
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) linear_join_kernel(LinearArgs p, int rows) {
     const int chunks = (p.N + kJoinEach - 1) / kJoinEach;
@@ -130,11 +135,15 @@ __global__ void __launch_bounds__(kJoinThreads) linear_join_kernel(LinearArgs p,
     const int row = (int)(id / chunks), n = (int)(id - (int64_t)row * chunks) * kJoinEach;
     if (row >= rows) return;
     float v[kJoinEach] = {};
-    for (int s = 0; s < p.splits; ++s) {
-        float q[kJoinEach];
-        Epilogue<T, kJoinEach>::load(p.part, 1, ((int64_t)s * rows + row) * p.N + n, p.N - n, q);
+    for (int s0 = 0; s0 < p.splits; s0 += kJoinAtOnce) {
+        float q[kJoinAtOnce][kJoinEach];
 #pragma unroll
-        for (int i = 0; i < kJoinEach; ++i) v[i] += q[i];
+        for (int k = 0; k < kJoinAtOnce; ++k)
+            Epilogue<T, kJoinEach>::load(p.part, 1, ((int64_t)(s0 + k < p.splits ? s0 + k : 0) * rows + row) * p.N + n, p.N - n, q[k]);
+#pragma unroll
+        for (int k = 0; k < kJoinAtOnce; ++k)
+#pragma unroll
+            for (int i = 0; i < kJoinEach; ++i) v[i] += s0 + k < p.splits ? q[k][i] : 0.f;
     }
     finish_at<T, kJoinEach>(p, row, n, v);
 }
@@ -146,9 +155,12 @@ int64_t workspace(const LinearArgs &a) {
 }
 
 template <Kind KIND>
-xtc_status launch(const LinearArgs &given, void *workspace, hipStream_t s) {
+xtc_status launch(const LinearArgs &given, void *workspace, int64_t bytes, hipStream_t s) {
     LinearArgs a = given;
     const Plan w = plan<KIND>(a);
+    const int64_t need = w.part_bytes + w.a_bytes + w.b_bytes;
+    if (need > bytes) return XTC_ERR_BAD_SHAPE;
+    if (need > 0 && !workspace) return XTC_ERR_NULL_POINTER;
     unsigned char *ws = static_cast<unsigned char *>(workspace);
     a.splits = w.splits;
     a.k_each = w.k_each;
@@ -239,11 +251,13 @@ __global__ void __launch_bounds__(kSlopeWaves * 64) activation_backward_kernel(A
 int64_t linear_workspace(const LinearArgs &a, bool b_rows_n) {
     return b_rows_n ? workspace<kBf16T>(a) : workspace<kBf16N>(a);
 }
-xtc_status launch_linear(const LinearArgs &a, bool b_rows_n, void *workspace, hipStream_t s) {
-    return b_rows_n ? launch<kBf16T>(a, workspace, s) : launch<kBf16N>(a, workspace, s);
+xtc_status launch_linear(const LinearArgs &a, bool b_rows_n, void *workspace, int64_t bytes, hipStream_t s) {
+    return b_rows_n ? launch<kBf16T>(a, workspace, bytes, s) : launch<kBf16N>(a, workspace, bytes, s);
 }
 int64_t linear_wgrad_workspace(const LinearArgs &a) { return workspace<kWgrad>(a); }
-xtc_status launch_linear_wgrad(const LinearArgs &a, void *workspace, hipStream_t s) { return launch<kWgrad>(a, workspace, s); }
+xtc_status launch_linear_wgrad(const LinearArgs &a, void *workspace, int64_t bytes, hipStream_t s) {
+    return launch<kWgrad>(a, workspace, bytes, s);
+}
 
 namespace {
 

@@ -202,12 +202,13 @@ xtc_status launch_grouped_bf16(const GroupedArgs &a, bool b_rows_n, hipStream_t 
 // bf16 A [T, K] and B [T, N]: C of group g [K, N] = A_g^T B_g
 xtc_status launch_grouped_wgrad(const GroupedArgs &a, hipStream_t s);
 
-// bf16 A [T, K] and B [K, N] (b_rows_n: [N, K]), with a workspace of linear_workspace() bytes.
+// bf16 A [T, K] and B [K, N] (b_rows_n: [N, K]), with a workspace of linear_workspace() bytes (of fewer:
+// XTC_ERR_BAD_SHAPE, before any HIP call).
 int64_t linear_workspace(const LinearArgs &a, bool b_rows_n);
-xtc_status launch_linear(const LinearArgs &a, bool b_rows_n, void *workspace, hipStream_t s);
+xtc_status launch_linear(const LinearArgs &a, bool b_rows_n, void *workspace, int64_t bytes, hipStream_t s);
 // C [K, N] = A^T B of bf16 A [T, K], B [T, N]
 int64_t linear_wgrad_workspace(const LinearArgs &a);
-xtc_status launch_linear_wgrad(const LinearArgs &a, void *workspace, hipStream_t s);
+xtc_status launch_linear_wgrad(const LinearArgs &a, void *workspace, int64_t bytes, hipStream_t s);
 int activation_slabs(int64_t T, int64_t N);
 xtc_status launch_activation_backward(const ActivationArgs &a, hipStream_t s);
 

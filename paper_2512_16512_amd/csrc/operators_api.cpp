@@ -290,10 +290,7 @@ xtc_status xtc_linear(int64_t T, int64_t N, int64_t K, const void *A, int64_t ld
         return XTC_ERR_MISALIGNED;
     if (T == 0 || N == 0) return XTC_OK;
     if (!C || (K > 0 && (!A || !B))) return XTC_ERR_NULL_POINTER;
-    const int64_t need = xtc_linear_workspace(T, N, K, A, lda, B, ldb, transpose_b);
-    if (workspace_bytes < need) return XTC_ERR_BAD_SHAPE;
-    if (need > 0 && !workspace) return XTC_ERR_NULL_POINTER;
-    return launch_linear(a, transpose_b != 0, workspace, static_cast<hipStream_t>(stream));
+    return launch_linear(a, transpose_b != 0, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
 }
 
 int64_t xtc_linear_wgrad_workspace(int64_t T, int64_t N, int64_t K, const void *A, int64_t lda, const void *DY,
@@ -321,10 +318,7 @@ xtc_status xtc_linear_wgrad(int64_t T, int64_t N, int64_t K, const void *A, int6
     if (!aligned_to(workspace, 16)) return XTC_ERR_MISALIGNED;
     if (N == 0 || K == 0) return XTC_OK;
     if (!DB || (T > 0 && (!A || !DY))) return XTC_ERR_NULL_POINTER;
-    const int64_t need = xtc_linear_wgrad_workspace(T, N, K, A, lda, DY, lddy);
-    if (workspace_bytes < need) return XTC_ERR_BAD_SHAPE;
-    if (need > 0 && !workspace) return XTC_ERR_NULL_POINTER;
-    return launch_linear_wgrad(a, workspace, static_cast<hipStream_t>(stream));
+    return launch_linear_wgrad(a, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
 }
 
 int64_t xtc_activation_backward_workspace(int64_t T, int64_t N) {

@@ -34,7 +34,7 @@ SIZES = [
     (2, 1, 3, 72, 133), (2, 1, 3, 4195, 200), (2, 1, 258, 520, 200), (2, 1, 1030, 235, 389), (2, 1, 4360, 72, 1208),
     (3, 0, 3, 2064, 3880), (3, 0, 332, 1208, 3272), (3, 0, 6662, 1176, 136), (3, 0, 3, 72, 72), (3, 0, 577, 72, 72),
     (3, 1, 3, 968, 4077), (3, 1, 1326, 4163, 72), (3, 1, 3, 72, 72), (3, 1, 513, 72, 72), (3, 1, 3, 2619, 3109),
-    (3, 1, 385, 2251, 1997), (3, 1, 3749, 2728, 141), (3, 1, 3, 3443, 1168), (3, 1, 1349, 3291, 272),
+    (3, 1, 385, 2251, 1997), (3, 1, 3749, 2728, 141), (3, 1, 3, 3443, 1168), (3, 1, 2584, 144, 2861),
 ]
 
 
