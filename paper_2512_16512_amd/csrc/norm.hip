@@ -63,6 +63,9 @@ __device__ __forceinline__ Raw8<float> raw_weight(const void *w, int w_f32, cons
 // bits, bound by memory: 52 us, 4.5 TB/s of its 236 MB where a copy reaches 5.3
 // (the loop kernel below, which reads a row twice, 67).  One row of 4096 columns
 // takes 3.9 us, the time of a launch and two trips to memory.
+// The layer norm (CENTER) reads and writes past the caches: 8192 x 4096 bf16 with a residual 49 us, 5.5 TB/s of its
+// 269 MB, as fast as a copy (64 through the caches; 103 with a wave a row, whose registers leave too few rows in
+// flight; rows at odd addresses, 8192 x 3001, 52 and 60).
 template <int NT>
 struct RowTeam {
     static constexpr int THREADS = NT > 256 ? NT : 256, ROWS = THREADS / NT;
@@ -219,9 +222,11 @@ __global__ void __launch_bounds__(kThreads) norm_loop_kernel(NormArgs p) {
 
 // The gradient in one pass: team by team, rows t, t + teams, ...; a thread keeps
 // the sums over its rows of its columns' part of DW (CENTER: and of DB), and the
-// workgroup leaves one row of partial sums (CENTER: of 2D, DW's first).  The next row is on its way while one is computed.
+// workgroup leaves one row of partial sums (CENTER: of 2D, DW's first; TEAMS of NT threads share it, so that
+// there are 256 such rows at most, and both sums of a row pass one barrier).  The next row is on its way while one is computed.
 // 8191 x 2048 bf16, bound by memory: 28.6 us, 4.7 TB/s; DX and DW by kernels of
-// their own, which read the rows twice, took 151 us.
+// their own, which read the rows twice, took 151 us.  The layer norm's, past the caches: 28.6 us and 4 for the join of
+// 256 rows of 4096 sums (37 us in all through the caches with 1024 rows of sums and two barriers a row, so 31).
 template <typename T, bool CENTER, int NT, int NV, int TEAMS>
 __global__ void __launch_bounds__(NT * TEAMS) norm_backward_kernel(NormBackwardArgs p) {
     typedef RowTeam<NT> Team;
@@ -351,7 +356,7 @@ __global__ void __launch_bounds__(NT * TEAMS) norm_backward_kernel(NormBackwardA
 
 // Rows of more columns than registers hold: DX and DW by kernels of their own, which
 // read X and DY three times in all (4096 x 16384 bf16: 311 us, 1.7 TB/s of what one
-// pass would move; 4096 x 8192 in one pass 64 us, 4.2 TB/s).
+// pass would move, the layer norm's 330; 4096 x 8192 in one pass 64 us, 4.2 TB/s, both).
 template <typename T, bool CENTER>
 __global__ void __launch_bounds__(kThreads) norm_dx_kernel(NormBackwardArgs p) {
     __shared__ float scratch[kThreads / 64];

@@ -13,6 +13,11 @@
 // The order of the rows (by expert, then by token) has no atomics in it that could change it: of 64
 // tokens each expert has a word of 64 bits, one a token, so that a row's place among them is a count of
 // bits; the workgroups' counts go to memory, and a second kernel adds up those before its own.
+//
+// Bound by latency, not by its few bytes: one token over 64 experts 6.2 us in one launch (top times a chain of
+// maxima over the lanes); 16383 over 128 experts, top 8, 8.5 us for the choices, with a team for each token of a
+// workgroup (16 teams that took four in turn 12.8), and 10 us for the places, whose counts are read in one go (one load after
+// the other 14.6).
 #include <type_traits>
 
 #include "activation.h"
@@ -329,7 +334,8 @@ __global__ void __launch_bounds__(kThreads) route_small_kernel(RouteArgs p) {
     place<kThreads>(p, h, 0, 1, true, true, smem);
 }
 
-// ds of the tokens blockIdx.x, + gridDim.x, ... of each team.
+// ds of the tokens blockIdx.x, + gridDim.x, ... of each team.  16384 x 64 fp32, top 6: 5.3 us with the launch, of which
+// its 9.6 MB are 1.8.
 template <typename T, typename O, int LANES, int VPT>
 __global__ void __launch_bounds__(kThreads) route_backward_kernel(RouteBackwardArgs p) {
     constexpr int TEAMS = kThreads / LANES;
