@@ -438,7 +438,8 @@ xtc_status xtc_matmul_fp8(int64_t M, int64_t N, int64_t K,
  *  bias   device, N values of bias_dtype (XTC_F32 or XTC_BF16), or NULL.
  *  R      device, T x N of r_dtype (XTC_F32 or XTC_BF16), row stride ldr, or NULL.
  *  activation  an xtc_activation, else XTC_ERR_BAD_SHAPE.
- *  C      device, out_dtype (XTC_F32 or XTC_BF16) T x N, row stride ldc.
+ *  C      device, out_dtype (XTC_F32 or XTC_BF16) T x N, row stride ldc.  It may be
+ *         R itself (ldc == ldr, out_dtype == r_dtype).
  *  Z      device, z in out_dtype for the activation's gradient, row stride ldz, or
  *         NULL.
  *  workspace  device, workspace_bytes >= xtc_linear_workspace() of the same operands
@@ -552,8 +553,9 @@ xtc_status xtc_matmul_grouped_fp8(int64_t G, int64_t T, int64_t N, int64_t K,
  *
  *  E, top     experts (1 to 1024) and how many a token chooses (1 to 16, at most E);
  *             T * top at most 0x7FFFFF00.
- *  scores     device, dtype (XTC_F32 or XTC_BF16) T x E, row stride lds.  -inf
- *             forbids an expert; a NaN counts as above every number.
+ *  scores     device, dtype (XTC_F32 or XTC_BF16) T x E, row stride lds.  An expert
+ *             at -inf has the weight 0, and is chosen only where fewer than top
+ *             others are left; a NaN counts as above every number.
  *  mask       device, T bytes, 0 for a token that goes nowhere (padding), or NULL.
  *  expert     T x top: the experts of each token, the highest score first, of equal
  *             scores the lowest index; -1 for a masked token.

@@ -755,9 +755,9 @@ def linear(a, b, bias=None, residual=None, activation=None, transpose_b=False, k
 
     ``a`` [T, K] and ``b`` [K, N] ([N, K] with ``transpose_b``) are bfloat16, ``bias`` [N] and ``residual`` [T, N] float32
     or bfloat16 each.  ``activation``: None, "relu", "gelu" (by the error function), "gelu_tanh" or "silu".  ``out``
-    [T, N] is float32 or bfloat16 (``dtype``, when allocated here; float32 unless given).  With ``keep`` the result is
-    ``(out, z)``, z = a @ b + bias in out's type for ``activation_backward``.  The gradient of ``a`` is the same call
-    on z's gradient with the other ``transpose_b``."""
+    [T, N] is float32 or bfloat16 (``dtype``, when allocated here; float32 unless given), and may be ``residual`` itself.
+    With ``keep`` the result is ``(out, z)``, z = a @ b + bias in out's type for ``activation_backward``.  The gradient of
+    ``a`` is the same call on z's gradient with the other ``transpose_b``."""
     code_act = _activation(activation)
     if _fast is not None:
         r = _fast.linear(a, b, bias, residual, code_act, transpose_b, keep, out, dtype)
@@ -924,7 +924,8 @@ def matmul_grouped_fp8(a, a_scale, b, b_scale, ends, out=None, relu=False, dtype
 #: What ``route_experts`` returns.  ``expert``, ``p``, ``row`` [T, top]: each token's experts (the highest score first),
 #: their weights, and the place of each choice among the rows sorted by expert; ``token`` [T * top]: the token of each of
 #: these rows; ``counts``, ``ends`` [E]: the rows of each expert and where they end (``matmul_grouped``'s ``ends``);
-#: ``loss``: the balance loss, a float32 scalar.  Places and counts are int32.
+#: ``loss``: the balance loss, a float32 scalar.  Places and counts are int32.  They may share one storage, which lives as
+#: long as any of them.
 Routing = namedtuple("Routing", "expert p row token counts ends loss")
 
 
@@ -944,6 +945,7 @@ def route_experts(scores, top, mask=None):
     ``scores`` [T, E] are float32 or bfloat16, E at most 1024 and ``top`` at most 16.  ``p`` is the softmax over a token's
     chosen scores; of equal scores the lowest expert comes first.  Tokens where the boolean ``mask`` [T] is false go to
     no expert: their ``expert`` and ``row`` are -1, their ``p`` zeros, and ``token`` is -1 for the rows behind ``ends[-1]``.
+    A score of -inf has the weight 0: its expert is chosen only where fewer than ``top`` others are left.
     The balance loss is ``E / (top * n**2) * sum_e counts[e] * sum_t softmax(scores[t])[e]`` over the n tokens that are
     left (1 where every expert has as many).  Nothing waits for the GPU."""
     if _fast is not None:

@@ -272,8 +272,10 @@ __global__ void __launch_bounds__(NT * TEAMS) norm_backward_kernel(NormBackwardA
         for (int v = 0; v < NV; ++v)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                // (of columns past the end y and w are zeros, whatever h)
-                h[v][i] = CENTER ? (rx[v].at(i) - centre) * rstd : rx[v].at(i) * rstd;
+                // (past the end y and w are zeros; -centre * rstd, which may leave fp32, is none)
+                h[v][i] = !CENTER                          ? rx[v].at(i) * rstd
+                          : (v * NT + tid) * 8 + i < D ? (rx[v].at(i) - centre) * rstd
+                                                       : 0.f;
                 const float y = ry[v].at(i);
                 dw[v][i] += y * h[v][i];
                 if constexpr (CENTER) db[v][i] += y;
@@ -373,7 +375,7 @@ __global__ void __launch_bounds__(kThreads) norm_dx_kernel(NormBackwardArgs p) {
             load_weight(p.W, p.w_f32, x, c, D - c, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                sum += (g[i] * w[i]) * ((CENTER ? h[i] - centre : h[i]) * rstd);
+                sum += (g[i] * w[i]) * ((CENTER ? (c + i < D ? h[i] - centre : 0.f) : h[i]) * rstd);
                 if constexpr (CENTER) sum_g += g[i] * w[i];
             }
         }

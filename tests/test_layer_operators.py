@@ -188,6 +188,30 @@ def test_layernorm_backward(T, D, dtype):
             within(host(gb), db, e_db, what + " dbias")
 
 
+@pytest.mark.parametrize("D,value", [(1, 2.0 ** 120), (100, 2.0 ** 113), (1001, 2.0 ** 113), (5001, 2.0 ** 113),
+                                     (8201, 2.0 ** 113)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_layernorm_of_equal_large_values(D, value, dtype):
+    """Powers of two whose sum of D is in fp32 and exact, but not their product with rstd = 1e6: centred they are 0."""
+    xs = as_type(torch.full((3, D), value, dtype=torch.float64), dtype)
+    xs[1] = 0
+    w, b = as_type(1 + 0.2 * normal(2, D), dtype), as_type(0.5 * normal(5, D), dtype)
+    dy = as_type(normal(6, 3, D), dtype)
+    n = x.layernorm(dev(xs), dev(w), dev(b), eps=1e-12)
+    assert torch.equal(host(n.out), b.double().expand(3, D))
+    assert torch.equal(host(n.mean), torch.tensor([value, 0, value], dtype=torch.float64))
+    rstd = n.rstd.cpu()
+    within(rstd.double(), torch.full((3,), 1e6, dtype=torch.float64), 4 * U * 1e6, "rstd")
+    gx, gw, gb = x.layernorm_backward(dev(dy), dev(xs), dev(w), n.mean, n.rstd)
+    g = dy.double() * w.double()
+    dx = rstd.double()[:, None] * (g - g.mean(1, keepdim=True))
+    e = rstd.double()[:, None] * (4 * U * g.abs() + (depth(D) + 8) * U * g.abs().mean(1, keepdim=True)) + 4 * U * dx.abs()
+    tail = BF16 if dtype == "bf16" else U
+    within(host(gx), dx, tail * dx.abs() + (1 + tail) * e, "dx")
+    assert not bool(gw.any())
+    within(host(gb), dy.double().sum(0), 4 * U * dy.double().abs().sum(0), "dbias")
+
+
 def test_layernorm_backward_against_differences():
     """Central differences of the 64-bit forward along random directions: their own error is about step^2."""
     T, D, eps, step = 9, 333, 1e-5, 1e-5
@@ -323,6 +347,16 @@ def test_linear_writes_its_own_columns_only():
             tail = BF16 if dtype == torch.bfloat16 else U
             within(host(got), y, tail * y.abs() + (1 + tail) * e, "out")
             assert bool((wide[:, :3] == 5).all()) and bool((wide[:, N + 3:] == 5).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,N,K", [(1, 4096, 4096), (5, 77, 130), (300, 520, 264), (1531, 2000, 4096)])
+def test_linear_adds_to_its_residual_in_place(T, N, K, dtype):
+    a, b, bias, r = linear_case(T, N, K, 5, 1 / 16)
+    a, b, bias, r = dev(a), dev(b), dev(as_type(bias, "f32")), dev(as_type(r, dtype))
+    apart = x.linear(a, b, bias, r, "silu", dtype=r.dtype)
+    assert x.linear(a, b, bias, r, "silu", out=r) is r
+    assert torch.equal(apart, r)
 
 
 @pytest.mark.parametrize("T", [3, 200])
