@@ -10,7 +10,9 @@ conveniences over torch device tensors (torch provides memory and the
 current stream, nothing else); the plain calls among theirs go through
 ``_binding.so`` (csrc/torch_binding.cpp), which saves the interpreter's share
 of a call.  ``rmsnorm``, ``rmsnorm_backward``, ``quantize_fp8``, ``matmul_fp8``,
-``matmul_grouped``, ``matmul_grouped_wgrad`` and ``matmul_grouped_fp8`` likewise
+``matmul_grouped``, ``matmul_grouped_wgrad``, ``matmul_grouped_fp8``, ``layernorm``,
+``linear``, ``route_experts``, ``combine_experts``, their ``_backward`` forms,
+``linear_wgrad`` and ``activation_backward`` likewise
 stand for the entry points of those names.  None of them records an autograd
 graph: a result does not require a gradient whatever its operands do, and the
 gradients are calls of their own.
