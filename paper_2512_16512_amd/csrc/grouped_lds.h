@@ -212,6 +212,65 @@ struct Carried {
     }
 };
 
+// The same for bf16 rows of eight values at least, SETS stages ahead: a load is never waited for before its stage is
+// stored, and none stands in a branch, whose end would have to wait for them all.  A chunk that ends past its row
+// (or the last of k) is read from 16 bytes before that end and shifted as it is stored.
+template <bool K_ROWS, int ROWS, int PER_WAVE, int KB, int SETS>
+struct CarriedAhead {
+    static constexpr int BK = KB / 2;
+    const unsigned char *base;   // of the stage to fetch next, or the last one again
+    int64_t ld;
+    int extent, left;            // (left: values of k from base on, one at least)
+    int64_t off[PER_WAVE];       // of the chunks' rows
+    u32x4 r[SETS][PER_WAVE];
+
+    __device__ __forceinline__ CarriedAhead(const unsigned char *p, int64_t ld_, int extent_, int k, int wave, int lane)
+        : base(p), ld(ld_), extent(extent_ < ROWS + 8 ? extent_ : ROWS + 8), left(k) {
+#pragma unroll
+        for (int q = 0; q < PER_WAVE; ++q) {
+            // (rows past the last one repeat it, of k past the last one the first: nothing of theirs is kept)
+            const int row = row_of(q, wave, lane);
+            off[q] = (K_ROWS || row < extent_ ? row : extent_ - 1) * ld;
+        }
+    }
+
+    // Where this lane's chunk q lies: its row (or k), and its first byte of it.
+    static __device__ __forceinline__ int row_of(int q, int wave, int lane) {
+        const int blk = wave * PER_WAVE + q;
+        return K_ROWS ? (blk * 1024 + lane * 16) / (ROWS * 2) : blk * (1024 / KB) + lane / (KB / 16);
+    }
+    static __device__ __forceinline__ int byte_of(int q, int wave, int lane) {
+        const int row = row_of(q, wave, lane);
+        if constexpr (K_ROWS) return (((wave * PER_WAVE + q) * 64 + lane) % (ROWS / 8) ^ swz_k<ROWS / 8>(row)) * 16;
+        else return ((lane % (KB / 16)) ^ swz_row<KB>(row)) * 16;
+    }
+    template <int SET>
+    __device__ __forceinline__ void fetch(int wave, int lane) {
+        const int last = (K_ROWS ? extent : left < BK + 8 ? left : BK + 8) * 2 - 16;
+#pragma unroll
+        for (int q = 0; q < PER_WAVE; ++q) {
+            const int at = byte_of(q, wave, lane);
+            const int64_t o = !K_ROWS || row_of(q, wave, lane) < left ? off[q] : 0;
+            __builtin_memcpy(&r[SET][q], base + o + (at < last ? at : last), 16);
+        }
+        const bool more = left > BK;
+        base += more ? (K_ROWS ? BK * ld : KB) : 0;
+        left -= more ? BK : 0;
+    }
+    // `of_k`: values of k from the stage's first on
+    template <int SET>
+    __device__ __forceinline__ void store(unsigned char *lds, int q, int of_k, int wave, int lane) const {
+        u32x4 v = r[SET][q];
+        if (of_k < BK || (K_ROWS && extent < ROWS)) {
+            const int end = K_ROWS ? (row_of(q, wave, lane) < of_k ? extent * 2 : 0) : of_k * 2;
+            const int over = byte_of(q, wave, lane) - (end - 16);
+            const u32x4 none = {0, 0, 0, 0};
+            v = over <= 0 ? v : over < 16 ? Carried<K_ROWS, ROWS, PER_WAVE, KB>::shifted(v, over) : none;
+        }
+        *reinterpret_cast<u32x4 *>(lds + q * 1024 + lane * 16) = v;
+    }
+};
+
 // Fragment of the rows (or columns) first .. first + MI - 1 from an operand's
 // stage at s, `ROWS` rows of it in all.
 template <bool K_ROWS, int ROWS, int KB>

@@ -3,7 +3,7 @@
 // e4m3 values; 64 or 32 bf16 ones) in a ring.
 //
 // Rows at any address (ANY) go through registers instead, one stage further
-// ahead.
+// ahead, or AHEAD of them.
 //
 // What bounds it.  Large products the matrix cores: the loop of a 256x256 tile
 // runs at 1583 TFLOP/s in bf16 and 2562 in e4m3, with the first data's way and the
@@ -49,7 +49,7 @@ struct TileCfg {
     static_assert(TM % 4 == 0, "the last two rows and the next stage's first two lie in four places");
 };
 
-template <Kind KIND, bool WIDE, int BM, int BN, int WM, int WN, int STAGES, int KB, bool ANY, typename Args>
+template <Kind KIND, bool WIDE, int BM, int BN, int WM, int WN, int STAGES, int KB, bool ANY, int AHEAD, typename Args>
 __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64, 2)
 grouped_tile_kernel(Args p) {
     typedef TileCfg<KIND, BM, BN, WM, WN, STAGES, KB> G;
@@ -68,14 +68,20 @@ grouped_tile_kernel(Args p) {
     const unsigned smem_base = lds_address(smem);
     const int KT = (t.k + G::BK - 1) / G::BK;
 
-    typedef std::conditional_t<ANY, Carried<G::A_K_ROWS, BM, G::A_PER_WAVE, KB>, Source<G::A_K_ROWS, BM, G::A_PER_WAVE, KB>> FromA;
-    typedef std::conditional_t<ANY, Carried<G::B_K_ROWS, BN, G::B_PER_WAVE, KB>, Source<G::B_K_ROWS, BN, G::B_PER_WAVE, KB>> FromB;
+    constexpr bool FAR = AHEAD > 1;
+    static_assert(!FAR || (ANY && KIND != kFp8), "bf16 rows at any address");
+    typedef std::conditional_t<ANY, Carried<G::A_K_ROWS, BM, G::A_PER_WAVE, KB>, Source<G::A_K_ROWS, BM, G::A_PER_WAVE, KB>> NearA;
+    typedef std::conditional_t<ANY, Carried<G::B_K_ROWS, BN, G::B_PER_WAVE, KB>, Source<G::B_K_ROWS, BN, G::B_PER_WAVE, KB>> NearB;
+    typedef std::conditional_t<FAR, CarriedAhead<G::A_K_ROWS, BM, G::A_PER_WAVE, KB, AHEAD>, NearA> FromA;
+    typedef std::conditional_t<FAR, CarriedAhead<G::B_K_ROWS, BN, G::B_PER_WAVE, KB, AHEAD>, NearB> FromB;
     FromA sa = [&]() __attribute__((always_inline)) {
-        if constexpr (ANY) return FromA(t.A, t.lda, t.m);
+        if constexpr (FAR) return FromA(t.A, t.lda, t.m, t.k, wave, lane);
+        else if constexpr (ANY) return FromA(t.A, t.lda, t.m);
         else return FromA(t.A, t.lda, t.m, wave, lane);
     }();
     FromB sb = [&]() __attribute__((always_inline)) {
-        if constexpr (ANY) return FromB(t.B, t.ldb, t.n);
+        if constexpr (FAR) return FromB(t.B, t.ldb, t.n, t.k, wave, lane);
+        else if constexpr (ANY) return FromB(t.B, t.ldb, t.n);
         else return FromB(t.B, t.ldb, t.n, wave, lane);
     }();
     // this lane's scale of a stage: rows of A, then the blocks of B's columns
@@ -100,13 +106,16 @@ grouped_tile_kernel(Args p) {
     // write zeros), so that one count of copies in flight holds throughout.
     // begin() settles the stage, piece(q) issues one of them.  Of rows at any
     // address (ANY) the stage's values are on their way to registers since
-    // fetch(), and piece(q) writes them.
+    // fetch(), and piece(q) writes them, from the set of registers SET where there are several.
     i32x4 ra, rb;
     int left = 0, next = 0;      // of k from stage `next` on
     unsigned at = 0;
     unsigned char *to = smem;
-    auto fetch = [&](int kt) __attribute__((always_inline)) {
-        if constexpr (ANY) {
+    auto fetch = [&](int kt, auto SET) __attribute__((always_inline)) {
+        if constexpr (FAR) {
+            sa.template fetch<SET()>(wave, lane);
+            sb.template fetch<SET()>(wave, lane);
+        } else if constexpr (ANY) {
             left = t.k - kt * G::BK;
             sa.template fetch<G::E>(left, (KIND == kWgrad ? p.K : t.k) * G::E >= 16, wave, lane);
             sb.template fetch<G::E>(left, (G::B_K_ROWS ? p.N : t.k) * G::E >= 16, wave, lane);
@@ -116,6 +125,7 @@ grouped_tile_kernel(Args p) {
     auto begin = [&](int kt, int slot) __attribute__((always_inline)) {
         if constexpr (ANY) {
             to = smem + slot * G::STAGE_BYTES;
+            if constexpr (FAR) left = t.k - kt * G::BK;
         } else {
             at = smem_base + slot * G::STAGE_BYTES;
             left = t.k - kt * G::BK;
@@ -124,11 +134,14 @@ grouped_tile_kernel(Args p) {
             rb = sb.stage(left, G::E);
         }
     };
-    auto piece = [&](auto Q) __attribute__((always_inline)) {
+    auto piece = [&](auto Q, auto SET) __attribute__((always_inline)) {
         constexpr int q = Q;
         constexpr bool of_a = q < G::A_PER_WAVE, of_b = !of_a && q < G::A_PER_WAVE + G::B_PER_WAVE;
         constexpr int qb = q - G::A_PER_WAVE;
-        if constexpr (ANY) {
+        if constexpr (FAR) {
+            if constexpr (of_a) sa.template store<SET()>(to + wave * G::A_PER_WAVE * 1024, q, left, wave, lane);
+            else sb.template store<SET()>(to + G::A_BYTES + wave * G::B_PER_WAVE * 1024, qb, left, wave, lane);
+        } else if constexpr (ANY) {
             if constexpr (of_a) sa.store(to + wave * G::A_PER_WAVE * 1024, q, lane);
             else if constexpr (of_b) sb.store(to + G::A_BYTES + wave * G::B_PER_WAVE * 1024, qb, lane);
             else reinterpret_cast<float *>(to + G::A_BYTES + G::B_BYTES)[wave * 64 + lane] = s_value;
@@ -198,12 +211,27 @@ grouped_tile_kernel(Args p) {
         for (int r = 0; r < 4; ++r) acc[i][j][r] += part[n % (LAG + 1)][r] * scale[0][i];
     };
 
+    // (AHEAD sets of registers: stage n is in the set n % AHEAD, and fetched when the one before in it has been stored)
+    if constexpr (FAR)
+        each_index([&](auto S) __attribute__((always_inline)) {
+            fetch(S, S);
+            __builtin_amdgcn_sched_barrier(0);
+        }, std::make_integer_sequence<int, AHEAD>());
     each_index([&](auto S) __attribute__((always_inline)) {
-        fetch(S);
+        constexpr std::integral_constant<int, S() % AHEAD> SET;
+        if constexpr (!FAR) fetch(S, SET);
         begin(S, S);
-        each_index([&](auto Q) __attribute__((always_inline)) { piece(Q); }, std::make_integer_sequence<int, G::LOADS>());
+        each_index([&](auto Q) __attribute__((always_inline)) { piece(Q, SET); }, std::make_integer_sequence<int, G::LOADS>());
+        if constexpr (FAR && S() + 1 < STAGES) {
+            __builtin_amdgcn_sched_barrier(0);
+            fetch(S + AHEAD, SET);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }, std::make_integer_sequence<int, STAGES>());
-    if constexpr (ANY) {
+    if constexpr (FAR) {
+        __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+    } else if constexpr (ANY) {
         __syncthreads();
     } else {
         wait_vmcnt<(STAGES - 1) * G::LOADS>();
@@ -221,8 +249,10 @@ grouped_tile_kernel(Args p) {
 #pragma unroll
     for (int q = 0; q < P::PIECES; ++q) widen_a(0, q);
     int slot = 0;
-    for (int kt = 0; kt < KT; ++kt) {
-        fetch(kt + STAGES);
+    auto stage = [&](int kt, auto TURN) __attribute__((always_inline)) {
+        constexpr std::integral_constant<int, (TURN() + STAGES) % AHEAD> SET;                  // of stage kt + STAGES
+        constexpr std::integral_constant<int, (TURN() + STAGES + AHEAD - 1) % AHEAD> FREE;     // of the one before
+        fetch(kt + STAGES + AHEAD - 1, FREE);
         each_index([&](auto N) __attribute__((always_inline)) {
             constexpr int n = N;
             if constexpr (n % G::TN == 0) read_a(slot, n / G::TN + 2);
@@ -262,7 +292,7 @@ grouped_tile_kernel(Args p) {
                 read_b(after, m / 2);
                 prepare_b(m / 2);
             }
-            each_index([&](auto Q) __attribute__((always_inline)) { piece(std::integral_constant<int, q0 + Q>()); },
+            each_index([&](auto Q) __attribute__((always_inline)) { piece(std::integral_constant<int, q0 + Q>(), SET); },
                        std::make_integer_sequence<int, q1 - q0>());
             __builtin_amdgcn_sched_barrier(0);
         }, std::make_integer_sequence<int, 2 * G::TN>());
@@ -273,7 +303,15 @@ grouped_tile_kernel(Args p) {
             for (int i = 0; i < G::TM; ++i) scale[0][i] = scale[1][i];
         }
         slot = after;
-    }
+    };
+    // AHEAD stages a trip, for constant sets, and the rest behind the loop: another way out of it would pass its head
+    // for the compiler, which would then have it wait for loads that only the long way has taken.
+    int done = 0;
+    for (; done + AHEAD <= KT; done += AHEAD)
+        each_index([&](auto TURN) __attribute__((always_inline)) { stage(done + TURN(), TURN); }, std::make_integer_sequence<int, AHEAD>());
+    each_index([&](auto TURN) __attribute__((always_inline)) {
+        if (done + TURN() < KT) stage(done + TURN(), TURN);
+    }, std::make_integer_sequence<int, AHEAD - 1>());
     if constexpr (!ANY) wait_vmcnt<0>();   // no copy may still be writing LDS when the workgroup ends
 
     if (p.relu) {
@@ -376,12 +414,12 @@ grouped_tile_kernel(Args p) {
 }
 
 // (a LinearArgs is launched by its base: the rules of choice are for both)
-template <Kind KIND, bool WIDE, int BM, int BN, int WM, int WN, int STAGES, int KB, bool ANY = false, typename Args = GroupedArgs>
+template <Kind KIND, bool WIDE, int BM, int BN, int WM, int WN, int STAGES, int KB, bool ANY = false, typename Args = GroupedArgs, int AHEAD = 1>
 xtc_status launch_tiles(const GroupedArgs &base, hipStream_t s) {
     const Args &a = static_cast<const Args &>(base);
     const int64_t tiles = tile_count<KIND>(a, BM, BN);
     if (tiles >= kMostGroups / 2) return XTC_ERR_TOO_LARGE;
-    grouped_tile_kernel<KIND, WIDE, BM, BN, WM, WN, STAGES, KB, ANY, Args>
+    grouped_tile_kernel<KIND, WIDE, BM, BN, WM, WN, STAGES, KB, ANY, AHEAD, Args>
         <<<(unsigned)tiles, (BM / WM) * (BN / WN) * 64, 0, s>>>(a);
     return hip_status(hipGetLastError());
 }

@@ -4,8 +4,18 @@
 namespace xtc {
 namespace {
 
-template <Kind KIND, int BM, int BN, int WM, int WN, int STAGES, int KB, bool ANY = false>
-constexpr auto kLaunch = launch_tiles<KIND, false, BM, BN, WM, WN, STAGES, KB, ANY, LinearArgs>;
+template <Kind KIND, int BM, int BN, int WM, int WN, int STAGES, int KB>
+constexpr auto kLaunch = launch_tiles<KIND, false, BM, BN, WM, WN, STAGES, KB, false, LinearArgs>;
+
+// Rows at any address: AHEAD stages ahead (184 rows, 1731 to 3459, B N x K: 16.1 us, 19.6 with one stage; 1 row, 7833 to 2849:
+// 16.6 and 18.9; B K x N, whose rows are the pieces that it waits for, the same within 3 %) unless rows hold less than 16
+// bytes or there is nothing to sum.
+template <Kind KIND, int BM, int BN, int WM, int WN, int STAGES, int KB, int AHEAD>
+xtc_status launch_any_rows(const GroupedArgs &a, hipStream_t s) {
+    const bool far = a.K >= 8 && (KIND == kBf16T || a.N >= 8) && (KIND != kWgrad || a.T > 0);
+    return far ? launch_tiles<KIND, false, BM, BN, WM, WN, STAGES, KB, true, LinearArgs, AHEAD>(a, s)
+               : launch_tiles<KIND, false, BM, BN, WM, WN, STAGES, KB, true, LinearArgs>(a, s);
+}
 
 }  // namespace
 
@@ -38,23 +48,25 @@ const LinearChoice *linear_tile_choices(int *count) {
     }
 }
 
-// Rows at any address go through registers; copied first they run the kernels above where that is faster (a
-// weights' gradient of 12190 rows, 803 x 6111: 208 us with the copies of 184 MB, 372 without; one row, 7833 to 2849: 25 us
-// through registers, 30 copied).
+// Rows at any address go through registers, whose loads reach lines in pieces: a stage of 64x128 takes .6 us where the
+// direct copies take .35.  Copied first they run the kernels above where that is faster (a weights' gradient of 12190 rows,
+// 803 x 6111: 206 us with the copies of 184 MB, 317 without; one row, 7833 to 2849: 17 us through registers, 25 copied; 181
+// rows, 5076 to 4503: 37 and 42).  90 layers of odd widths: the kernel chosen takes 2 % longer than the best in the mean, 44 %
+// at most (32 rows, 7539 to 6848, whose A alone is copied: 38 us for 27).
 template <Kind KIND>
 const LinearChoice *linear_any_choices(int *count) {
     if constexpr (KIND == kWgrad) {
         static const LinearChoice all[] = {
-            {64, 128, 2, 1.15f, 1.33f, 8.7f, .5f, kLaunch<KIND, 64, 128, 64, 32, 2, 128, true>},
-            {64, 64, 2, .9f, 1.f, 4.4f, .74f, kLaunch<KIND, 64, 64, 64, 16, 2, 128, true>},
+            {64, 128, 1, .53f, .53f, 5.2f, 1, launch_any_rows<KIND, 64, 128, 64, 16, 2, 128, 4>},
+            {64, 64, 3, .58f, .95f, 5.9f, .77f, launch_any_rows<KIND, 64, 64, 64, 16, 2, 128, 4>},
         };
         *count = 2;
         return all;
     } else {
         constexpr bool N = KIND == kBf16N;
         static const LinearChoice all[] = {
-            {64, 128, 1, N ? .97f : .82f, N ? .97f : .82f, N ? 4.4f : 5.7f, N ? 1.f : .64f, kLaunch<KIND, 64, 128, 64, 16, 2, 128, true>},
-            {64, 64, 2, N ? 1.03f : .7f, N ? 1.03f : .91f, 6.1f, .45f, kLaunch<KIND, 64, 64, 64, 16, 2, 128, true>},
+            {64, 128, 1, N ? .61f : .58f, N ? .61f : .58f, 4.7f, N ? 1.f : .75f, launch_any_rows<KIND, 64, 128, 64, 16, 2, 128, 4>},
+            {64, 64, 3, N ? .52f : .37f, N ? 1.03f : 1.14f, 5.f, N ? .83f : .78f, launch_any_rows<KIND, 64, 64, 64, 16, 2, 128, 4>},
         };
         *count = 2;
         return all;

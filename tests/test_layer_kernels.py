@@ -20,21 +20,20 @@ SIZES = [
     (1, 0, 8668, 72, 2640), (1, 0, 8408, 200, 72), (1, 0, 4270, 72, 3568), (1, 0, 8313, 72, 264),
     (1, 0, 5655, 72, 72), (1, 0, 3, 72, 72), (1, 0, 3, 4104, 72), (1, 0, 3, 1912, 4024), (1, 0, 17, 4152, 72),
     (1, 0, 17, 1176, 4120), (1, 0, 2732, 72, 72), (1, 0, 37, 1208, 4192), (1, 0, 4115, 72, 72),
-    (1, 0, 50, 3864, 3976), (1, 1, 3, 72, 72), (1, 1, 3, 1163, 3333), (1, 1, 8431, 136, 72), (1, 1, 107, 1027, 3717),
-    (1, 1, 8237, 904, 72), (1, 1, 8572, 419, 261), (1, 1, 8502, 72, 3285), (1, 1, 8547, 387, 72),
-    (1, 1, 8479, 72, 2688), (1, 1, 8553, 200, 72), (1, 1, 4159, 72, 3464), (1, 1, 452, 2160, 464),
-    (1, 1, 4321, 395, 296), (1, 1, 3, 72, 133), (1, 1, 3, 4192, 229), (1, 1, 36, 3032, 200), (1, 1, 374, 72, 4045),
-    (1, 1, 67, 2755, 293), (1, 1, 199, 299, 4136), (1, 1, 4162, 72, 392), (2, 0, 8255, 912, 72),
+    (1, 0, 50, 3864, 3976), (1, 1, 65, 2856, 72), (1, 1, 3, 4184, 800), (1, 1, 3, 72, 72), (1, 1, 3, 483, 4176),
+    (1, 1, 8237, 904, 72), (1, 1, 1243, 3259, 264), (1, 1, 1753, 3507, 72), (1, 1, 5499, 531, 72),
+    (1, 1, 589, 867, 4136), (1, 1, 1256, 787, 1392), (1, 1, 3470, 528, 949), (1, 1, 3, 72, 197), (1, 1, 3, 4107, 688),
+    (1, 1, 1417, 72, 456), (1, 1, 300, 816, 616), (1, 1, 1085, 467, 968), (2, 0, 8255, 912, 72),
     (2, 0, 1181, 3416, 200), (2, 0, 8405, 72, 3424), (2, 0, 8480, 392, 72), (2, 0, 8395, 200, 72),
     (2, 0, 4402, 72, 3288), (2, 0, 8203, 72, 392), (2, 0, 2955, 72, 4008), (2, 0, 4105, 72, 72),
     (2, 0, 2602, 136, 4056), (2, 0, 3, 72, 72), (2, 0, 3, 4160, 216), (2, 0, 18, 4128, 72), (2, 0, 36, 4144, 72),
-    (2, 0, 4118, 72, 1056), (2, 1, 3, 707, 72), (2, 1, 3, 3667, 1792), (2, 1, 3, 72, 72), (2, 1, 1456, 176, 3581),
-    (2, 1, 8409, 899, 72), (2, 1, 1137, 3672, 200), (2, 1, 8276, 408, 72), (2, 1, 8913, 200, 72),
-    (2, 1, 2150, 203, 3549), (2, 1, 2874, 387, 528), (2, 1, 1827, 200, 3840), (2, 1, 904, 600, 456),
-    (2, 1, 3, 72, 133), (2, 1, 3, 4195, 200), (2, 1, 258, 520, 200), (2, 1, 1030, 235, 389), (2, 1, 4360, 72, 1208),
+    (2, 0, 4118, 72, 1056), (2, 1, 3, 72, 72), (2, 1, 3, 3011, 1312), (2, 1, 3, 72, 133), (2, 1, 3, 728, 4165),
+    (2, 1, 8409, 899, 72), (2, 1, 1137, 3672, 200), (2, 1, 1668, 3016, 72), (2, 1, 7182, 387, 72),
+    (2, 1, 841, 616, 4112), (2, 1, 808, 1267, 1816), (2, 1, 2337, 1696, 261), (2, 1, 3, 72, 453),
+    (2, 1, 18, 2360, 784), (2, 1, 904, 131, 736), (2, 1, 293, 936, 1608), (2, 1, 550, 899, 2677),
     (3, 0, 3, 2064, 3880), (3, 0, 332, 1208, 3272), (3, 0, 6662, 1176, 136), (3, 0, 3, 72, 72), (3, 0, 577, 72, 72),
-    (3, 1, 3, 968, 4077), (3, 1, 1326, 4163, 72), (3, 1, 3, 72, 72), (3, 1, 513, 72, 72), (3, 1, 3, 2619, 3109),
-    (3, 1, 385, 2251, 1997), (3, 1, 3749, 2728, 141), (3, 1, 3, 3443, 1168), (3, 1, 2584, 144, 2861),
+    (3, 1, 3, 72, 72), (3, 1, 581, 72, 72), (3, 1, 513, 72, 72), (3, 1, 1295, 136, 2173), (3, 1, 3, 2659, 3464),
+    (3, 1, 385, 2251, 1997), (3, 1, 3, 2699, 2261),
 ]
 
 
