@@ -200,29 +200,33 @@ xtc_status launch(const LinearArgs &given, void *workspace, int64_t bytes, hipSt
     return hip_status(hipGetLastError());
 }
 
-// dz = dy act'(z), and the column sums of a slab of rows: a wave takes 512 columns of a row at
-// a time, eight a lane, the workgroup's four waves rows in turn, kSlopeRows on their way together.  Bound by memory:
+// dz = dy act'(z), and the column sums of a slab of rows: LANES lanes take eight columns of a row each, the
+// workgroup's teams of LANES rows in turn, kSlopeRows on their way together.  Of many rows a team is a wave.  Bound by memory:
 // 8192 x 4096 bf16 (gelu_tanh) 37 to 40 us, 5 to 5.4 TB/s past the caches, and 4.5 for the join of 256 rows of sums (one row
 // at a time through the caches 47).  About 25 vector instructions an element, two of them at a quarter of the rate,
 // take half of that time beside the memory's.
-constexpr int kSlopeColumns = 512, kSlopeWaves = 4, kSlopeRows = 4;   // (rows on their way at once)
-template <typename TY, typename TZ>
-__global__ void __launch_bounds__(kSlopeWaves * 64) activation_backward_kernel(ActivationArgs p) {
-    __shared__ float sums[kSlopeWaves - 1][8][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int c = blockIdx.x * kSlopeColumns + lane * 8, valid = p.N - c;
+// Of few rows 32 teams of eight lanes share a workgroup that has them all, and whose sums are the result: one launch (64 x
+// 2816 bf16 5.0 us, 9.2 by two; 256 rows 7.2 and 8.3, 384 9.6 and 11.4 but of 512 columns 9.1 and 7.6).
+constexpr int kSlopeThreads = 256, kSlopeRows = 4;   // (rows on their way at once)
+constexpr int kSlopeMany = 64, kSlopeFew = 8, kFewRows = 256;
+template <typename TY, typename TZ, int LANES>
+__global__ void __launch_bounds__(kSlopeThreads) activation_backward_kernel(ActivationArgs p) {
+    constexpr int COLUMNS = LANES * 8, TEAMS = kSlopeThreads / LANES;
+    __shared__ __attribute__((aligned(16))) float sums[TEAMS][COLUMNS];
+    const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES;
+    const int c = blockIdx.x * COLUMNS + lane * 8, valid = p.N - c;
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     with_activation(p.act, [&](auto ACT) __attribute__((always_inline)) {
-        const int64_t step = (int64_t)gridDim.y * kSlopeWaves;
-        for (int64_t t = (int64_t)blockIdx.y * kSlopeWaves + wave; t < p.T; t += kSlopeRows * step) {
+        const int64_t step = (int64_t)gridDim.y * TEAMS;
+        for (int64_t t = (int64_t)blockIdx.y * TEAMS + team; t < p.T; t += kSlopeRows * step) {
             Raw8<TY> y[kSlopeRows];
             Raw8<TZ> z[kSlopeRows];
 #pragma unroll
             for (int r = 0; r < kSlopeRows; ++r) {
-                const int64_t at = t + r * step;
-                const int in = at < p.T ? valid : 0;
-                y[r] = raw8_once(static_cast<const TY *>(p.DY) + at * p.lddy + c, in);
-                z[r] = raw8_once(static_cast<const TZ *>(p.Z) + at * p.ldz + c, in);
+                // (past the last row that one again: loads in a branch would wait for it)
+                const int64_t at = t + r * step < p.T ? t + r * step : p.T - 1;
+                y[r] = raw8_once(static_cast<const TY *>(p.DY) + at * p.lddy + c, valid);
+                z[r] = raw8_once(static_cast<const TZ *>(p.Z) + at * p.ldz + c, valid);
             }
 #pragma unroll
             for (int r = 0; r < kSlopeRows; ++r) {
@@ -231,24 +235,22 @@ __global__ void __launch_bounds__(kSlopeWaves * 64) activation_backward_kernel(A
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     d[i] = y[r].at(i) * slope<ACT()>(z[r].at(i));
-                    sum[i] += d[i];
+                    sum[i] += at < p.T ? d[i] : 0.f;
                 }
                 store8_to(static_cast<Bf16 *>(p.DZ) + at * p.lddz + c, at < p.T ? valid : 0, d, p.past);
             }
         }
     });
     if (!p.DB) return;
-    if (wave > 0) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sums[wave - 1][i][lane] = sum[i];
-    }
+    __builtin_memcpy(__builtin_assume_aligned(&sums[team][lane * 8], 16), sum, sizeof(sum));
     __syncthreads();
-    if (wave > 0) return;
+    float *to = gridDim.y > 1 ? p.partial + (int64_t)blockIdx.y * p.N : p.DB;
+    for (int q = threadIdx.x; q < COLUMNS; q += kSlopeThreads) {
+        float s = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int w = 0; w < kSlopeWaves - 1; ++w) sum[i] += sums[w][i][lane];
-    store8(p.partial + (int64_t)blockIdx.y * p.N + c, valid, sum);
+        for (int w = 0; w < TEAMS; ++w) s += sums[w][q];
+        if ((int)blockIdx.x * COLUMNS + q < p.N) to[blockIdx.x * COLUMNS + q] = s;
+    }
 }
 
 }  // namespace
@@ -292,19 +294,30 @@ int linear_kernel(const LinearArgs &a, int kind, int *kernels, int *splits) {
 }
 
 int activation_slabs(int64_t T, int64_t N) {
-    const int64_t across = cdiv(N, kSlopeColumns), rows = cdiv(T, kSlopeWaves), most = across < 2048 ? 2048 / across : 1;
-    return (int)(rows < most ? (rows > 1 ? rows : 1) : most);
+    if (T <= kFewRows) return 1;
+    const int64_t across = cdiv(N, kSlopeMany * 8), rows = cdiv(T, kSlopeThreads / kSlopeMany), most = across < 2048 ? 2048 / across : 1;
+    return (int)(rows < most ? rows : most);
 }
+
+namespace {
+
+template <int LANES>
+auto slope_kernel(const ActivationArgs &a) {
+    return a.dy_f32 ? (a.z_f32 ? activation_backward_kernel<float, float, LANES> : activation_backward_kernel<float, Bf16, LANES>)
+                    : (a.z_f32 ? activation_backward_kernel<Bf16, float, LANES> : activation_backward_kernel<Bf16, Bf16, LANES>);
+}
+
+}  // namespace
 
 xtc_status launch_activation_backward(const ActivationArgs &given, hipStream_t s) {
     ActivationArgs a = given;
     a.past = whole_lines(a.DZ, a.lddz, 2);
     const int slabs = activation_slabs(a.T, a.N);
-    const auto kernel = a.dy_f32 ? (a.z_f32 ? activation_backward_kernel<float, float> : activation_backward_kernel<float, Bf16>)
-                                 : (a.z_f32 ? activation_backward_kernel<Bf16, float> : activation_backward_kernel<Bf16, Bf16>);
-    kernel<<<dim3((unsigned)cdiv(a.N, kSlopeColumns), (unsigned)slabs), kSlopeWaves * 64, 0, s>>>(a);
+    const bool few = a.T <= kFewRows;
+    const auto kernel = few ? slope_kernel<kSlopeFew>(a) : slope_kernel<kSlopeMany>(a);
+    kernel<<<dim3((unsigned)cdiv(a.N, few ? kSlopeFew * 8 : kSlopeMany * 8), (unsigned)slabs), kSlopeThreads, 0, s>>>(a);
     const xtc_status st = hip_status(hipGetLastError());
-    if (st != XTC_OK || !a.DB) return st;
+    if (st != XTC_OK || !a.DB || slabs == 1) return st;
     return launch_column_sums(a.partial, slabs, a.N, a.DB, nullptr, s);
 }
 

@@ -358,29 +358,25 @@ __global__ void __launch_bounds__(NT * TEAMS) norm_backward_kernel(NormBackwardA
 
 // Rows of more columns than registers hold: DX and DW by kernels of their own, which
 // read X and DY three times in all (4096 x 16384 bf16: 311 us, 1.7 TB/s of what one
-// pass would move, the layer norm's 330; 4096 x 8192 in one pass 64 us, 4.2 TB/s, both).
-template <typename T, bool CENTER>
+// pass would move; 4096 x 8192 in one pass 64 us, 4.2 TB/s, the layer norm's too).
+template <typename T>
 __global__ void __launch_bounds__(kThreads) norm_dx_kernel(NormBackwardArgs p) {
     __shared__ float scratch[kThreads / 64];
     const int tid = threadIdx.x, D = p.D;
     for (int64_t t = blockIdx.x; t < p.T; t += gridDim.x) {
         const T *x = static_cast<const T *>(p.X) + t * p.ldx;
         const T *dy = static_cast<const T *>(p.DY) + t * p.lddy;
-        const float rstd = p.rstd[t], centre = CENTER ? p.mean[t] : 0.f;
-        float sum = 0.f, sum_g = 0.f;
+        const float rstd = p.rstd[t];
+        float sum = 0.f;
         for (int c = tid * 8; c < D; c += kStep) {
             float h[8], g[8], w[8];
             load8(x + c, D - c, h);
             load8(dy + c, D - c, g);
             load_weight(p.W, p.w_f32, x, c, D - c, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                sum += (g[i] * w[i]) * ((CENTER ? (c + i < D ? h[i] - centre : 0.f) : h[i]) * rstd);
-                if constexpr (CENTER) sum_g += g[i] * w[i];
-            }
+            for (int i = 0; i < 8; ++i) sum += (g[i] * w[i]) * (h[i] * rstd);
         }
         const float mean = group_sum(sum, scratch) / (float)D;
-        const float mean_g = CENTER ? group_sum(sum_g, scratch) / (float)D : 0.f;
         for (int c = tid * 8; c < D; c += kStep) {
             float h[8], g[8], w[8], d[8];
             load8(x + c, D - c, h);
@@ -389,8 +385,7 @@ __global__ void __launch_bounds__(kThreads) norm_dx_kernel(NormBackwardArgs p) {
             if (p.DR) load8(static_cast<const T *>(p.DR) + t * p.lddr + c, D - c, d);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float v = CENTER ? rstd * (g[i] * w[i] - mean_g - (h[i] - centre) * rstd * mean)
-                                       : rstd * (g[i] * w[i] - h[i] * rstd * mean);
+                const float v = rstd * (g[i] * w[i] - h[i] * rstd * mean);
                 d[i] = p.DR ? d[i] + v : v;
             }
             store8(static_cast<T *>(p.DX) + t * p.lddx + c, D - c, d);
@@ -398,26 +393,145 @@ __global__ void __launch_bounds__(kThreads) norm_dx_kernel(NormBackwardArgs p) {
     }
 }
 
-// Sums of dy * xh (CENTER: and of dy) over the slab blockIdx.y of rows.
-template <typename T, bool CENTER>
+// A row of the layer norm's DX, held in registers between its sums and its outputs, NV groups of eight columns a thread; wider
+// rows (NV 0) are read twice.
+template <typename T, int NT, int NV>
+__device__ __forceinline__ void layernorm_dx_rows(const NormBackwardArgs &p, int64_t first, int64_t step, float (&both)[2][NT / 64]) {
+    constexpr int HELD = NV > 0 ? NV : 1;
+    const int tid = threadIdx.x, D = p.D;
+    for (int64_t t = first; t < p.T; t += step) {
+        const T *x = static_cast<const T *>(p.X) + t * p.ldx;
+        const T *dy = static_cast<const T *>(p.DY) + t * p.lddy;
+        const float rstd = p.rstd[t], centre = p.mean[t];
+        Raw8<T> rx[HELD], ry[HELD];
+        float sum = 0.f, sum_g = 0.f;
+        auto add = [&](int c, const Raw8<T> &a, const Raw8<T> &b) __attribute__((always_inline)) {
+            const Raw8<float> w = raw_weight(p.W, p.w_f32, x, c, D - c);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                // (past the end b and w are zeros; -centre * rstd, which may leave fp32, is none)
+                const float g = b.at(i) * w.v[i];
+                sum += g * (c + i < D ? (a.at(i) - centre) * rstd : 0.f);
+                sum_g += g;
+            }
+        };
+        if constexpr (NV > 0) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int c = (v * NT + tid) * 8;
+                rx[v] = raw8(x + c, D - c);
+                ry[v] = raw8(dy + c, D - c);
+            }
+#pragma unroll
+            for (int v = 0; v < NV; ++v) add((v * NT + tid) * 8, rx[v], ry[v]);
+        } else {
+            for (int c = tid * 8; c < D; c += NT * 8) add(c, raw8(x + c, D - c), raw8(dy + c, D - c));
+        }
+        sum = lanes_sum<64>(sum);
+        sum_g = lanes_sum<64>(sum_g);
+        __syncthreads();
+        if ((tid & 63) == 0) {
+            both[0][tid >> 6] = sum;
+            both[1][tid >> 6] = sum_g;
+        }
+        __syncthreads();
+        sum = sum_g = 0.f;
+#pragma unroll
+        for (int i = 0; i < NT / 64; ++i) {
+            sum += both[0][i];
+            sum_g += both[1][i];
+        }
+        const float mean = sum / (float)D, mean_g = sum_g / (float)D;
+        auto write = [&](int c, const Raw8<T> &a, const Raw8<T> &b) __attribute__((always_inline)) {
+            const Raw8<float> w = raw_weight(p.W, p.w_f32, x, c, D - c);
+            Raw8<T> r = {};
+            if (p.DR) r = raw8(static_cast<const T *>(p.DR) + t * p.lddr + c, D - c);
+            float o[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[i] = r.at(i) + rstd * (b.at(i) * w.v[i] - mean_g - (a.at(i) - centre) * rstd * mean);
+            store8_to(static_cast<T *>(p.DX) + t * p.lddx + c, D - c, o, p.past);
+        };
+        if constexpr (NV > 0) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) write((v * NT + tid) * 8, rx[v], ry[v]);
+        } else {
+            for (int c = tid * 8; c < D; c += NT * 8) write(c, raw8(x + c, D - c), raw8(dy + c, D - c));
+        }
+    }
+}
+
+// The layer norm's DW and DB take the rows' mean and rstd, but no sums of theirs: workgroups of 64 columns and a slab of rows
+// (eight lanes of eight columns, NT / 8 rows at once) leave them beside those of the rows.  X and DY are read twice (rows of
+// more than 16384 columns three times), but few rows take one launch, and no thread holds columns' sums over its rows.  64 x
+// 1152 bf16 4.4 us (in two launches 9.7); 4096 x 16384 227 us, 2.4 TB/s of what one pass would move (DX and DW one after the
+// other 330; one pass spills 160 registers of 1024 threads, 300 of 512).
+constexpr int kFewColumns = 64, kFewLanes = kFewColumns / 8;
+template <typename T, int NT, int NV>
+__global__ void __launch_bounds__(NT) norm_apart_backward_kernel(NormBackwardArgs p, int column_groups, int slabs) {
+    constexpr int TEAMS = NT / kFewLanes;
+    __shared__ __attribute__((aligned(16))) float sums[2][TEAMS][kFewColumns];
+    const int before = column_groups * slabs, id = (int)blockIdx.x;
+    if (id >= before) {
+        __shared__ float both[2][NT / 64];
+        layernorm_dx_rows<T, NT, NV>(p, id - before, (int)gridDim.x - before, both);
+        return;
+    }
+    const int lane = threadIdx.x % kFewLanes, team = threadIdx.x / kFewLanes, slab = id / column_groups;
+    const int64_t step = (int64_t)slabs * TEAMS;
+    for (int c0 = (id - slab * column_groups) * kFewColumns; c0 < p.D; c0 += column_groups * kFewColumns) {
+        const int c = c0 + lane * 8, valid = p.D - c;
+        float sum[2][8] = {};
+        constexpr int AT_ONCE = 4;
+        for (int64_t t = (int64_t)slab * TEAMS + team; t < p.T; t += AT_ONCE * step) {
+            Raw8<T> x[AT_ONCE], y[AT_ONCE];
+            float rstd[AT_ONCE], centre[AT_ONCE];
+#pragma unroll
+            for (int r = 0; r < AT_ONCE; ++r) {
+                // (past the last row that one again: loads in a branch would wait for it)
+                const int64_t at = t + r * step < p.T ? t + r * step : p.T - 1;
+                x[r] = raw8(static_cast<const T *>(p.X) + at * p.ldx + c, valid);
+                y[r] = raw8(static_cast<const T *>(p.DY) + at * p.lddy + c, valid);
+                rstd[r] = p.rstd[at];
+                centre[r] = p.mean[at];
+            }
+#pragma unroll
+            for (int r = 0; r < AT_ONCE; ++r)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const bool in = t + r * step < p.T;
+                    sum[0][i] += in ? y[r].at(i) * ((x[r].at(i) - centre[r]) * rstd[r]) : 0.f;
+                    sum[1][i] += in ? y[r].at(i) : 0.f;
+                }
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) __builtin_memcpy(__builtin_assume_aligned(&sums[k][team][lane * 8], 16), sum[k], sizeof(sum[k]));
+        __syncthreads();
+        if (threadIdx.x < 2 * kFewColumns) {
+            const int k = threadIdx.x / kFewColumns, q = threadIdx.x % kFewColumns, at = c0 + q;
+            float s = 0.f;
+#pragma unroll
+            for (int i = 0; i < TEAMS; ++i) s += sums[k][i][q];
+            if (at < p.D) (slabs > 1 ? p.partial + ((int64_t)slab * 2 + k) * p.D : k ? p.DB : p.DW)[at] = s;
+        }
+        __syncthreads();
+    }
+}
+
+// Sums of dy * xh over the slab blockIdx.y of rows.
+template <typename T>
 __global__ void __launch_bounds__(kThreads) norm_dw_kernel(NormBackwardArgs p) {
     const int c = (blockIdx.x * kThreads + threadIdx.x) * 8, valid = p.D - c;
     if (valid <= 0) return;
-    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0}, sum_y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     for (int64_t t = blockIdx.y; t < p.T; t += gridDim.y) {
         float h[8], g[8];
         load8(static_cast<const T *>(p.X) + t * p.ldx + c, valid, h);
         load8(static_cast<const T *>(p.DY) + t * p.lddy + c, valid, g);
-        const float rstd = p.rstd[t], centre = CENTER ? p.mean[t] : 0.f;
+        const float rstd = p.rstd[t];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            sum[i] += g[i] * ((CENTER ? h[i] - centre : h[i]) * rstd);
-            if constexpr (CENTER) sum_y[i] += g[i];
-        }
+        for (int i = 0; i < 8; ++i) sum[i] += g[i] * (h[i] * rstd);
     }
-    float *to = p.partial + (int64_t)blockIdx.y * p.D * (CENTER ? 2 : 1) + c;
-    store8(to, valid, sum);
-    if constexpr (CENTER) store8(to + p.D, valid, sum_y);
+    store8(p.partial + (int64_t)blockIdx.y * p.D + c, valid, sum);
 }
 
 // Column sums of the slabs: sixteen columns a workgroup, 64 runs of slabs, each
@@ -515,6 +629,14 @@ __global__ void __launch_bounds__(kThreads) quantize_blocks_kernel(QuantArgs p) 
     if (threadIdx.x == 0) p.S[mb * p.lds + b] = s;
 }
 
+// Whether the layer norm's gradient goes by norm_apart_backward_kernel, and its slabs of rows there: one and a single launch
+// up to kFewRows, and many rows of what registers hold with their sums as long as the caches have them when they are read
+// again (bf16, us, apart and not: 1024 x 4096 14.5 and 20.1, 2048 x 4096 20.5 and 25.3, 4096 x 4096 36.7 and 35.8; 1024 x 600
+// 11.3 and 9.6).
+constexpr int kFewRows = 256, kApartSlabs = 64;
+bool apart(int64_t T, int64_t D) { return D > 8192 || T <= kFewRows || (D > 1024 && T <= 2048); }
+int apart_slabs(int64_t T) { return (int)(T <= kFewRows ? 1 : T <= kFewRows * kApartSlabs ? (T + kFewRows - 1) / kFewRows : kApartSlabs); }
+
 unsigned grid_of(int64_t groups) { return (unsigned)(groups < 1 << 20 ? groups : 1 << 20); }
 
 // Calls f(threads, groups) with the threads that share a row of D columns and
@@ -560,6 +682,7 @@ bool with_backward_team(int64_t D, F &&f) {
 // (CENTER, of two sums a column: teams share a workgroup, whose sums are one row.)
 template <bool CENTER>
 static int backward_slabs(int64_t T, int64_t D) {
+    if (CENTER && apart(T, D)) return T > 0 ? apart_slabs(T) : 0;
     int64_t groups = T, most = 512;
     with_backward_team<CENTER>(D, [&](auto nt, auto nv, auto teams) {
         groups = (T + teams() - 1) / teams();
@@ -615,15 +738,30 @@ xtc_status launch_norm(const NormArgs &a, xtc_dtype dtype, bool quantize, hipStr
 template <bool CENTER>
 xtc_status launch_norm_backward(const NormBackwardArgs &a, xtc_dtype dtype, hipStream_t s) {
     const int slabs = backward_slabs<CENTER>(a.T, a.D);
-    if (a.T > 0) {
+    if (CENTER && a.T > 0 && apart(a.T, a.D)) {
+        const int64_t across = ((int64_t)a.D + kFewColumns - 1) / kFewColumns, groups = across < 1 << 16 ? across : 1 << 16;
+        const int64_t rows = a.T < 1 << 20 ? a.T : 1 << 20;
+        auto run = [&](auto nt, auto nv) {
+            const auto kernel = dtype == XTC_F32 ? norm_apart_backward_kernel<float, nt(), nv()> : norm_apart_backward_kernel<Bf16, nt(), nv()>;
+            kernel<<<(unsigned)(groups * slabs + rows), nt(), 0, s>>>(a, (int)groups, slabs);
+        };
+        typedef std::integral_constant<int, kThreads> Threads;
+        if (a.D <= kStep) run(Threads(), std::integral_constant<int, 1>());
+        else if (a.D <= 2 * kStep) run(Threads(), std::integral_constant<int, 2>());
+        else if (a.D <= 4 * kStep) run(Threads(), std::integral_constant<int, 4>());
+        else if (a.D <= 8 * kStep) run(std::integral_constant<int, 2 * kThreads>(), std::integral_constant<int, 4>());
+        else run(Threads(), std::integral_constant<int, 0>());
+        const xtc_status st = hip_status(hipGetLastError());
+        if (st != XTC_OK || slabs == 1) return st;
+    } else if (a.T > 0) {
         const bool done = with_backward_team<CENTER>(a.D, [&](auto nt, auto nv, auto teams) {
             constexpr int NT = nt(), NV = nv(), TEAMS = teams();
             const auto kernel = dtype == XTC_F32 ? norm_backward_kernel<float, CENTER, NT, NV, TEAMS> : norm_backward_kernel<Bf16, CENTER, NT, NV, TEAMS>;
             kernel<<<(unsigned)slabs, NT * TEAMS, 0, s>>>(a);
         });
-        if (!done) {
-            const auto dx = dtype == XTC_F32 ? norm_dx_kernel<float, CENTER> : norm_dx_kernel<Bf16, CENTER>;
-            const auto dw = dtype == XTC_F32 ? norm_dw_kernel<float, CENTER> : norm_dw_kernel<Bf16, CENTER>;
+        if constexpr (!CENTER) if (!done) {
+            const auto dx = dtype == XTC_F32 ? norm_dx_kernel<float> : norm_dx_kernel<Bf16>;
+            const auto dw = dtype == XTC_F32 ? norm_dw_kernel<float> : norm_dw_kernel<Bf16>;
             dx<<<grid_of(a.T), kThreads, 0, s>>>(a);
             dw<<<dim3((unsigned)(((int64_t)a.D + kStep - 1) / kStep), (unsigned)slabs), kThreads, 0, s>>>(a);
         }

@@ -166,7 +166,7 @@ def backward_reference(dy, xs, w, mean, rstd, dr):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("T,D", [(0, 64), (1, 1), (1, 4096), (3, 129), (600, 40), (1030, 257), (37, 2050), (513, 1024),
                                  (270, 5001), (9, 8192), (2, 20001), (9001, 40), (2501, 1100), (2301, 2100), (601, 5001),
-                                 (1201, 8200)])
+                                 (1201, 8200), (256, 2300), (2100, 4500), (300, 16500)])
 def test_layernorm_backward(T, D, dtype):
     for residual in (False, True):
         xs, w, _, _ = norm_case(T, D, dtype, False, 7 * D + T)
@@ -388,7 +388,7 @@ def test_linear_wgrad(T, N, K):
 
 
 @pytest.mark.parametrize("act", ACTS)
-@pytest.mark.parametrize("T,N", [(1, 1), (3, 7), (5, 512), (600, 130), (33, 1021), (2049, 520), (9000, 40)])
+@pytest.mark.parametrize("T,N", [(1, 1), (3, 7), (5, 512), (600, 130), (33, 1021), (256, 1100), (257, 1100), (2049, 520), (9000, 40)])
 def test_activation_backward(T, N, act):
     for dy_t, z_t in (("bf16", "bf16"), ("f32", "f32"), ("f32", "bf16")):
         dy, z = as_type(normal(T, T, N), dy_t), as_type(3 * normal(N, T, N), z_t)
