@@ -15,9 +15,8 @@
 // bits; the workgroups' counts go to memory, and a second kernel adds up those before its own.
 //
 // Bound by latency, not by its few bytes: one token over 64 experts 6.2 us in one launch (top times a chain of
-// maxima over the lanes); 16383 over 128 experts, top 8, 8.5 us for the choices, with a team for each token of a
-// workgroup (16 teams that took four in turn 12.8), and 10 us for the places, whose counts are read in one go (one load after
-// the other 14.6).
+// maxima over the lanes); 16383 over 128 experts, top 8, 17 us in two, a team for each token of a group (16 teams that took
+// four in turn 4 us more) and the counts read in one go (one load after the other 4 us more).
 #include <type_traits>
 
 #include "activation.h"
@@ -28,12 +27,12 @@ namespace xtc {
 namespace {
 
 constexpr int kThreads = 256, kManyThreads = 1024, kGroup = 64;   // tokens whose bits fill a word
+constexpr int kSmallGroup = 16;                                   // of few tokens, for more workgroups to have some
 
-// The value of the lane N places on, around the 16 (N 8, 4, 2, 1) or 64 (N 16, 32) that share a token.
+// The value of the lane N places on, around the 16 that share a token.
 template <int N>
 __device__ __forceinline__ unsigned rotated(unsigned v) {
-    if constexpr (N < 16) return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x120 + N, 0xF, 0xF, false);
-    else return (unsigned)__shfl_xor((int)v, N, 64);
+    return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x120 + N, 0xF, 0xF, false);
 }
 // f over the lanes, in all of them alike: each step joins halves that hold the same values.
 template <int LANES, typename V, typename F>
@@ -45,8 +44,13 @@ __device__ __forceinline__ V over_lanes(V v, F &&f) {
     v = step(rotated<2>(__builtin_bit_cast(unsigned, v)));
     v = step(rotated<1>(__builtin_bit_cast(unsigned, v)));
     if constexpr (LANES == 64) {
-        v = step(rotated<16>(__builtin_bit_cast(unsigned, v)));
-        v = step(rotated<32>(__builtin_bit_cast(unsigned, v)));
+        // the even rows of 16 lanes and the odd ones, each twice; then the halves
+        const unsigned u = __builtin_bit_cast(unsigned, v);
+        const auto rows = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+        v = f(__builtin_bit_cast(V, (unsigned)rows[0]), __builtin_bit_cast(V, (unsigned)rows[1]));
+        const unsigned w = __builtin_bit_cast(unsigned, v);
+        const auto halves = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+        v = f(__builtin_bit_cast(V, (unsigned)halves[0]), __builtin_bit_cast(V, (unsigned)halves[1]));
     }
     return v;
 }
@@ -104,9 +108,9 @@ __device__ __forceinline__ int fours(int E) { return (E + 3) & ~3; }
 
 // Tokens t0 .. t0 + p.each - 1: their experts and weights, their rows' places among the workgroup's, its counts
 // and sums of q.
-template <typename T, int LANES, int VPT, int THREADS, bool SMALL>
+template <typename T, int LANES, int VPT, int THREADS, int GROUP, bool SMALL>
 __device__ __forceinline__ void choose(const RouteArgs &p, const Halfway &h, int block, unsigned char *smem) {
-    constexpr int TEAMS = THREADS / LANES, EACH = kGroup / TEAMS, WAVES = THREADS / 64;
+    constexpr int TEAMS = THREADS / LANES, EACH = GROUP / TEAMS, WAVES = THREADS / 64;
     const int E = p.E, top = p.top, tid = threadIdx.x, team = tid / LANES, lane = tid % LANES, e0 = lane * VPT;
     unsigned long long *bits = reinterpret_cast<unsigned long long *>(smem);
     int *before = reinterpret_cast<int *>(bits + E);
@@ -116,7 +120,7 @@ __device__ __forceinline__ void choose(const RouteArgs &p, const Halfway &h, int
 #pragma unroll
     for (int i = 0; i < VPT; ++i) total[i] = 0.f;
     const int64_t first = (int64_t)block * p.each, end = first + p.each < p.T ? first + p.each : p.T;
-    for (int64_t t0 = first; t0 < end; t0 += kGroup) {
+    for (int64_t t0 = first; t0 < end; t0 += GROUP) {
         for (int e = tid; e < E; e += THREADS) bits[e] = 0;
         __syncthreads();
         int mine[EACH];              // lane j: the expert of choice j (-1: none)
@@ -211,6 +215,7 @@ __device__ __forceinline__ void choose(const RouteArgs &p, const Halfway &h, int
     }
 }
 
+constexpr int kMostTurns = 64;
 // What there is once (block == blocks), or the places of a workgroup's rows: those of all lower experts, of
 // this expert in the workgroups before, and the place among its own.
 template <int THREADS>
@@ -234,7 +239,9 @@ __device__ __forceinline__ void place(const RouteArgs &p, const Halfway &h, int 
     __syncthreads();
     // the workgroups' counts, four experts a load, the threads taking the workgroups in turn; whole numbers,
     // whose sums do not depend on the order
-    const int width = fours(E) / 4, turns = THREADS / width, g = tid % width, turn = tid / width;
+    // (kMostTurns of them at most: their sums of q are added one after the other)
+    const int width = fours(E) / 4, fit = THREADS / width < kMostTurns ? THREADS / width : kMostTurns;
+    const int turns = fit < blocks ? fit : blocks, g = tid % width, turn = tid / width;
     if (turn < turns) {
         int sum[4] = {0, 0, 0, 0}, mine[4] = {0, 0, 0, 0};
         float q[4] = {0.f, 0.f, 0.f, 0.f};
@@ -331,10 +338,10 @@ size_t place_bytes(int E, int threads) { return (size_t)E * 8 + (size_t)threads 
 
 __device__ __forceinline__ Halfway in_memory(const RouteArgs &p) { return Halfway{p.counts_of, p.sums_of, p.expert, p.row, 0}; }
 
-template <typename T, int LANES, int VPT>
-__global__ void __launch_bounds__(kManyThreads) route_choose_kernel(RouteArgs p) {
+template <typename T, int LANES, int VPT, int THREADS, int GROUP>
+__global__ void __launch_bounds__(THREADS) route_choose_kernel(RouteArgs p) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    choose<T, LANES, VPT, kManyThreads, false>(p, in_memory(p), blockIdx.x, smem);
+    choose<T, LANES, VPT, THREADS, GROUP, false>(p, in_memory(p), blockIdx.x, smem);
 }
 
 // (one workgroup more than route_choose_kernel's)
@@ -350,10 +357,10 @@ template <typename T, int LANES, int VPT>
 __global__ void __launch_bounds__(kThreads) route_small_kernel(RouteArgs p) {
     __shared__ __attribute__((aligned(16))) int32_t counts[LANES * VPT];
     __shared__ __attribute__((aligned(16))) float sums[LANES * VPT];
-    __shared__ int32_t expert[kGroup * kMostChoices], rank[kGroup * kMostChoices];
+    __shared__ int32_t expert[kSmallGroup * kMostChoices], rank[kSmallGroup * kMostChoices];
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const Halfway h = {counts, sums, expert, rank, 0};
-    choose<T, LANES, VPT, kThreads, true>(p, h, 0, smem);
+    choose<T, LANES, VPT, kThreads, kSmallGroup, true>(p, h, 0, smem);
     __syncthreads();
     place<kThreads>(p, h, 0, 1, true, true, smem);
 }
@@ -426,12 +433,20 @@ void with_lanes(int E, F &&f) {
     else if (E <= 64) f(Row(), std::integral_constant<int, 4>());
     else if (E <= 128) f(Row(), std::integral_constant<int, 8>());
     else if (E <= 256) f(Row(), std::integral_constant<int, 16>());
+    else if (E <= 512) f(std::integral_constant<int, 64>(), std::integral_constant<int, 8>());
     else f(std::integral_constant<int, 64>(), std::integral_constant<int, 16>());
 }
 
-constexpr int kMostBlocks = 256;
-// Tokens of a workgroup (whole groups), and the workgroups.
-int64_t each_of(int64_t T) { return ((T + kGroup - 1) / kGroup + kMostBlocks - 1) / kMostBlocks * kGroup; }
+// Tokens of a workgroup (whole groups), and the workgroups.  Every one of them reads the counts of all: 128 up to 128 tokens
+// each, 256 beyond (16384 tokens, 200 experts 24.7 us, with 256 27.5).  Groups of 16 as long as 128 workgroups hold the
+// tokens (1291 tokens, 200 experts 14.1 us, with groups of 64 17.7), and one of them is a single launch (64 tokens in one 21.7
+// us, by two 12.6).
+constexpr int kFewBlocks = 128, kManyBlocks = 256;
+int64_t each_of(int64_t T) {
+    if (T <= kFewBlocks * kSmallGroup) return kSmallGroup;
+    const int64_t most = T <= kFewBlocks * 2 * kGroup ? kFewBlocks : kManyBlocks;
+    return ((T + kGroup - 1) / kGroup + most - 1) / most * kGroup;
+}
 int blocks_of(int64_t T) { return T > 0 ? (int)((T + each_of(T) - 1) / each_of(T)) : 1; }
 
 }  // namespace
@@ -441,7 +456,7 @@ int64_t route_workspace(int64_t T, int64_t E) { return blocks_of(T) > 1 ? (int64
 xtc_status launch_route(const RouteArgs &given, xtc_dtype dtype, void *workspace, hipStream_t s) {
     RouteArgs a = given;
     const int blocks = blocks_of(a.T);
-    a.each = a.T > 0 ? (int)each_of(a.T) : kGroup;
+    a.each = (int)each_of(a.T);
     a.counts_of = static_cast<int32_t *>(workspace);
     a.sums_of = workspace ? reinterpret_cast<float *>(a.counts_of + (int64_t)blocks * ((a.E + 3) / 4 * 4)) : nullptr;
     with_lanes(a.E, [&](auto lanes, auto vpt) {
@@ -451,8 +466,13 @@ xtc_status launch_route(const RouteArgs &given, xtc_dtype dtype, void *workspace
             const auto kernel = dtype == XTC_F32 ? route_small_kernel<float, LANES, VPT> : route_small_kernel<Bf16, LANES, VPT>;
             kernel<<<1, kThreads, one > two ? one : two, s>>>(a);
         } else {
-            const auto kernel = dtype == XTC_F32 ? route_choose_kernel<float, LANES, VPT> : route_choose_kernel<Bf16, LANES, VPT>;
-            kernel<<<(unsigned)blocks, kManyThreads, choose_bytes(a.E, kManyThreads), s>>>(a);
+            auto run = [&](auto threads, auto group) {
+                constexpr int THREADS = threads(), GROUP = group();
+                const auto kernel = dtype == XTC_F32 ? route_choose_kernel<float, LANES, VPT, THREADS, GROUP> : route_choose_kernel<Bf16, LANES, VPT, THREADS, GROUP>;
+                kernel<<<(unsigned)blocks, THREADS, choose_bytes(a.E, THREADS), s>>>(a);
+            };
+            if (a.each == kSmallGroup) run(std::integral_constant<int, kThreads>(), std::integral_constant<int, kSmallGroup>());
+            else run(std::integral_constant<int, kManyThreads>(), std::integral_constant<int, kGroup>());
             route_place_kernel<<<(unsigned)blocks + 1, kManyThreads, place_bytes(a.E, kManyThreads), s>>>(a, blocks);
         }
     });

@@ -81,7 +81,8 @@ def check_routing(r, scores, top, mask, what):
 
 
 SIZES = [(1, 1, 1), (1, 64, 8), (2, 7, 7), (5, 16, 2), (63, 8, 2), (64, 64, 6), (65, 33, 4), (130, 60, 6), (1000, 128, 8),
-         (257, 256, 8), (70, 200, 16), (3, 257, 8), (300, 1024, 16), (200, 600, 3), (4097, 16, 1)]
+         (257, 256, 8), (70, 200, 16), (3, 257, 8), (300, 1024, 16), (200, 600, 3), (4097, 16, 1), (16, 300, 4),
+         (17, 20, 2), (2100, 400, 4), (2049, 1000, 2), (9000, 40, 2), (16700, 12, 2)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
