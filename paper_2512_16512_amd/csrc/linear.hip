@@ -206,9 +206,9 @@ xtc_status launch(const LinearArgs &given, void *workspace, int64_t bytes, hipSt
 // at a time through the caches 47).  About 25 vector instructions an element, two of them at a quarter of the rate,
 // take half of that time beside the memory's.
 // Of few rows 32 teams of eight lanes share a workgroup that has them all, and whose sums are the result: one launch (64 x
-// 2816 bf16 5.0 us, 9.2 by two; 256 rows 7.2 and 8.3, 384 9.6 and 11.4 but of 512 columns 9.1 and 7.6).
+// 2816 bf16 5.0 us, 8.4 by two; 256 rows 8.0 and 8.4, in fp32 10.6 and 8.8).
 constexpr int kSlopeThreads = 256, kSlopeRows = 4;   // (rows on their way at once)
-constexpr int kSlopeMany = 64, kSlopeFew = 8, kFewRows = 256;
+constexpr int kSlopeMany = 64, kSlopeFew = 8, kFewRows = 128;
 template <typename TY, typename TZ, int LANES>
 __global__ void __launch_bounds__(kSlopeThreads) activation_backward_kernel(ActivationArgs p) {
     constexpr int COLUMNS = LANES * 8, TEAMS = kSlopeThreads / LANES;
@@ -295,7 +295,8 @@ int linear_kernel(const LinearArgs &a, int kind, int *kernels, int *splits) {
 
 int activation_slabs(int64_t T, int64_t N) {
     if (T <= kFewRows) return 1;
-    const int64_t across = cdiv(N, kSlopeMany * 8), rows = cdiv(T, kSlopeThreads / kSlopeMany), most = across < 2048 ? 2048 / across : 1;
+    // (a trip of kSlopeRows rows a team at least: 1024 x 4096 10.7 us, with one row a team 22)
+    const int64_t across = cdiv(N, kSlopeMany * 8), rows = cdiv(T, kSlopeThreads / kSlopeMany * kSlopeRows), most = across < 2048 ? 2048 / across : 1;
     return (int)(rows < most ? rows : most);
 }
 
