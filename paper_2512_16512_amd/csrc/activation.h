@@ -19,13 +19,34 @@ __device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f
 // 1 / (1 + e^-v)
 __device__ __forceinline__ float logistic(float v) { return __builtin_amdgcn_rcpf(1.f + exp_of(-v)); }
 
-constexpr float kSqrtHalf = 0.70710678f, kTanhScale = 1.59576912f, kTanhCube = 0.044715f;   // (2 sqrt(2/pi))
+constexpr float kTanhScale = 1.59576912f, kTanhCube = 0.044715f;   // (2 sqrt(2/pi))
+
+// Phi(v), and e^(-v^2 / 2) in `density`.  Left of zero it is that times t P(t), t = 1 / (1 + 0.35 |v|), right of zero 1 less
+// as much: no sum cancels on the left (1 + erf is 4 % off at -5 and zero from -6 on, where Phi is 1e-9).  P is of degree 8,
+// fitted for the least relative error up to |v| = 13.5, 2^-25; with the roundings Phi is within (1.5 v^2 + 16) 2^-24 of itself.
+// (gelu behind a product, 8192 x 4096 to 4096, 220 us, by erff 227, by erfcf 237; its derivative 48 us, 55 and 65.)
+__device__ __forceinline__ float normal_cdf(float v, float &density) {
+    const float t = __builtin_amdgcn_rcpf(1.f + 0.35f * __builtin_fabsf(v));
+    float p = __builtin_fmaf(t, -0.0291259643f, 0.143872693f);
+    p = __builtin_fmaf(t, p, -0.255505472f);
+    p = __builtin_fmaf(t, p, 0.158930287f);
+    p = __builtin_fmaf(t, p, -0.0229377821f);
+    p = __builtin_fmaf(t, p, 0.105433188f);
+    p = __builtin_fmaf(t, p, 0.119852379f);
+    p = __builtin_fmaf(t, p, 0.139859095f);
+    p = __builtin_fmaf(t, p, 0.139621571f);
+    density = exp_of(-0.5f * v * v);
+    const float left = density * (t * p);
+    return v > 0.f ? 1.f - left : left;
+}
 
 template <int ACT>
 __device__ __forceinline__ float activated(float v) {
     if constexpr (ACT == XTC_RELU) return v < 0.f ? 0.f : v;
-    else if constexpr (ACT == XTC_GELU) return 0.5f * v * (1.f + erff(v * kSqrtHalf));
-    else if constexpr (ACT == XTC_GELU_TANH) return v * logistic(kTanhScale * v * (1.f + kTanhCube * v * v));
+    else if constexpr (ACT == XTC_GELU) {
+        float density;
+        return v * normal_cdf(v, density);
+    } else if constexpr (ACT == XTC_GELU_TANH) return v * logistic(kTanhScale * v * (1.f + kTanhCube * v * v));
     else if constexpr (ACT == XTC_SILU) return v * logistic(v);
     else return v;
 }
@@ -36,9 +57,11 @@ template <int ACT>
 __device__ __forceinline__ float slope(float v) {
     if constexpr (ACT == XTC_RELU) return v > 0.f ? 1.f : v <= 0.f ? 0.f : v;      // (a NaN stays one)
     v = v > 100.f ? 100.f : v < -100.f ? -100.f : v;
-    if constexpr (ACT == XTC_GELU)
-        return 0.5f * (1.f + erff(v * kSqrtHalf)) + v * 0.39894228f * exp_of(-0.5f * v * v);
-    else if constexpr (ACT == XTC_GELU_TANH) {
+    if constexpr (ACT == XTC_GELU) {
+        float density;
+        const float cdf = normal_cdf(v, density);
+        return cdf + v * 0.39894228f * density;
+    } else if constexpr (ACT == XTC_GELU_TANH) {
         // q + v q (1 - q) u', u' = 2 sqrt(2/pi) (1 + 3 * 0.044715 v^2)
         const float s = kTanhCube * v * v, q = logistic(kTanhScale * v * (1.f + s));
         return q + v * q * (1.f - q) * kTanhScale * (1.f + 3.f * s);

@@ -207,10 +207,12 @@ xtc_status launch(const LinearArgs &given, void *workspace, int64_t bytes, hipSt
 // take half of that time beside the memory's.
 // Of few rows 32 teams of eight lanes share a workgroup that has them all, and whose sums are the result: one launch (64 x
 // 2816 bf16 5.0 us, 8.4 by two; 256 rows 8.0 and 8.4, in fp32 10.6 and 8.8).
+// Four waves a SIMD, whatever the registers would allow: with five their loads find fewer lines together (8192 x 4096 in bf16,
+// gelu_tanh, 43.0 us with four, 44.0 with five).
 constexpr int kSlopeThreads = 256, kSlopeRows = 4;   // (rows on their way at once)
 constexpr int kSlopeMany = 64, kSlopeFew = 8, kFewRows = 128;
 template <typename TY, typename TZ, int LANES>
-__global__ void __launch_bounds__(kSlopeThreads) activation_backward_kernel(ActivationArgs p) {
+__global__ void __launch_bounds__(kSlopeThreads) __attribute__((amdgpu_waves_per_eu(4, 4))) activation_backward_kernel(ActivationArgs p) {
     constexpr int COLUMNS = LANES * 8, TEAMS = kSlopeThreads / LANES;
     __shared__ __attribute__((aligned(16))) float sums[TEAMS][COLUMNS];
     const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES;
