@@ -457,8 +457,9 @@ xtc_status xtc_linear(int64_t T, int64_t N, int64_t K, const void *A, int64_t ld
                       void *workspace, int64_t workspace_bytes,
                       xtc_dtype dtype, xtc_dtype out_dtype, void *stream);
 
-/* Bytes of workspace; -1 for extents outside the limits.  Pure host function: of the
- * pointers and strides it takes the alignment (rows off 16 bytes may be copied first). */
+/* Bytes of workspace, 640 MiB at most; -1 for extents outside the limits.  Pure host function:
+ * of the pointers and strides it takes the alignment (rows off 16 bytes may be copied first,
+ * where the copies take 512 MiB at most; the sums of a divided reduction take the rest). */
 int64_t xtc_linear_workspace(int64_t T, int64_t N, int64_t K, const void *A, int64_t lda,
                              const void *B, int64_t ldb, int32_t transpose_b);
 

@@ -23,6 +23,9 @@ struct Plan {
 constexpr int kSplitStep = 128;      // parts of the reduction are whole stages of every kernel
 constexpr int kMostSplits = 16;
 constexpr double kJoinUs = 2.4, kJoinPartUs = .15;
+// Bytes of the copies, whatever they would save: a workspace must not grow with the operands (1000000 x 4095 to 4096 asked
+// for 8.2 GB).  Beyond it rows off 16 bytes run as they are, at half the rate (70000 x 4097 to 4096 4.3 ms, copied 2.2).
+constexpr int64_t kMostCopied = int64_t(512) << 20;
 
 int64_t padded(int64_t n) { return cdiv(n, 8) * 8; }
 int64_t room(int64_t bytes) { return cdiv(bytes, 256) * 256; }
@@ -60,6 +63,9 @@ Plan plan(const LinearArgs &a) {
     const double size_a = (double)a.T * a.K, size_b = (KIND == kWgrad ? (double)a.T : (double)a.K) * a.N, sums = (double)rows * a.N;
     const double memory = 2 + (size_a + size_b) * 2 / 5e6;
     const double copying = a_fits && b_fits ? 0 : copy_us((a_fits ? 0 : 2 * size_a) + (b_fits ? 0 : 2 * size_b));
+    const int64_t ld_a = padded(a.K), ld_b = KIND == kBf16T ? padded(a.K) : padded(a.N);
+    const int64_t a_bytes = a_fits ? 0 : room(a.T * ld_a * 2);
+    const int64_t b_bytes = b_fits ? 0 : room((KIND == kBf16T ? a.N : KIND == kWgrad ? a.T : a.K) * ld_b * 2);
     auto look = [&](const LinearChoice *c, int count, bool copies) {
         for (int i = 0; i < count; ++i, ++seen) {
             const uint32_t bm = (uint32_t)c[i].bm, bn = (uint32_t)c[i].bn;
@@ -78,10 +84,10 @@ Plan plan(const LinearArgs &a) {
                 w.splits = splits;
                 w.k_each = (int)each;
                 w.place = seen;
-                w.ld_a = padded(a.K);
-                w.ld_b = KIND == kBf16T ? padded(a.K) : padded(a.N);
-                if (copies && !a_fits) w.a_bytes = room(a.T * w.ld_a * 2);
-                if (copies && !b_fits) w.b_bytes = room((KIND == kBf16T ? a.N : KIND == kWgrad ? a.T : a.K) * w.ld_b * 2);
+                w.ld_a = ld_a;
+                w.ld_b = ld_b;
+                if (copies) w.a_bytes = a_bytes;
+                if (copies) w.b_bytes = b_bytes;
                 w.copy_a = w.a_bytes > 0;
                 w.copy_b = w.b_bytes > 0;
                 if (splits > 1) w.part_bytes = room(4 * (int64_t)splits * rows * a.N);
@@ -96,7 +102,7 @@ Plan plan(const LinearArgs &a) {
         look(any, count, false);
     }
     const int64_t most = (int64_t(1) << 31) / 257;
-    if ((a_fits || padded(a.K) * 2 < most) && (b_fits || padded(KIND == kBf16T ? a.K : a.N) * 2 < most)) {
+    if (a_bytes + b_bytes <= kMostCopied && (a_fits || ld_a * 2 < most) && (b_fits || ld_b * 2 < most)) {
         const LinearChoice *tiles = linear_tile_choices<KIND>(&count);
         look(tiles, count, true);
         if constexpr (KIND != kWgrad) {
