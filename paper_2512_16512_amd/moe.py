@@ -29,8 +29,10 @@ MOST_EXPERTS, MOST_CHOSEN = 1024, 16      # what route_experts takes
 
 
 def _fits(t):
-    """Whether the operators take a matrix of values as it is."""
-    return t.is_cuda and t.dtype in (torch.float32, torch.bfloat16) and (t.shape[1] <= 1 or t.stride(1) == 1)
+    """Whether the operators take a matrix of values as it is: rows of neighbouring values that do not overlap."""
+    rows, cols = t.shape
+    return (t.is_cuda and t.dtype in (torch.float32, torch.bfloat16) and (cols <= 1 or t.stride(1) == 1) and
+            (rows <= 1 or t.stride(0) >= max(cols, 1)))
 
 
 def routing(scores, top):
@@ -114,6 +116,7 @@ def train_step(x, residual, norm, router, w1, w2, dout, top=2, bias=None, balanc
     an expert for every token.  With any of these the result is a ``TrainStep``."""
     bf16 = torch.bfloat16
     dout = dout if _fits(dout) else dout.float().contiguous()
+    router = router if _fits(router) else router.contiguous()
     n = _normed(x, norm, bias, residual)
     scores = linear(n.out, router, transpose_b=True) if router.dtype == bf16 else n.out.float() @ router.float().t()
     r = routing(scores, top)
