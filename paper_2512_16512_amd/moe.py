@@ -35,26 +35,51 @@ def _fits(t):
             (rows <= 1 or t.stride(0) >= max(cols, 1)))
 
 
-def routing(scores, top):
-    """``route_experts``, or for more experts or choices than it takes the same from torch (without the loss)."""
-    T, E = scores.shape
-    if E <= MOST_EXPERTS and top <= MOST_CHOSEN and _fits(scores):
-        return route_experts(scores, top)
+def _watched(t):
+    """Whether torch follows what happens to ``t``, which the library's calls do not show it: for a gradient, a tangent, a
+    trace or a transformation."""
+    return ((t.requires_grad and torch.is_grad_enabled()) or type(t) not in (torch.Tensor, torch.nn.Parameter) or
+            torch.compiler.is_compiling() or torch.jit.is_tracing() or torch._C._len_torch_dispatch_stack() > 0 or
+            torch._C._functorch.is_functorch_wrapped_tensor(t) or
+            torch.autograd.forward_ad.unpack_dual(t).tangent is not None)
+
+
+def _takes(scores, top):
+    """Whether ``route_experts`` and its gradient take these scores."""
+    return scores.shape[1] <= MOST_EXPERTS and top <= MOST_CHOSEN and _fits(scores)
+
+
+def _sorted_choices(scores, top):
+    """By torch: each token's weights and experts [T, top], the places of these choices in the rows' order, and the rows'
+    ends."""
     p, chosen = torch.topk(scores.float(), top)
     p = torch.softmax(p, 1)
     expert, which = torch.sort(chosen.flatten(), stable=True)
     # (a count of each expert's rows would be a call that waits for the GPU)
-    ends = torch.searchsorted(expert, torch.arange(E, device=expert.device), right=True, out_int32=True)
-    row = torch.empty(T * top, dtype=torch.int32, device=expert.device)
-    row[which] = torch.arange(T * top, dtype=torch.int32, device=expert.device)
-    return Routing(chosen.int(), p, row.view(T, top), (which // top).int(), torch.diff(ends, prepend=ends.new_zeros(1)),
+    ends = torch.searchsorted(expert, torch.arange(scores.shape[1], device=expert.device), right=True, out_int32=True)
+    return p, chosen, which, ends
+
+
+def routing(scores, top):
+    """``route_experts``, or the same from torch (without the loss; of equal scores any comes first): for more experts or
+    choices than it takes, and where torch follows the scores, so that ``p`` carries their gradient."""
+    if not _watched(scores) and _takes(scores, top):
+        return route_experts(scores, top)
+    p, chosen, which, ends = _sorted_choices(scores, top)
+    row = torch.empty(which.shape[0], dtype=torch.int32, device=which.device)
+    row[which] = torch.arange(which.shape[0], dtype=torch.int32, device=which.device)
+    return Routing(chosen.int(), p, row.view(chosen.shape), (which // top).int(), torch.diff(ends, prepend=ends.new_zeros(1)),
                    ends, None)
 
 
 def route(scores, top):
     """The rows of a grouped product for each token's ``top`` experts: ``token`` (the token of each row, rows sorted
-    by expert), ``ends`` (int32, for the operators), ``p`` (its weight) and ``which`` (its place in [T, top])."""
-    r = routing(scores, top)
+    by expert), ``ends`` (int32, for the operators), ``p`` (its weight, with the gradient of scores that require one) and
+    ``which`` (its place in [T, top])."""
+    if _watched(scores) or not _takes(scores, top):
+        p, _, which, ends = _sorted_choices(scores, top)
+        return which // top, ends, p.flatten()[which], which
+    r = route_experts(scores, top)
     row = r.row.flatten().long()
     which = torch.empty_like(row)
     which[row] = torch.arange(row.shape[0], device=row.device)
@@ -110,25 +135,34 @@ def train_step(x, residual, norm, router, w1, w2, dout, top=2, bias=None, balanc
                activation="gelu_tanh"):
     """Forward and backward in bfloat16 for the output's gradient ``dout`` [T, D].
 
-    Returns (out, gradients of x (the residual's is the same), norm, w1, w2), the routing taken as given.  With
+    Returns (out, gradients of x (the residual's is the same), norm, w1, w2), the routing taken as given; of a router
+    that requires a gradient ``out`` carries it, through the weights of the chosen experts (by torch's products).  With
     ``bias`` [D] the norm is a layer norm; with the number ``balance`` the router is trained too, through the weights
-    of the chosen experts and ``balance`` times the balance loss; ``shared`` = (v1 [D, S], c1 [S], v2 [S, D], c2 [D]) is
-    an expert for every token.  With any of these the result is a ``TrainStep``."""
+    of the chosen experts and ``balance`` times the balance loss, its gradient a result like the others and ``out`` without
+    one; ``shared`` = (v1 [D, S], c1 [S], v2 [S, D], c2 [D]) is an expert for every token.  With any of these the result is a
+    ``TrainStep``."""
     bf16 = torch.bfloat16
     dout = dout if _fits(dout) else dout.float().contiguous()
+    router = router if balance is None else router.detach()
     router = router if _fits(router) else router.contiguous()
     n = _normed(x, norm, bias, residual)
-    scores = linear(n.out, router, transpose_b=True) if router.dtype == bf16 else n.out.float() @ router.float().t()
+    own = router.dtype == bf16 and not _watched(router)
+    scores = linear(n.out, router, transpose_b=True) if own else n.out.float() @ router.float().t()
     r = routing(scores, top)
+    followed = _watched(r.p)
     rows = n.out[r.token]
     h = matmul_grouped(rows, w1, r.ends, relu=True, dtype=bf16)
     y = matmul_grouped(h, w2, r.ends, dtype=bf16)
-    out = combine_experts(y, r.row, r.p)
+    if followed:
+        out = (y.float()[r.row.long()] * r.p[:, :, None]).sum(1)
+        r = r._replace(p=r.p.detach())
+    else:
+        out = combine_experts(y, r.row, r.p)
     dense = dshared = drouter = None
     if shared is not None:
         v1, c1, v2, c2 = shared
         dense, z = linear(n.out, v1, c1, activation=activation, keep=True, dtype=bf16)
-        out = linear(dense, v2, c2, residual=out)
+        out = out + linear(dense, v2, c2) if followed else linear(dense, v2, c2, residual=out)
 
     dy, dp = combine_experts_backward(dout, y, r.row, r.token, r.p)
     dw2 = matmul_grouped_wgrad(h, dy, r.ends)
