@@ -86,6 +86,34 @@ def route(scores, top):
     return r.token.long(), r.ends, r.p.flatten()[which], which
 
 
+def _balance(scores, counts, top):
+    """What the balance loss is made of, by torch: its factor, each token's softmax over all experts (zeros where all its
+    scores are -inf), and the experts' counts."""
+    T, E = scores.shape
+    v = scores.float()
+    q = torch.where(v.amax(1, keepdim=True) == -torch.inf, 0.0, torch.softmax(v, 1))
+    return E / (top * max(T, 1) ** 2), q, counts.float()
+
+
+def balance_loss(scores, r):
+    """The balance loss of the routing ``r`` of these scores, where ``routing`` left it out too."""
+    if r.loss is not None:
+        return r.loss
+    factor, q, c = _balance(scores, r.counts, r.p.shape[1])
+    return factor * (c * q.sum(0)).sum()
+
+
+def routing_backward(dp, scores, r, dloss, dtype):
+    """``route_experts_backward`` of the routing ``r``, or for more experts or choices than that takes the same from
+    torch."""
+    top = r.p.shape[1]
+    if _takes(scores, top):
+        return route_experts_backward(dp, scores, r.expert, r.p, r.counts, dloss, dtype=dtype)
+    factor, q, c = _balance(scores, r.counts, top)
+    ds = dloss * factor * q * (c - (q * c).sum(1, keepdim=True))
+    return ds.scatter_add(1, r.expert.long(), r.p * (dp - (r.p * dp).sum(1, keepdim=True))).to(dtype)
+
+
 def sum_experts(rows, which, T):
     """The sum of each token's rows, which go to the places ``which`` of [T, top]: in the order of its experts whatever
     the run (sums by atomics would give a token of three experts or more other bits from call to call)."""
@@ -171,7 +199,7 @@ def train_step(x, residual, norm, router, w1, w2, dout, top=2, bias=None, balanc
     dw1 = matmul_grouped_wgrad(rows, dh, r.ends)
     dn = combine_experts(matmul_grouped(dh, w1, r.ends, transpose_b=True), r.row)
     if balance is not None:
-        ds = route_experts_backward(dp, scores, r.expert, r.p, r.counts, float(balance), dtype=bf16)
+        ds = routing_backward(dp, scores, r, float(balance), bf16)
         drouter = linear_wgrad(ds, n.out)
         dn = linear(ds, router.to(bf16), residual=dn)
     if shared is not None:
@@ -187,7 +215,7 @@ def train_step(x, residual, norm, router, w1, w2, dout, top=2, bias=None, balanc
         dx, dnorm, dbias = layernorm_backward(dn, n.residual, norm, n.mean, n.rstd)
     if bias is None and balance is None and shared is None:
         return out, dx, dnorm, dw1, dw2
-    return TrainStep(out, dx, dnorm, dw1, dw2, dbias, drouter, dshared, r.loss)
+    return TrainStep(out, dx, dnorm, dw1, dw2, dbias, drouter, dshared, balance_loss(scores, r))
 
 
 def weights(E, D, F, device="cuda", seed=0):
