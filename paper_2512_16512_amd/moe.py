@@ -199,9 +199,14 @@ def train_step(x, residual, norm, router, w1, w2, dout, top=2, bias=None, balanc
     dw1 = matmul_grouped_wgrad(rows, dh, r.ends)
     dn = combine_experts(matmul_grouped(dh, w1, r.ends, transpose_b=True), r.row)
     if balance is not None:
-        ds = routing_backward(dp, scores, r, float(balance), bf16)
-        drouter = linear_wgrad(ds, n.out)
-        dn = linear(ds, router.to(bf16), residual=dn)
+        ds = routing_backward(dp, scores, r, float(balance), bf16 if own else torch.float32)
+        if own:
+            drouter = linear_wgrad(ds, n.out)
+            dn = linear(ds, router, residual=dn)
+        else:
+            # (as its scores, no router is rounded to bf16, nor what reaches it)
+            drouter = ds.t() @ n.out.float()
+            dn = torch.addmm(dn, ds, router.float())
     if shared is not None:
         d2, dc2 = activation_backward(dout, None, None)
         d1, dc1 = activation_backward(linear(d2, v2, transpose_b=True, dtype=bf16), z, activation)
