@@ -114,14 +114,6 @@ def routing_backward(dp, scores, r, dloss, dtype):
     return ds.scatter_add(1, r.expert.long(), r.p * (dp - (r.p * dp).sum(1, keepdim=True))).to(dtype)
 
 
-def sum_experts(rows, which, T):
-    """The sum of each token's rows, which go to the places ``which`` of [T, top]: in the order of its experts whatever
-    the run (sums by atomics would give a token of three experts or more other bits from call to call)."""
-    placed = torch.empty_like(rows)
-    placed[which] = rows
-    return placed.view(T, rows.shape[0] // max(T, 1), rows.shape[1]).sum(1)
-
-
 def quantize_family(w):
     """Matrices [E, N, K] as float8_e4m3fn with a scale per 128 x 128 block, laid out once."""
     q, s = zip(*(quantize_fp8(m, block_rows=128) for m in w))
