@@ -538,11 +538,11 @@ __global__ void __launch_bounds__(kThreads) norm_dw_kernel(NormBackwardArgs p) {
 // in its order, joined by halves (1024 rows of 2048 sums: 5 us, a few trips to
 // memory and as many barriers).
 constexpr int kJoinColumns = 16, kJoinThreads = 1024;
-__global__ void __launch_bounds__(kJoinThreads) column_sums_kernel(const float *partial, int slabs, int D, float *DW, float *DB) {
+__global__ void __launch_bounds__(kJoinThreads) column_sums_kernel(const float *partial, int slabs, int D, float *DW, float *DB, int64_t first) {
     __shared__ float s[kJoinThreads];
     const int run = threadIdx.x / kJoinColumns;
     // (with DB: 2D sums a slab)
-    const int64_t c = (int64_t)blockIdx.x * kJoinColumns + threadIdx.x % kJoinColumns, columns = DB ? 2 * (int64_t)D : D;
+    const int64_t c = first + (int64_t)blockIdx.x * kJoinColumns + threadIdx.x % kJoinColumns, columns = DB ? 2 * (int64_t)D : D;
     constexpr int RUNS = kJoinThreads / kJoinColumns;
     float sum = 0.f;
     if (c < columns) {
@@ -696,7 +696,12 @@ int layernorm_backward_slabs(int64_t T, int64_t D) { return backward_slabs<true>
 
 xtc_status launch_column_sums(const float *partial, int slabs, int D, float *DW, float *DB, hipStream_t s) {
     const int64_t columns = DB ? 2 * (int64_t)D : D;
-    column_sums_kernel<<<(unsigned)((columns + kJoinColumns - 1) / kJoinColumns), kJoinThreads, 0, s>>>(partial, slabs, D, DW, DB);
+    // (a launch has fewer than 2^32 threads)
+    constexpr int64_t kMost = (int64_t(1) << 31) / kJoinThreads * kJoinColumns;
+    for (int64_t first = 0; first < columns; first += kMost) {
+        const int64_t n = columns - first < kMost ? columns - first : kMost;
+        column_sums_kernel<<<(unsigned)((n + kJoinColumns - 1) / kJoinColumns), kJoinThreads, 0, s>>>(partial, slabs, D, DW, DB, first);
+    }
     return hip_status(hipGetLastError());
 }
 
