@@ -322,7 +322,8 @@ xtc_status launch_activation_backward(const ActivationArgs &given, hipStream_t s
     ActivationArgs a = given;
     a.past = whole_lines(a.DZ, a.lddz, 2);
     const int slabs = activation_slabs(a.T, a.N);
-    const bool few = a.T <= kFewRows;
+    // (64 columns a workgroup there: 2^30 of them would be 2^32 threads, which are no launch)
+    const bool few = a.T <= kFewRows && a.N <= 1 << 29;
     const auto kernel = few ? slope_kernel<kSlopeFew>(a) : slope_kernel<kSlopeMany>(a);
     kernel<<<dim3((unsigned)cdiv(a.N, few ? kSlopeFew * 8 : kSlopeMany * 8), (unsigned)slabs), kSlopeThreads, 0, s>>>(a);
     const xtc_status st = hip_status(hipGetLastError());

@@ -54,3 +54,12 @@ def test_gradients_of_no_rows():
         say("no rows", f.__name__)
         for g in f(none, none, w, *stats)[1:]:
             assert g.shape == (D,) and not bool(g.any())
+
+
+def test_activation_gradient():
+    N = 2 ** 30                                # the widest row there may be
+    z, dy = filled(1, N, 3), filled(1, N, 4)
+    say("activation_backward", N)
+    dz, db = x.activation_backward(dy, z, "relu")
+    want = dy.float() * (z > 0)
+    assert torch.equal(db, want[0]) and torch.equal(dz, want.bfloat16())
