@@ -63,7 +63,11 @@ def _sorted_choices(scores, top):
 def routing(scores, top):
     """``route_experts``, or the same from torch (without the loss; of equal scores any comes first): for more experts or
     choices than it takes, and where torch follows the scores, so that ``p`` carries their gradient."""
-    if not _watched(scores) and _takes(scores, top):
+    return _routing(scores, top, _watched(scores))
+
+
+def _routing(scores, top, followed):
+    if not followed and _takes(scores, top):
         return route_experts(scores, top)
     p, chosen, which, ends = _sorted_choices(scores, top)
     row = torch.empty(which.shape[0], dtype=torch.int32, device=which.device)
@@ -139,7 +143,7 @@ class Served:
     def step(self, x, residual):
         """(out [T, D] float32, the sum that was normed): any number of tokens, one among them."""
         n = _normed(x, self.norm, self.bias, residual, quantize=True)
-        r = routing(matmul_fp8(n.out, n.scale, *self.router), self.top)
+        r = _routing(matmul_fp8(n.out, n.scale, *self.router), self.top, False)
         rows = n.out.view(torch.uint8)[r.token].view(torch.float8_e4m3fn)
         h = matmul_grouped_fp8(rows, n.scale[r.token], *self.w1, r.ends, relu=True, dtype=torch.bfloat16)
         y = matmul_grouped_fp8(*quantize_fp8(h), *self.w2, r.ends, dtype=torch.bfloat16)
@@ -166,10 +170,10 @@ def train_step(x, residual, norm, router, w1, w2, dout, top=2, bias=None, balanc
     router = router if balance is None else router.detach()
     router = router if _fits(router) else router.contiguous()
     n = _normed(x, norm, bias, residual)
-    own = router.dtype == bf16 and not _watched(router)
+    followed = _watched(router)
+    own = router.dtype == bf16 and not followed
     scores = linear(n.out, router, transpose_b=True) if own else n.out.float() @ router.float().t()
-    r = routing(scores, top)
-    followed = _watched(r.p)
+    r = _routing(scores, top, followed)
     rows = n.out[r.token]
     h = matmul_grouped(rows, w1, r.ends, relu=True, dtype=bf16)
     y = matmul_grouped(h, w2, r.ends, dtype=bf16)
