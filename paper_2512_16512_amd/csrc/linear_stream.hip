@@ -11,8 +11,8 @@ constexpr auto kLaunch = launch_streams<KIND, false, BM, BN, NW, STAGES, LinearA
 
 template <Kind KIND>
 const LinearChoice *linear_stream_choices(int *count) {
-    // B that is K x N is read in pieces of 32 bytes by strips of 16 columns, 64 by 32 (1 x 4096 to 4096: 11.4 us,
-    // the other layout's whole lines 8.0).
+    // B that is K x N is read in pieces of 32 bytes by strips of 16 columns, 64 by 32 (1 x 4096 to 4096: 11.2 us,
+    // the other layout's whole lines 7.8).
     constexpr bool N = KIND == kBf16N;
     static const LinearChoice all[] = {
         {16, 16, 2, N ? .128f : .045f, N ? .225f : .112f, N ? 3.f : 3.3f, N ? .41f : .8f, kLaunch<KIND, 16, 16, 4, 4>},

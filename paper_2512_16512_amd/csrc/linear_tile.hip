@@ -21,8 +21,9 @@ xtc_status launch_any_rows(const GroupedArgs &a, hipStream_t s) {
 
 // Measured, these and those of linear_stream.hip, on 145 layers of 1 to 16384 rows and widths of 512 to 8192, each
 // kernel with 1 to 16 splits: the kernel chosen by the estimate takes 1.5 % longer than the best of all in the mean,
-// 30 % at most (2 rows, 4608 to 576: 9.0 us for 6.9).  8192 x 4096 to 4096 216 us (tiles of 256x256, 1275 TFLOP/s; those
-// of 128x128 263), 1531 x 4096 to 2000 35 us (128x128 in two splits; 56 with the choices of the grouped products).
+// 30 % at most (2 rows, 4608 to 576: 9.0 us for 6.9).  8192 x 4096 to 4096 with gelu_tanh 210 us, z kept too 223 (tiles of
+// 256x256; those of 128x128 a fifth longer), 1531 x 4096 to 2000 36 us (B N x K, 128x128 with four stages, the reduction
+// whole; 56 with the choices of the grouped products).
 template <Kind KIND>
 const LinearChoice *linear_tile_choices(int *count) {
     if constexpr (KIND == kWgrad) {

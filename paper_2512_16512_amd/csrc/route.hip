@@ -14,7 +14,7 @@
 // tokens each expert has a word of 64 bits, one a token, so that a row's place among them is a count of
 // bits; the workgroups' counts go to memory, and a second kernel adds up those before its own.
 //
-// Bound by latency, not by its few bytes: one token over 64 experts 6.2 us in one launch (top times a chain of
+// Bound by latency, not by its few bytes: one token over 64 experts 5.8 us in one launch (top times a chain of
 // maxima over the lanes); 16383 over 128 experts, top 8, 17 us in two, a team for each token of a group (16 teams that took
 // four in turn 4 us more) and the counts read in one go (one load after the other 4 us more).
 #include <type_traits>
@@ -149,14 +149,13 @@ __device__ __forceinline__ void choose(const RouteArgs &p, const Halfway &h, int
                     int e;
                     if constexpr (sizeof(T) == 2) {
                         // 16 bits hold a score, the others its expert, the lowest one the largest: no two are equal, and one
-                        // maximum finds both (with the choices fetched early by place(): 16383 tokens 18.0 us, 18.4 before)
+                        // maximum finds both
                         e = 0xFFFF - (int)(best & 0xFFFFu);
 #pragma unroll
                         for (int i = 0; i < VPT; ++i) key[i] = key[i] == best ? 0u : key[i];
                         best = best >> 31 ? best & 0xFFFF0000u : best | 0xFFFFu;
                     } else {
-                        // (by the votes of the lanes and a permutation, which takes longer than the lanes' minimum, 6.6 us for one
-                        // token where this is 6.4)
+                        // (the lanes' minimum: their votes and a permutation take 0.2 us longer for one token's eight choices)
                         e = 0x7FFFFFFF;
 #pragma unroll
                         for (int i = VPT - 1; i >= 0; --i) e = key[i] == best ? e0 + i : e;
@@ -365,7 +364,7 @@ __global__ void __launch_bounds__(kThreads) route_small_kernel(RouteArgs p) {
     place<kThreads>(p, h, 0, 1, true, true, smem);
 }
 
-// ds of the tokens blockIdx.x, + gridDim.x, ... of each team.  16384 x 64 fp32, top 6: 5.3 us with the launch, of which
+// ds of the tokens blockIdx.x, + gridDim.x, ... of each team.  16384 x 64 fp32, top 6: 4.8 us with the launch, of which
 // its 9.6 MB are 1.8.
 template <typename T, typename O, int LANES, int VPT>
 __global__ void __launch_bounds__(kThreads) route_backward_kernel(RouteBackwardArgs p) {
@@ -439,8 +438,8 @@ void with_lanes(int E, F &&f) {
 
 // Tokens of a workgroup (whole groups), and the workgroups.  Every one of them reads the counts of all: 128 up to 128 tokens
 // each, 256 beyond (16384 tokens, 200 experts 24.7 us, with 256 27.5).  Groups of 16 as long as 128 workgroups hold the
-// tokens (1291 tokens, 200 experts 14.1 us, with groups of 64 17.7), and one of them is a single launch (64 tokens in one 21.7
-// us, by two 12.6).
+// tokens (1291 tokens, 200 experts 14.1 us, with groups of 64 17.7), and one of them is a single launch (64 tokens in one
+// launch 9 us longer than in two, 9.4).
 constexpr int kFewBlocks = 128, kManyBlocks = 256;
 int64_t each_of(int64_t T) {
     if (T <= kFewBlocks * kSmallGroup) return kSmallGroup;
