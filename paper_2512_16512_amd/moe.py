@@ -38,7 +38,7 @@ def _fits(t):
 def _watched(t):
     """Whether torch follows what happens to ``t``, which the library's calls do not show it: for a gradient, a tangent, a
     trace or a transformation."""
-    return ((t.requires_grad and torch.is_grad_enabled()) or type(t) not in (torch.Tensor, torch.nn.Parameter) or
+    return (type(t) not in (torch.Tensor, torch.nn.Parameter) or (t.requires_grad and torch.is_grad_enabled()) or
             torch.compiler.is_compiling() or torch.jit.is_tracing() or torch._C._len_torch_dispatch_stack() > 0 or
             torch._C._functorch.is_functorch_wrapped_tensor(t) or
             torch.autograd.forward_ad.unpack_dual(t).tangent is not None)

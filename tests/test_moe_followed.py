@@ -53,6 +53,14 @@ def test_fake_scores_are_routed_as_shapes():
     assert r.expert.shape == r.row.shape == (8, 2) and r.counts.shape == (16,)
 
 
+def test_symbols_and_compiled_programs_on_the_cpu():
+    scores = scores_of(6, 9, torch.float32)
+    want = moe.route(scores, 2)
+    for name, f in (("symbols", torch.fx.symbolic_trace(lambda s: moe.route(s, 2))),
+                    ("compiled", torch.compile(lambda s: moe.route(s, 2), backend="eager", fullgraph=True))):
+        assert all(torch.equal(a, b) for a, b in zip(f(scores), want)), name
+
+
 def test_gradient_of_the_weights_on_the_cpu():
     scores = scores_of(5, 7, torch.float64).requires_grad_()
     p = moe.route(scores, 3)[2]
