@@ -102,7 +102,7 @@ Plan plan(const LinearArgs &a) {
         look(any, count, false);
     }
     const int64_t most = (int64_t(1) << 31) / 257;
-    if (a_bytes + b_bytes <= kMostCopied && (a_fits || ld_a * 2 < most) && (b_fits || ld_b * 2 < most)) {
+    if (a_bytes <= kMostCopied && b_bytes <= kMostCopied - a_bytes && (a_fits || ld_a * 2 < most) && (b_fits || ld_b * 2 < most)) {
         const LinearChoice *tiles = linear_tile_choices<KIND>(&count);
         look(tiles, count, true);
         if constexpr (KIND != kWgrad) {

@@ -18,7 +18,8 @@ def workspaces(T, N, K, off=0, pad=0):
 
 
 @pytest.mark.parametrize("T,N,K", [(600000, 1024, 4097), (1000000, 4096, 4095), (300000, 4096, 8193), (1 << 26, 8, 9),
-                                   (70000, 4096, 4097), (5, 300001, 8193), (4096, 4097, 300001), (0x7FFFFF00, 1, 1)])
+                                   (70000, 4096, 4097), (5, 300001, 8193), (4096, 4097, 300001), (0x7FFFFF00, 1, 1),
+                                   (0x7FFFFF00, 0x7FFFFF00, 0x7FFFFF00), (0x7FFFFEFF, 0x7FFFFEFF, 0x7FFFFEFF)])
 def test_large_operands_at_odd_widths(T, N, K):
     assert all(0 <= w <= MOST for w in workspaces(T, N, K))
 
